@@ -387,6 +387,86 @@ nq_status nq_maxpool_i8(const int8_t *d_x, int64_t B, int64_t H, int64_t W, int6
 nq_status nq_avgpool_i8(const int8_t *d_x, int64_t B, int64_t HW, int64_t C, float in_scale,
                         float inv_out_scale, int8_t *d_y, void *stream);
 
+/* ---- 8-bit floating point layers of a transformer (beyond the paper) ------------------------------------- *
+ * The activations of a transformer's layers have channels that stand out; one int8 step for the whole tensor
+ * (Sec. 4.2) loses the others.  These three calls run such a layer on e4m3 codes with one fp32 scale for each
+ * block of 128 columns: the quantiser, the matrix product, and what stands between two blocks of layers.
+ * e4m3: 1 sign, 4 exponent (bias 7) and 3 mantissa bits, largest value 448, no infinities, 0x7f / 0xff = NaN. */
+
+typedef enum { NQ_DT_F32 = 0, NQ_DT_F16 = 1, NQ_DT_BF16 = 2 } nq_dtype;
+
+/* A matrix of e4m3 codes [rows][cols], row r at byte r * ld.  The scale of the block that holds (r, c) is
+ * d_scale[(r / block_rows) * scale_row_step + (c / 128) * scale_col_step]; it stands for scale * code.
+ * block_rows: 1 (activations: a scale for each 1 x 128) or 128 (weights).  The last block of a row, and the last
+ * rows' blocks, may be cut off by the matrix's end.  The codes take rows * ld bytes of memory, of which those past
+ * a row's cols-th are never written and may hold anything.  Any alignment and any ld >= cols are right; d_q on 16
+ * bytes with ld a multiple of 16 is fast.  Steps are in floats and not negative; a row step of 1 (the scales of a
+ * column block beside each other) is the fast order for a matrix of many rows. */
+typedef struct {
+    uint8_t *d_q;            /* device, rows * ld bytes      */
+    int64_t rows, cols, ld;
+    float *d_scale;          /* device, 4-byte aligned       */
+    int64_t scale_row_step, scale_col_step;
+    int32_t block_rows;      /* 1 or 128                     */
+    int32_t reserved_;
+} nq_fp8;
+
+/* v = act(x) * mul (fp32; mul may be NULL), then codes and scales of v into q's memory.  For a block with the
+ * largest magnitude a:  scale = max(a / 448, 2^-126), or 1 where a is 0;  code = e4m3(v * (1 / scale)), rounded to
+ * nearest even (each of the two quotients and the product rounded to fp32).  A block that holds a NaN or an
+ * infinity gets a scale that is not finite, and so a product with it comes out as NaN.
+ * d_x, d_mul: device [q->rows][q->cols] of `dtype`, rows ldx and ldmul elements apart (the up and the gate half of one
+ * [rows][2 * cols] tensor, say), aligned to their type.  rows or cols of 0: no-op.
+ * GELU is x * Phi(x), GELU_TANH its tanh form, SILU x / (1 + exp(-x)).  NQ_ERR_SHAPE: cols > NQ_MAX_K, ld below
+ * cols. */
+typedef enum { NQ_ACT_NONE = 0, NQ_ACT_RELU = 1, NQ_ACT_SILU = 2, NQ_ACT_GELU = 3, NQ_ACT_GELU_TANH = 4 } nq_act;
+nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, const void *d_mul, int64_t ldmul, int act,
+                          const nq_fp8 *q, void *stream);
+
+/* Y[m][n] = sum_b sx[m][b] * sw[n / 128][b] * (sum over the columns k of block b of x[m][k] * w[n][k]) + bias[n],
+ * sums in fp32, rounded to `dtype` once.  x: block_rows 1; w: block_rows 128 (NQ_ERR_UNSUPPORTED otherwise);
+ * x->cols == w->cols <= NQ_MAX_K, w->rows <= 2^31 (NQ_ERR_SHAPE).  d_bias: device fp32[w->rows] or NULL.
+ * d_y: device [x->rows][w->rows] of `dtype`, rows ldy elements apart, aligned to its type.  From one row on: few
+ * rows stream the weights, many are tiled; each output is summed in an order that its matrix's sizes alone fix, so
+ * equal calls give equal bits.  No columns: Y = bias. */
+nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *d_bias, void *d_y, int dtype, int64_t ldy,
+                      void *stream);
+
+/* What stands between two blocks of layers: norm after the first, gate, residual sum, norm before the second.
+ *   p  = post(y);  h' = residual_scale * h + branch_scale * gate * p;  x = pre(h')
+ *   NONE: v.   RMS: v * w / sqrt(mean(v^2) + eps).   LAYER: (v - mean(v)) * w / sqrt(mean((v - mean(v))^2) + eps) + b.
+ * All of it in fp32, x from the h' that has not been rounded yet.  w and b: device fp32[D] or NULL (1 and 0).
+ * d_h [M][D] of h_dtype; d_y [M][D] of dtype, or NULL (no branch yet: h' = residual_scale * h);
+ * d_gate of dtype or NULL (1): row m takes row m / gate_rows of it (1: a gate for each row, M: one for all, the tokens
+ * of an image: a gate for each image).
+ * Out, each may be NULL: d_h_out [M][D] of h_dtype (may be d_h itself, with the same ld); d_x [M][D] of dtype; q: x as
+ * codes and 1 x 128 scales as nq_quantize_fp8 makes them (q->rows == M, q->cols == D, block_rows 1).
+ * h_dtype is dtype or fp32.  Leading dimensions in elements.  1 <= D <= NQ_NORM_MAX_D.  M == 0: no-op. */
+#define NQ_NORM_MAX_D 32768
+typedef enum { NQ_NORM_NONE = 0, NQ_NORM_RMS = 1, NQ_NORM_LAYER = 2 } nq_norm_kind;
+typedef struct {
+    int32_t kind;            /* nq_norm_kind */
+    float eps;
+    const float *d_weight, *d_bias;
+} nq_norm;
+typedef struct {
+    const void *d_h;
+    int64_t ldh;
+    const void *d_y;
+    int64_t ldy;
+    const void *d_gate;
+    int64_t ldgate, gate_rows;
+    int32_t h_dtype, dtype;
+    float residual_scale, branch_scale;
+    nq_norm post, pre;
+    void *d_h_out;
+    int64_t ldh_out;
+    void *d_x;
+    int64_t ldx;
+    const nq_fp8 *q;         /* host: read before the call returns */
+} nq_norm_job;
+nq_status nq_block_norm(const nq_norm_job *job, int64_t M, int64_t D, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

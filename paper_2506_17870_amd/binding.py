@@ -27,6 +27,10 @@ NQ_LOW_UNSIGNED_L, NQ_LOW_SIGNED_L1 = 0, 1
 NQ_LAYOUT_DENSE, NQ_LAYOUT_PAPER_U64 = 0, 1
 NQ_MAX_K = 65536
 NQ_TUNE_KERNEL, NQ_TUNE_BIG_TM, NQ_TUNE_GC_UNITS, NQ_TUNE_STAT_ROWS = 0, 1, 2, 3
+NQ_DT_F32, NQ_DT_F16, NQ_DT_BF16 = 0, 1, 2
+NQ_ACT_NONE, NQ_ACT_RELU, NQ_ACT_SILU, NQ_ACT_GELU, NQ_ACT_GELU_TANH = range(5)
+NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER = range(3)
+NQ_NORM_MAX_D = 32768
 
 EXPORTS = ["nq_version", "nq_status_string", "nq_packed_bytes", "nq_quantize", "nq_tensor_scale", "nq_quantize_tensor", "nq_quantize_decompose_pack",
            "nq_decompose", "nq_pack", "nq_decompose_pack", "nq_decompose_pack_batch",
@@ -34,7 +38,7 @@ EXPORTS = ["nq_version", "nq_status_string", "nq_packed_bytes", "nq_quantize", "
            "nq_weight_init_group", "nq_page_out_low_batch", "nq_page_in_low_batch",
            "nq_gemm_full", "nq_gemm_part", "nq_gemm_batch_workspace_bytes", "nq_gemm_batch", "nq_gemm_batch_static", "nq_conv_full", "nq_conv_part", "nq_gconv_full", "nq_gconv_part",
            "nq_set_tuning", "nq_profile_next_launch", "nq_profile_last_kernel", "nq_event_create", "nq_event_destroy",
-           "nq_event_elapsed_ms", "nq_maxpool_i8", "nq_avgpool_i8"]
+           "nq_event_elapsed_ms", "nq_maxpool_i8", "nq_avgpool_i8", "nq_quantize_fp8", "nq_gemm_fp8", "nq_block_norm"]
 
 
 class nq_cfg(ctypes.Structure):
@@ -76,6 +80,24 @@ class nq_conv_shape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int64), ("H", ctypes.c_int64), ("W", ctypes.c_int64), ("Cin", ctypes.c_int64),
                 ("Cout", ctypes.c_int64), ("KH", ctypes.c_int32), ("KW", ctypes.c_int32),
                 ("stride", ctypes.c_int32), ("pad", ctypes.c_int32)]
+
+
+class nq_fp8(ctypes.Structure):
+    _fields_ = [("d_q", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("d_scale", ctypes.c_void_p), ("scale_row_step", ctypes.c_int64), ("scale_col_step", ctypes.c_int64),
+                ("block_rows", ctypes.c_int32), ("reserved_", ctypes.c_int32)]
+
+
+class nq_norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("d_weight", ctypes.c_void_p), ("d_bias", ctypes.c_void_p)]
+
+
+class nq_norm_job(ctypes.Structure):
+    _fields_ = [("d_h", ctypes.c_void_p), ("ldh", ctypes.c_int64), ("d_y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+                ("d_gate", ctypes.c_void_p), ("ldgate", ctypes.c_int64), ("gate_rows", ctypes.c_int64),
+                ("h_dtype", ctypes.c_int32), ("dtype", ctypes.c_int32), ("residual_scale", ctypes.c_float),
+                ("branch_scale", ctypes.c_float), ("post", nq_norm), ("pre", nq_norm), ("d_h_out", ctypes.c_void_p),
+                ("ldh_out", ctypes.c_int64), ("d_x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("q", ctypes.POINTER(nq_fp8))]
 
 
 if not os.path.exists(LIB_PATH):
@@ -123,6 +145,9 @@ _SIGS = {
     "nq_event_elapsed_ms": (_int, [_vp, _vp, ctypes.POINTER(ctypes.c_float)]),
     "nq_maxpool_i8": (_int, [_vp, _i64, _i64, _i64, _i64, _int, _int, _int, _vp, _vp]),
     "nq_avgpool_i8": (_int, [_vp, _i64, _i64, _i64, _f, _f, _vp, _vp]),
+    "nq_quantize_fp8": (_int, [_vp, _int, _i64, _vp, _i64, _int, ctypes.POINTER(nq_fp8), _vp]),
+    "nq_gemm_fp8": (_int, [ctypes.POINTER(nq_fp8), ctypes.POINTER(nq_fp8), _vp, _vp, _int, _i64, _vp]),
+    "nq_block_norm": (_int, [ctypes.POINTER(nq_norm_job), _i64, _i64, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -155,6 +180,8 @@ _fast.setup(torch.Tensor, nq_weight, nq_epilogue, nq_conv_shape, nq_cfg,
             *[ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value
               for n in ("nq_gemm_part", "nq_gemm_full", "nq_conv_part", "nq_conv_full", "nq_gconv_part", "nq_gconv_full",
                         "nq_quantize_decompose_pack")])
+_fast.setup_fp8(nq_fp8, nq_norm_job, *[ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value
+                                       for n in ("nq_quantize_fp8", "nq_gemm_fp8", "nq_block_norm")])
 # a forked child has to go through torch's own initialisation (and its error) again
 os.register_at_fork(after_in_child=lambda: _fast.set_stream_ready(False))
 
@@ -165,6 +192,14 @@ def _ptr(t):
     if isinstance(t, int):
         return t
     assert t.is_contiguous(), "tensors handed to libnq must be contiguous"
+    return t.data_ptr()
+
+
+def _rows(t):
+    """The address of a matrix whose rows may lie apart (the call is told how far); the elements of a row may not."""
+    if t is None or isinstance(t, int):
+        return t
+    assert t.numel() == 0 or t.shape[-1] <= 1 or t.stride(-1) == 1, "the elements of a row must lie beside each other"
     return t.data_ptr()
 
 
@@ -426,6 +461,79 @@ def nq_maxpool_i8(d_x, B, H, W, C, ksize, stride, pad, d_y, stream=None):
 def nq_avgpool_i8(d_x, B, HW, C, in_scale, inv_out_scale, d_y, stream=None):
     _check(_lib.nq_avgpool_i8(_ptr(d_x), B, HW, C, in_scale, inv_out_scale, _ptr(d_y), _stream(stream)),
            "nq_avgpool_i8")
+
+
+def make_fp8(d_q, cols, d_scale, block_rows=1) -> nq_fp8:
+    """Descriptor of e4m3 codes: d_q [rows][>= cols] of one-byte elements, d_scale fp32 [blocks of rows][blocks of 128
+    columns], any two strides (e.g. the transpose of a [blocks of columns][rows] tensor).  It keeps both alive."""
+    rows = d_q.shape[0]
+    want = (-(-rows // block_rows) if block_rows > 0 else 0, -(-cols // 128))
+    if d_q.dim() != 2 or d_q.element_size() != 1 or cols > d_q.shape[1] or (d_q.numel() and d_q.stride(1) != 1 and cols > 1):
+        raise ValueError("d_q must be a matrix of one-byte elements, those of a row beside each other")
+    if d_scale.dtype != torch.float32 or tuple(d_scale.shape) != want:
+        raise ValueError(f"d_scale must be fp32 {want}, got {d_scale.dtype} {tuple(d_scale.shape)}")
+    # (of a matrix of one row torch may name any stride)
+    desc = nq_fp8(d_q.data_ptr(), rows, cols, d_q.stride(0) if rows > 1 else max(d_q.shape[1], cols), d_scale.data_ptr(),
+                  d_scale.stride(0) if want[0] > 1 else 1, d_scale.stride(1) if want[1] > 1 else 1, block_rows, 0)
+    desc._keep = (d_q, d_scale)
+    return desc
+
+
+def make_norm(kind=NQ_NORM_RMS, eps=1e-5, d_weight=None, d_bias=None) -> nq_norm:
+    """A norm over rows; d_weight and d_bias fp32[D] or None."""
+    norm = nq_norm(kind, eps, _ptr(d_weight), _ptr(d_bias))
+    norm._keep = (d_weight, d_bias)
+    return norm
+
+
+def make_block_norm(d_h, h_dtype, ldh, d_y, dtype, ldy, d_gate, ldgate, gate_rows, residual_scale, branch_scale, post: nq_norm,
+                    pre: nq_norm, d_h_out, ldh_out, d_x, ldx, q: nq_fp8 | None = None) -> nq_norm_job:
+    """Descriptor of one nq_block_norm call; None for what is not there.  It keeps everything it names alive."""
+    job = nq_norm_job(_rows(d_h), ldh, _rows(d_y), ldy, _rows(d_gate), ldgate, gate_rows, h_dtype, dtype, residual_scale, branch_scale,
+                      post, pre, _rows(d_h_out), ldh_out, _rows(d_x), ldx, ctypes.pointer(q) if q is not None else None)
+    job._keep = (d_h, d_y, d_gate, post, pre, d_h_out, d_x, q)
+    return job
+
+
+def nq_quantize_fp8(d_x, dtype, ldx, d_mul, ldmul, act, q: nq_fp8, stream=None):
+    st = _fast.quantize_fp8(d_x, dtype, ldx, d_mul, ldmul, act, q, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_quantize_fp8")
+    _check(_lib.nq_quantize_fp8(_rows(d_x), dtype, ldx, _rows(d_mul), ldmul, act, ctypes.byref(q), _stream(stream)), "nq_quantize_fp8")
+
+
+def nq_gemm_fp8(x: nq_fp8, w: nq_fp8, d_bias, d_y, dtype, ldy, stream=None):
+    st = _fast.gemm_fp8(x, w, d_bias, d_y, dtype, ldy, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_gemm_fp8")
+    _check(_lib.nq_gemm_fp8(ctypes.byref(x), ctypes.byref(w), _ptr(d_bias), _rows(d_y), dtype, ldy, _stream(stream)), "nq_gemm_fp8")
+
+
+def nq_block_norm(job: nq_norm_job, M, D, stream=None):
+    st = _fast.block_norm(job, M, D, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_block_norm")
+    _check(_lib.nq_block_norm(ctypes.byref(job), M, D, _stream(stream)), "nq_block_norm")
+
+
+class Fp8Matrix:
+    """Owner of the memory of one nq_fp8 descriptor (memory plumbing only): codes with rows on 16 bytes, and the scales of a
+    column block beside each other, the order the matrix product reads fastest."""
+
+    def __init__(self, rows, cols, block_rows=1, device="cuda"):
+        self.rows, self.cols = rows, cols
+        # (zeros: what lies past a row's end is nobody's, but a reader who looks at it finds no surprises)
+        self.q = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.uint8, device=device)
+        self.scale = torch.ones(-(-cols // 128), -(-rows // block_rows), dtype=torch.float32, device=device)
+        self.desc = make_fp8(self.q, cols, self.scale.t(), block_rows)
+
+    @classmethod
+    def from_float(cls, d_w, block_rows=128, stream=None):
+        """nq_quantize_fp8 of [rows][cols] floats (weights; block_rows=1: activations)."""
+        dtype = {torch.float32: NQ_DT_F32, torch.float16: NQ_DT_F16, torch.bfloat16: NQ_DT_BF16}[d_w.dtype]
+        self = cls(d_w.shape[0], d_w.shape[1], block_rows, d_w.device)
+        nq_quantize_fp8(d_w, dtype, d_w.stride(0) if d_w.shape[0] > 1 else d_w.shape[1], None, 0, NQ_ACT_NONE, self.desc, stream)
+        return self
 
 
 class NestedWeight:

@@ -27,6 +27,14 @@ conv_fn conv_of[2];
 gconv_fn gconv_of[2];
 qpack_fn qpack_of;
 
+PyObject *t_fp8, *t_norm_job;
+typedef nq_status (*qfp8_fn)(const void *, int, int64_t, const void *, int64_t, int, const nq_fp8 *, void *);
+typedef nq_status (*gfp8_fn)(const nq_fp8 *, const nq_fp8 *, const float *, void *, int, int64_t, void *);
+typedef nq_status (*norm_fn)(const nq_norm_job *, int64_t, int64_t, void *);
+qfp8_fn qfp8_of;
+gfp8_fn gfp8_of;
+norm_fn norm_of;
+
 // A descriptor's memory for the length of a call.
 struct Struct {
     Py_buffer view;
@@ -247,6 +255,63 @@ PyObject *setup(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// (x, dtype, ldx, mul, ldmul, act, q, stream)
+PyObject *quantize_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct q;
+    void *x, *mul, *s;
+    int64_t dtype, ldx, ldmul, act;
+    if (n != 8 || !pointer(a[0], &x) || !integer(a[1], &dtype) || dtype != (int)dtype || !integer(a[2], &ldx) || !pointer(a[3], &mul) ||
+        !integer(a[4], &ldmul) || !integer(a[5], &act) || act != (int)act || !q.take(a[6], t_fp8, sizeof(nq_fp8)) || !stream(a[7], &s))
+        return not_plain();
+    NQ_CALL(st, qfp8_of(x, (int)dtype, ldx, mul, ldmul, (int)act, q.as<nq_fp8>(), s));
+    return PyLong_FromLong(st);
+}
+
+// (x, w, bias, y, dtype, ldy, stream)
+PyObject *gemm_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct x, w;
+    void *bias, *y, *s;
+    int64_t dtype, ldy;
+    if (n != 7 || !x.take(a[0], t_fp8, sizeof(nq_fp8)) || !w.take(a[1], t_fp8, sizeof(nq_fp8)) || !pointer(a[2], &bias) ||
+        !pointer(a[3], &y) || !integer(a[4], &dtype) || dtype != (int)dtype || !integer(a[5], &ldy) || !stream(a[6], &s))
+        return not_plain();
+    NQ_CALL(st, gfp8_of(x.as<nq_fp8>(), w.as<nq_fp8>(), (const float *)bias, y, (int)dtype, ldy, s));
+    return PyLong_FromLong(st);
+}
+
+// (job, M, D, stream)
+PyObject *block_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct j;
+    void *s;
+    int64_t M, D;
+    if (n != 4 || !j.take(a[0], t_norm_job, sizeof(nq_norm_job)) || !integer(a[1], &M) || !integer(a[2], &D) || !stream(a[3], &s))
+        return not_plain();
+    NQ_CALL(st, norm_of(j.as<nq_norm_job>(), M, D, s));
+    return PyLong_FromLong(st);
+}
+
+// (types: fp8 matrix, norm job; addresses: quantise, gemm, norm)
+PyObject *setup_fp8(PyObject *, PyObject *args)
+{
+    PyObject *o[2], *f[3];
+    if (!PyArg_ParseTuple(args, "OOOOO", o, o + 1, f, f + 1, f + 2)) return nullptr;
+    void *at[3];
+    for (int i = 0; i < 3; ++i)
+        if (!(at[i] = PyLong_AsVoidPtr(f[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "no address");
+    for (PyObject *p : o)
+        if (!PyType_Check(p)) return PyErr_Format(PyExc_TypeError, "not a type");
+    for (PyObject *p : o) Py_INCREF(p);                        // held for the life of the process
+    t_fp8 = o[0];
+    t_norm_job = o[1];
+    qfp8_of = (qfp8_fn)at[0];
+    gfp8_of = (gfp8_fn)at[1];
+    norm_of = (norm_fn)at[2];
+    Py_RETURN_NONE;
+}
+
 PyObject *set_stream_ready(PyObject *, PyObject *v)
 {
     stream_ready = PyObject_IsTrue(v) == 1;
@@ -255,6 +320,7 @@ PyObject *set_stream_ready(PyObject *, PyObject *v)
 
 #define NQ_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NQ_FAST(gemm), NQ_FAST(conv), NQ_FAST(gconv), NQ_FAST(quantize_pack), NQ_FAST(layer),
+                         NQ_FAST(quantize_fp8), NQ_FAST(gemm_fp8), NQ_FAST(block_norm), {"setup_fp8", setup_fp8, METH_VARARGS, nullptr},
                          {"setup", setup, METH_VARARGS, nullptr},
                          {"set_stream_ready", set_stream_ready, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

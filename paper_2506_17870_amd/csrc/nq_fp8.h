@@ -1,0 +1,211 @@
+// Shared by the fp8 kernels (include/nq.h: nq_quantize_fp8, nq_gemm_fp8, nq_block_norm): element types, the e4m3 codes of
+// eight values, host-side checks of a descriptor.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "nq_common.h"
+
+namespace nq {
+
+typedef _Float16 f8_h8 __attribute__((ext_vector_type(8)));
+typedef float f8_f4 __attribute__((ext_vector_type(4)));
+
+struct bf16_t {
+    uint16_t bits;
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(_Float16 v) { return (float)v; }
+__device__ __forceinline__ float to_float(bf16_t v) { return __builtin_bit_cast(float, (uint32_t)v.bits << 16); }
+
+// fp32 -> the type, rounded to nearest even (bf16 by the conversion instruction, two at a time)
+typedef __bf16 f8_b2 __attribute__((ext_vector_type(2)));
+typedef float f8_f2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f8_f2{a, b}, f8_b2));
+}
+__device__ __forceinline__ void from_float(float v, float *o) { *o = v; }
+__device__ __forceinline__ void from_float(float v, _Float16 *o) { *o = (_Float16)v; }
+__device__ __forceinline__ void from_float(float v, bf16_t *o) { o->bits = (uint16_t)pack_bf16(v, v); }
+
+// Eight neighbouring elements as they lie in memory.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    uint4 a, b;
+};
+template <>
+struct Raw8<_Float16> {
+    uint4 a;
+};
+template <>
+struct Raw8<bf16_t> {
+    uint4 a;
+};
+
+__device__ __forceinline__ void raw_to_float(const Raw8<float> &r, float (&v)[8])
+{
+    const uint32_t d[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float, d[i]);
+}
+__device__ __forceinline__ void raw_to_float(const Raw8<_Float16> &r, float (&v)[8])
+{
+    const f8_h8 h = __builtin_bit_cast(f8_h8, r.a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+}
+__device__ __forceinline__ void raw_to_float(const Raw8<bf16_t> &r, float (&v)[8])
+{
+    const uint32_t d[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __builtin_bit_cast(float, d[i] << 16);
+        v[2 * i + 1] = __builtin_bit_cast(float, d[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void float_to_raw(const float (&v)[8], Raw8<float> &r)
+{
+    r.a = __builtin_bit_cast(uint4, f8_f4{v[0], v[1], v[2], v[3]});
+    r.b = __builtin_bit_cast(uint4, f8_f4{v[4], v[5], v[6], v[7]});
+}
+__device__ __forceinline__ void float_to_raw(const float (&v)[8], Raw8<_Float16> &r)
+{
+    f8_h8 h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = (_Float16)v[i];
+    r.a = __builtin_bit_cast(uint4, h);
+}
+__device__ __forceinline__ void float_to_raw(const float (&v)[8], Raw8<bf16_t> &r)
+{
+    r.a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+
+// n (0..8) of eight neighbouring elements, the others as zeros.  VEC: p is 16-byte aligned.
+template <bool VEC, typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *p, int n)
+{
+    Raw8<T> r{};
+    if (VEC && n == 8) {
+        r = *reinterpret_cast<const Raw8<T> *>(p);
+    } else {
+        T e[8] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) e[i] = p[i];
+        r = __builtin_bit_cast(Raw8<T>, e);
+    }
+    return r;
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
+{
+    if (VEC && n == 8) {
+        Raw8<T> r;
+        float_to_raw(v, r);
+        *reinterpret_cast<Raw8<T> *>(p) = r;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) from_float(v[i], p + i);
+    }
+}
+
+// The scale of a block with largest magnitude a (its bits, so that a NaN, the largest pattern of all, wins every maximum),
+// and the factor of its codes.
+__device__ __forceinline__ float fp8_scale(uint32_t a_bits, float *inverse)
+{
+    const float a = __builtin_bit_cast(float, a_bits);
+    float s = a / 448.0f;
+    s = s < 0x1p-126f ? 0x1p-126f : s;                    // (a NaN stays)
+    s = a_bits == 0 ? 1.0f : s;
+    *inverse = 1.0f / s;
+    return s;
+}
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+
+// Codes of eight values.  |v * inverse| <= 448 (1 + 2^-22) in a block with finite values, which rounds to 448 at most, so no
+// clamp is needed; NaN becomes the NaN code.
+__device__ __forceinline__ uint2 fp8_codes(const float (&v)[8], float inverse)
+{
+    uint32_t d[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int w = 0;
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] * inverse, v[4 * i + 1] * inverse, w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] * inverse, v[4 * i + 3] * inverse, w, true);
+        d[i] = (uint32_t)w;
+    }
+    return make_uint2(d[0], d[1]);
+}
+// VEC: p is 8-byte aligned
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t *p, int n, uint2 c)
+{
+    if (VEC && n == 8) {
+        *reinterpret_cast<uint2 *>(p) = c;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (uint8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+    }
+}
+
+// The larger of the lanes' values over each 16 neighbouring lanes.
+__device__ __forceinline__ uint32_t max16(uint32_t v)
+{
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, m));
+    return v;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+inline int dtype_bytes(int dtype) { return dtype == NQ_DT_F32 ? 4 : 2; }
+inline bool is_dtype(int dtype) { return dtype == NQ_DT_F32 || dtype == NQ_DT_F16 || dtype == NQ_DT_BF16; }
+inline bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// rows * ld elements stay far inside 64 bits for every size that is let through
+constexpr int64_t FP8_MAX_ROWS = int64_t(1) << 40, FP8_MAX_LD = int64_t(1) << 20;
+
+inline nq_status check_fp8(const nq_fp8 *q)
+{
+    if (!q || q->rows < 0 || q->cols < 0 || q->scale_row_step < 0 || q->scale_col_step < 0) return NQ_ERR_INVALID_ARG;
+    if (q->block_rows != 1 && q->block_rows != 128) return NQ_ERR_INVALID_ARG;
+    if (q->cols > NQ_MAX_K || q->rows > FP8_MAX_ROWS || q->ld < q->cols || q->ld > FP8_MAX_LD) return NQ_ERR_SHAPE;
+    if (q->scale_row_step > FP8_MAX_LD || q->scale_col_step > FP8_MAX_ROWS) return NQ_ERR_SHAPE;
+    if (q->rows == 0 || q->cols == 0) return NQ_OK;
+    if (!q->d_q || !q->d_scale) return NQ_ERR_INVALID_ARG;
+    return aligned_to(q->d_scale, 4) ? NQ_OK : NQ_ERR_ALIGN;
+}
+
+// A [rows][cols] operand of `dtype`, rows ld elements apart.
+inline nq_status check_matrix(const void *p, int dtype, int64_t cols, int64_t ld)
+{
+    if (!p) return NQ_ERR_INVALID_ARG;
+    if (ld < cols || ld > (int64_t(1) << 32)) return NQ_ERR_SHAPE;
+    return aligned_to(p, dtype_bytes(dtype)) ? NQ_OK : NQ_ERR_ALIGN;
+}
+inline bool rows_on_16(const void *p, int dtype, int64_t ld) { return !p || (aligned16(p) && ld * dtype_bytes(dtype) % 16 == 0); }
+
+// n / d == (n * m) >> (32 + s) for every n < 2^31 and 1 <= d < 2^31, m and s made here (m fits 32 bits: 2^(32+s) / d with
+// 2^s <= d < 2^(s+1) lies in (2^31, 2^32]; rounded up it is off by less than one part in 2^31 / n).  d = 1 gives m = 2^32,
+// kept as 0 and taken apart in divide().
+struct Divider {
+    uint32_t d, m;
+    int s;
+};
+inline Divider make_divider(uint32_t d)
+{
+    int s = 0;
+    while ((d >> (s + 1)) != 0) ++s;
+    if ((d & (d - 1)) == 0) return Divider{d, 0, s};     // a power of two: a shift
+    return Divider{d, (uint32_t)(((uint64_t(1) << (32 + s)) + d - 1) / d), s};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider &v) { return v.m ? __umulhi(n, v.m) >> v.s : n >> v.s; }
+
+}  // namespace nq

@@ -1,0 +1,113 @@
+// The e4m3 matrix product with block scales: what its kernels share.
+//
+//   Y[m][n] = sum_b sx[m][b] * sw[n / 128][b] * P_b[m][n] + bias[n],   P_b = sum over block b's 128 columns of x[m][k] * w[n][k]
+//
+// One v_mfma_f32_16x16x128_f8f6f4 makes P_b of 16 weight rows and 16 tokens.  The weights are its A operand and the
+// tokens its B operand, so that in the result a lane holds one token (lane % 16) and four neighbouring outputs
+// 4 * (lane / 16) + i: the token's scale is one value per lane and the weights' scale one per wave, a single factor for the
+// lane's four sums, and the four outputs are stored side by side.  The products of a block start from zero and are added
+// to the running sums with four fused multiply-adds in fp32, as the formula says.  (The matrix core can scale its operands
+// itself, but by powers of two only.)  A lane of either operand holds 32 bytes of a row; which of the block's columns they
+// are does not matter as long as both operands agree, so a lane takes the 16-byte pieces lane / 16 and 4 + lane / 16.
+#pragma once
+#include "nq_fp8.h"
+
+namespace nq {
+
+typedef int f8_v8i __attribute__((ext_vector_type(8)));
+typedef int f8_v4i __attribute__((ext_vector_type(4)));
+
+struct Fp8GemmParams {
+    const uint8_t *x, *w;
+    const float *sx, *sw, *bias;
+    void *y;
+    int64_t ldx, ldw, ldy, sxr, sxc, swr, swc;
+    int M, N, K, KB;                       // KB: column blocks
+    int y_vec;                             // four outputs may be stored at once
+};
+
+__device__ __forceinline__ f8_v8i fp8_frag(f8_v4i lo, f8_v4i hi)
+{
+    return f8_v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+}
+
+// A lane's 32 codes of a block as the matrix core takes them.
+//
+// WIDE = false: the codes themselves.  The fp8 matrix instructions (all of them, measured) put products that lie close together
+// on the exponent of the largest and cut them off about 14 bits below it before they add them in fp32: 1.4e-5 of the result
+// (2-norm) for normal codes, 5e-5 for codes of every size alike.  That is a fifteenth of what rounding the result to f16 costs
+// and a hundredth of bf16's, so 16-bit outputs are made with it.
+// WIDE = true, for fp32 outputs, whose own rounding would be a thousand times smaller: every code is exactly an f16 number and
+// every product of two exactly an fp32 one; the f16 instruction cuts nothing off (1e-8 on the same codes).  It has half the
+// rate, and a conversion for every two codes comes before it.
+typedef _Float16 f8_h2 __attribute__((ext_vector_type(2)));
+template <bool WIDE>
+struct Fp8Operand {
+    f8_v8i v;
+    __device__ __forceinline__ void set(f8_v8i codes) { v = codes; }
+};
+template <>
+struct Fp8Operand<true> {
+    f8_h8 v[4];
+    __device__ __forceinline__ void set(f8_v8i codes)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const f8_h2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[i], 1.0f, false);
+            const f8_h2 hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[i], 1.0f, true);
+            const int at = 4 * (i & 1);
+            v[i >> 1][at] = lo[0];
+            v[i >> 1][at + 1] = lo[1];
+            v[i >> 1][at + 2] = hi[0];
+            v[i >> 1][at + 3] = hi[1];
+        }
+    }
+};
+
+// P of one block.  (both scale operands 0: the instruction without scales)
+__device__ __forceinline__ f8_f4 fp8_mfma(const Fp8Operand<false> &w, const Fp8Operand<false> &x)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, f8_f4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ f8_f4 fp8_mfma(const Fp8Operand<true> &w, const Fp8Operand<true> &x)
+{
+    f8_f4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], r, 0, 0, 0);
+    return r;
+}
+__device__ __forceinline__ void fp8_add(f8_f4 &acc, f8_f4 p, float s)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(p[i], s, acc[i]);
+}
+
+// Outputs n .. n + 3 of token m.
+template <typename T>
+__device__ __forceinline__ void fp8_store(const Fp8GemmParams &p, int m, int n, f8_f4 v)
+{
+    if (m >= p.M || n >= p.N) return;
+    T *y = static_cast<T *>(p.y) + (int64_t)m * p.ldy + n;
+    const int left = p.N - n;
+    if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) v[i] += p.bias[n + i];
+    }
+    if (p.y_vec && left >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f8_f4 *>(y) = v;
+        } else {
+            T o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) from_float(v[i], o + i);
+            *reinterpret_cast<uint2 *>(y) = __builtin_bit_cast(uint2, o);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) from_float(v[i], y + i);
+    }
+}
+
+}  // namespace nq

@@ -1,0 +1,132 @@
+// nq_gemm_fp8: the kernels and the choice between them.  nq_fp8_gemm.h has the mathematics.
+#include "nq_fp8_gemm.h"
+
+namespace nq {
+
+// ---- any alignment ---------------------------------------------------------------------------------------------
+// Rows that start on any byte: a piece of 16 bytes is put together from the aligned dwords around it, of which only those
+// are read that hold a byte of the row.
+__device__ __forceinline__ f8_v4i fp8_piece(const uint8_t *p, int n)
+{
+    f8_v4i r = {0, 0, 0, 0};
+    if (n <= 0) return r;
+    const int a = (int)(reinterpret_cast<uintptr_t>(p) & 3);
+    const uint32_t *q = reinterpret_cast<const uint32_t *>(p - a);
+    uint32_t d[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) d[i] = 4 * i - a < n && (i < 4 || a != 0) ? q[i] : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t v = __builtin_amdgcn_alignbyte(d[i + 1], d[i], a);
+        const int left = n - 4 * i;                        // bytes of this dword that belong to the row
+        v = left >= 4 ? v : left <= 0 ? 0u : v & ((1u << (8 * left)) - 1u);
+        r[i] = (int)v;
+    }
+    return r;
+}
+
+// Tile of 64 weight rows x 64 tokens, four waves of 32 x 32, one column block at a time through LDS.  A row's eight 16-byte
+// pieces lie exchanged, piece c at c ^ ((row / 2) & 7): two rows are once round the 64 banks, and sixteen rows' pieces c in
+// sixteen different places.
+template <typename T>
+__global__ void __launch_bounds__(256) k_fp8_gemm_any(const Fp8GemmParams p)
+{
+    __shared__ f8_v4i panel[2][64 * 8];                    // weights, tokens
+    const int nblocks = (p.N + 63) / 64;
+    const int bm = blockIdx.x / nblocks, bn = blockIdx.x - bm * nblocks;
+    const int m0 = bm * 64, n0 = bn * 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wn = (wave & 1) * 32, wm = (wave >> 1) * 32;
+    const int r16 = lane & 15, g = lane >> 4;
+    f8_f4 acc[2][2] = {};
+    for (int kb = 0; kb < p.KB; ++kb) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int id = (i & 1) * 256 + threadIdx.x, row = id >> 3, c = id & 7, k = kb * 128 + c * 16;
+            const bool tokens = i >= 2;
+            const int at = (tokens ? m0 : n0) + row;
+            const int n = at < (tokens ? p.M : p.N) ? min(16, p.K - k) : 0;
+            const uint8_t *src = (tokens ? p.x + (int64_t)at * p.ldx : p.w + (int64_t)at * p.ldw) + k;
+            panel[tokens][row * 8 + (c ^ ((row >> 1) & 7))] = fp8_piece(src, n);
+        }
+        __syncthreads();
+        const float sw = p.sw[(int64_t)((n0 + wn) >> 7) * p.swr + (int64_t)kb * p.swc];
+        auto frag = [&](int which, int row) {
+            const f8_v4i *q = panel[which] + row * 8;
+            const int s = (row >> 1) & 7;
+            Fp8Operand<sizeof(T) == 4> o;
+            o.set(fp8_frag(q[g ^ s], q[(g + 4) ^ s]));
+            return o;
+        };
+        const auto w0 = frag(0, wn + r16), w1 = frag(0, wn + 16 + r16);
+#pragma unroll
+        for (int tm = 0; tm < 2; ++tm) {
+            const int m = m0 + wm + tm * 16 + r16;
+            const float s = m < p.M ? p.sx[(int64_t)m * p.sxr + (int64_t)kb * p.sxc] * sw : 0.0f;
+            const auto x = frag(1, wm + tm * 16 + r16);
+            fp8_add(acc[tm][0], fp8_mfma(w0, x), s);
+            fp8_add(acc[tm][1], fp8_mfma(w1, x), s);
+        }
+    }
+#pragma unroll
+    for (int tm = 0; tm < 2; ++tm)
+#pragma unroll
+        for (int tn = 0; tn < 2; ++tn) fp8_store<T>(p, m0 + wm + tm * 16 + r16, n0 + wn + tn * 16 + 4 * g, acc[tm][tn]);
+}
+
+template <typename T>
+static void launch_gemm(const Fp8GemmParams &p, hipStream_t s)
+{
+    k_fp8_gemm_any<T><<<(unsigned)(ceil_div(p.M, 64) * ceil_div(p.N, 64)), 256, 0, s>>>(p);
+}
+
+}  // namespace nq
+
+using namespace nq;
+
+extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *d_bias, void *d_y, int dtype, int64_t ldy,
+                                 void *stream)
+{
+    if (!is_dtype(dtype)) return NQ_ERR_INVALID_ARG;
+    nq_status st;
+    if ((st = check_fp8(x)) != NQ_OK || (st = check_fp8(w)) != NQ_OK) return st;
+    if (x->block_rows != 1 || w->block_rows != 128) return NQ_ERR_UNSUPPORTED;
+    if (x->cols != w->cols || w->rows > (int64_t(1) << 31) - 128) return NQ_ERR_SHAPE;
+    if (x->rows == 0 || w->rows == 0) return NQ_OK;
+    if ((st = check_matrix(d_y, dtype, w->rows, ldy)) != NQ_OK) return st;
+    if (!aligned_to(d_bias, 4)) return NQ_ERR_ALIGN;
+
+    Fp8GemmParams p;
+    p.w = w->d_q;
+    p.sw = w->d_scale;
+    p.bias = d_bias;
+    p.ldx = x->ld;
+    p.ldw = w->ld;
+    p.ldy = ldy;
+    p.sxr = x->scale_row_step;
+    p.sxc = x->scale_col_step;
+    p.swr = w->scale_row_step;
+    p.swc = w->scale_col_step;
+    p.N = (int)w->rows;
+    p.K = (int)w->cols;
+    p.KB = (p.K + 127) / 128;
+    const int es = dtype_bytes(dtype);
+    p.y_vec = aligned_to(d_y, 4 * es) && ldy % 4 == 0;
+    // at most 2^30 tiles of 64 x 64 to a launch
+    const int64_t step = std::max<int64_t>(1, (int64_t(1) << 30) / ceil_div(p.N, 64)) * 64;
+    for (int64_t m = 0; m < x->rows; m += std::min<int64_t>(step, 1 << 30)) {
+        p.M = (int)std::min<int64_t>(std::min<int64_t>(step, 1 << 30), x->rows - m);
+        p.x = x->d_q ? x->d_q + m * x->ld : nullptr;
+        p.sx = x->d_scale ? x->d_scale + m * x->scale_row_step : nullptr;
+        p.y = static_cast<uint8_t *>(d_y) + m * ldy * es;
+        if (dtype == NQ_DT_F32)
+            launch_gemm<float>(p, (hipStream_t)stream);
+        else if (dtype == NQ_DT_F16)
+            launch_gemm<_Float16>(p, (hipStream_t)stream);
+        else
+            launch_gemm<bf16_t>(p, (hipStream_t)stream);
+        if ((st = launch_status()) != NQ_OK) return st;
+    }
+    return NQ_OK;
+}

@@ -1,0 +1,185 @@
+// nq_quantize_fp8: floats -> e4m3 codes with a scale for each block of 128 columns, behind an activation function and a product.
+// Bound by the bytes: each input is read once and each code written once, and the block's values stay in registers between
+// the maximum and the codes.
+#include "nq_fp8.h"
+
+namespace nq {
+
+struct QuantParams {
+    const void *x, *mul;
+    uint8_t *q;
+    float *scale;
+    int64_t ldx, ldmul, ldq, srow, scol, row0;
+    uint32_t rows, groups;                 // rows of this launch; rows * column blocks
+    int K;
+    Divider by_blocks;                     // column blocks of a row
+};
+
+// The exponentials go through the hardware's base-2 one: its error, a few parts in 2^23 of the sigmoid, is far below a code's step.
+template <int ACT>
+__device__ __forceinline__ float activate(float v)
+{
+    if constexpr (ACT == NQ_ACT_RELU) return v < 0.0f ? 0.0f : v;             // (NaN stays)
+    if constexpr (ACT == NQ_ACT_SILU) return v / (1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
+    if constexpr (ACT == NQ_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
+    // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
+    if constexpr (ACT == NQ_ACT_GELU_TANH)
+        return v / (1.0f + __builtin_amdgcn_exp2f(-2.30220821f * (v + 0.044715f * v * v * v)));
+    return v;
+}
+
+template <int ACT, typename T>
+__device__ __forceinline__ uint32_t act_and_max(const Raw8<T> &x, const Raw8<T> *m, float (&v)[8])
+{
+    raw_to_float(x, v);
+    float u[8];
+    if (m) raw_to_float(*m, u);
+    uint32_t a = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = activate<ACT>(v[i]);
+        if (m) v[i] *= u[i];
+        a = max(a, abs_bits(v[i]));
+    }
+    return a;
+}
+
+// A scale for each 1 x 128: eight columns per thread, sixteen threads per block of columns.
+template <typename T, int ACT, bool MUL, bool VEC>
+__global__ void __launch_bounds__(256) k_fp8_rows(const QuantParams p)
+{
+    const uint32_t group = blockIdx.x * 16u + (threadIdx.x >> 4);
+    if (group >= p.groups) return;
+    const uint32_t r = divide(group, p.by_blocks), b = group - r * p.by_blocks.d;
+    const int64_t row = p.row0 + r;
+    const int c = (int)b * 128 + (threadIdx.x & 15) * 8;
+    const int n = min(8, max(0, p.K - c));
+    const Raw8<T> x = load8<VEC>(static_cast<const T *>(p.x) + row * p.ldx + c, n);
+    Raw8<T> m{};
+    if constexpr (MUL) m = load8<VEC>(static_cast<const T *>(p.mul) + row * p.ldmul + c, n);
+    float v[8], inverse;
+    const uint32_t a = max16(act_and_max<ACT>(x, MUL ? &m : nullptr, v));
+    const float s = fp8_scale(a, &inverse);
+    store_codes<VEC>(p.q + row * p.ldq + c, n, fp8_codes(v, inverse));
+    if ((threadIdx.x & 15) == 0) p.scale[row * p.srow + b * p.scol] = s;
+}
+
+// A scale for each 128 x 128: a workgroup per block, eight columns of each sixteenth row per thread.
+template <typename T, int ACT, bool MUL, bool VEC>
+__global__ void __launch_bounds__(256) k_fp8_tiles(const QuantParams p)
+{
+    __shared__ uint32_t largest[4];
+    const uint32_t rb = divide(blockIdx.x, p.by_blocks), b = blockIdx.x - rb * p.by_blocks.d;
+    const int c = (int)b * 128 + (threadIdx.x & 15) * 8;
+    const int n = min(8, max(0, p.K - c));
+    const uint32_t r0 = rb * 128 + (threadIdx.x >> 4);
+    Raw8<T> x[8], m[MUL ? 8 : 1];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = p.row0 + r0 + 16 * i;
+        const int here = r0 + 16 * i < p.rows ? n : 0;
+        x[i] = load8<VEC>(static_cast<const T *>(p.x) + row * p.ldx + c, here);
+        if constexpr (MUL) m[i] = load8<VEC>(static_cast<const T *>(p.mul) + row * p.ldmul + c, here);
+    }
+    uint32_t a = 0;
+    float v[8], inverse;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = max(a, act_and_max<ACT>(x[i], MUL ? &m[i] : nullptr, v));
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, k));
+    if ((threadIdx.x & 63) == 0) largest[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = max(max(largest[0], largest[1]), max(largest[2], largest[3]));
+    const float s = fp8_scale(a, &inverse);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = p.row0 + r0 + 16 * i;
+        const int here = r0 + 16 * i < p.rows ? n : 0;
+        act_and_max<ACT>(x[i], MUL ? &m[i] : nullptr, v);
+        store_codes<VEC>(p.q + row * p.ldq + c, here, fp8_codes(v, inverse));
+    }
+    if (threadIdx.x == 0) p.scale[(p.row0 / 128 + rb) * p.srow + b * p.scol] = s;
+}
+
+template <typename T, int ACT, bool MUL>
+static void launch_quant(const QuantParams &p, bool vec, int block_rows, hipStream_t s)
+{
+    if (block_rows == 1) {
+        const dim3 grid((p.groups + 15) / 16);
+        if (vec)
+            k_fp8_rows<T, ACT, MUL, true><<<grid, 256, 0, s>>>(p);
+        else
+            k_fp8_rows<T, ACT, MUL, false><<<grid, 256, 0, s>>>(p);
+    } else {
+        const dim3 grid((p.rows + 127) / 128 * p.by_blocks.d);
+        if (vec)
+            k_fp8_tiles<T, ACT, MUL, true><<<grid, 256, 0, s>>>(p);
+        else
+            k_fp8_tiles<T, ACT, MUL, false><<<grid, 256, 0, s>>>(p);
+    }
+}
+
+template <typename T>
+static void launch_act(const QuantParams &p, int act, bool vec, int block_rows, hipStream_t s)
+{
+#define NQ_QUANT_ACT(A)                                                   \
+    case A:                                                               \
+        if (p.mul)                                                        \
+            launch_quant<T, A, true>(p, vec, block_rows, s);              \
+        else                                                              \
+            launch_quant<T, A, false>(p, vec, block_rows, s);             \
+        break;
+    switch (act) {
+        NQ_QUANT_ACT(NQ_ACT_NONE)
+        NQ_QUANT_ACT(NQ_ACT_RELU)
+        NQ_QUANT_ACT(NQ_ACT_SILU)
+        NQ_QUANT_ACT(NQ_ACT_GELU)
+        NQ_QUANT_ACT(NQ_ACT_GELU_TANH)
+    default: break;
+    }
+#undef NQ_QUANT_ACT
+}
+
+}  // namespace nq
+
+using namespace nq;
+
+extern "C" nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, const void *d_mul, int64_t ldmul, int act,
+                                     const nq_fp8 *q, void *stream)
+{
+    if (!is_dtype(dtype) || act < NQ_ACT_NONE || act > NQ_ACT_GELU_TANH) return NQ_ERR_INVALID_ARG;
+    nq_status st = check_fp8(q);
+    if (st != NQ_OK) return st;
+    if (q->rows == 0 || q->cols == 0) return NQ_OK;
+    if ((st = check_matrix(d_x, dtype, q->cols, ldx)) != NQ_OK) return st;
+    if (d_mul && (st = check_matrix(d_mul, dtype, q->cols, ldmul)) != NQ_OK) return st;
+
+    QuantParams p;
+    p.x = d_x;
+    p.mul = d_mul;
+    p.q = q->d_q;
+    p.scale = q->d_scale;
+    p.ldx = ldx;
+    p.ldmul = ldmul;
+    p.ldq = q->ld;
+    p.srow = q->scale_row_step;
+    p.scol = q->scale_col_step;
+    p.K = (int)q->cols;
+    const uint32_t blocks = (uint32_t)ceil_div(q->cols, 128);
+    p.by_blocks = make_divider(blocks);
+    const bool vec = rows_on_16(d_x, dtype, ldx) && rows_on_16(d_mul, dtype, ldmul) && aligned_to(q->d_q, 8) && q->ld % 8 == 0;
+    // at most 2^30 blocks to a launch, whole blocks of 128 rows
+    const int64_t step = std::max<int64_t>(128, (int64_t(1) << 30) / blocks / 128 * 128);
+    for (p.row0 = 0; p.row0 < q->rows; p.row0 += step) {
+        p.rows = (uint32_t)std::min(step, q->rows - p.row0);
+        p.groups = p.rows * blocks;
+        if (dtype == NQ_DT_F32)
+            launch_act<float>(p, act, vec, q->block_rows, (hipStream_t)stream);
+        else if (dtype == NQ_DT_F16)
+            launch_act<_Float16>(p, act, vec, q->block_rows, (hipStream_t)stream);
+        else
+            launch_act<bf16_t>(p, act, vec, q->block_rows, (hipStream_t)stream);
+        if ((st = launch_status()) != NQ_OK) return st;
+    }
+    return NQ_OK;
+}

@@ -1,0 +1,487 @@
+"""The fp8 operators (nq_quantize_fp8, nq_gemm_fp8, nq_block_norm) against plain implementations in 64 bits.
+
+Bounds.  Where every step of the definition is one rounded fp32 operation, results are compared bit for bit.  A product's
+sum is held to (columns of a block + blocks + 4) * 2^-23 of the sum of the terms' magnitudes: every addition and every
+multiplication may be off by one unit of the running fp32 sum (the matrix core's may truncate), none of which is larger than
+that sum of magnitudes; on top of it half a unit of the output type.  16-bit outputs are made by the fp8 matrix instructions,
+which cut a product off at 2^-14 of the largest one added with it: each of a block's products is off by that much of the
+block's largest, at most, and all of them together by 2^-14 of the result (2-norm; 1.4e-5 was measured on codes like these).
+Integers and powers of two come out exactly in every type.  A norm's sums are added over at most 64 terms per thread,
+6 steps within a wave and 8 between the waves: 80 * 2^-23."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_UNIT = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}     # of a value's magnitude, at most
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -133}
+
+
+@pytest.fixture(scope="module")
+def nq():
+    import paper_2506_17870_amd as nq
+    return nq
+
+
+def dt(nq, name):
+    return {"f32": nq.NQ_DT_F32, "f16": nq.NQ_DT_F16, "bf16": nq.NQ_DT_BF16}[name]
+
+
+def code_values():
+    """The value of each of the 256 codes, from the format's definition."""
+    v = np.empty(256)
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        v[c] = np.nan if (c & 0x7f) == 0x7f else (-1.0) ** (c >> 7) * (m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7))
+    return v
+
+
+VALUES = code_values()
+
+
+def nearest_codes(v):
+    """e4m3 codes of fp32 values, |v| <= 448, to nearest even by the list of all values."""
+    order = np.argsort(VALUES[:0x7f], kind="stable")
+    mags = VALUES[:0x7f][order]
+    a = np.abs(v.astype(np.float64))
+    hi = np.clip(np.searchsorted(mags, a), 0, 0x7e)
+    lo = np.maximum(hi - 1, 0)
+    up = np.where(mags[hi] - a < a - mags[lo], True, np.where(mags[hi] - a > a - mags[lo], False, hi % 2 == 0))
+    c = np.where(up, hi, lo).astype(np.uint8)
+    c = np.where(np.isnan(a), 0x7f, c).astype(np.uint8)
+    return c | (np.signbit(v).astype(np.uint8) << 7)
+
+
+def blocks(n):
+    return -(-n // 128)
+
+
+def reference_codes(v, block_rows):
+    """Codes and scales [row blocks][column blocks] of fp32 values, in the definition's fp32 steps."""
+    M, K = v.shape
+    q, scale = np.empty((M, K), np.uint8), np.empty((-(-M // block_rows), blocks(K)), np.float32)
+    with np.errstate(all="ignore"):
+        for rb in range(scale.shape[0]):
+            for cb in range(scale.shape[1]):
+                at = np.s_[rb * block_rows:(rb + 1) * block_rows, cb * 128:(cb + 1) * 128]
+                a = np.abs(v[at]).max()                    # (NaN wins)
+                s = np.float32(1) if a == 0 else a / np.float32(448)
+                s = np.float32(2.0 ** -126) if s < np.float32(2.0 ** -126) else s
+                scale[rb, cb] = s
+                q[at] = nearest_codes(v[at] * (np.float32(1) / s))
+    return q, scale
+
+
+def same_codes(got, want):
+    """Equal, or both NaN (whose sign is nobody's)."""
+    return np.array_equal(np.where((got & 0x7f) == 0x7f, 0x7f, got), np.where((want & 0x7f) == 0x7f, 0x7f, want))
+
+
+def strided(t, ld, offset=0):
+    """A copy of the matrix with rows `ld` elements apart, `offset` elements into a buffer; what is around it is set to 77."""
+    buf = torch.full((offset + t.shape[0] * ld + 8,), 77, dtype=t.dtype, device="cuda")
+    view = buf[offset:offset + t.shape[0] * ld].view(t.shape[0], ld)[:, :t.shape[1]]
+    view.copy_(t)
+    return view
+
+
+class Codes:
+    """Memory of a matrix of codes with a guard around it."""
+
+    def __init__(self, nq, M, K, ld=None, offset=0, block_rows=1, by_row=False):
+        self.M, self.K, self.ld, self.offset = M, K, ld or K, offset
+        self.buf = torch.full((offset + M * self.ld + 64,), 0x7f, dtype=torch.uint8, device="cuda")
+        self.q = self.buf[offset:offset + M * self.ld].view(M, self.ld)
+        nb = -(-M // block_rows)
+        self.scale = torch.full((nb, blocks(K)) if by_row else (blocks(K), nb), -7.0, device="cuda")
+        self.scales = self.scale if by_row else self.scale.t()
+        self.desc = nq.make_fp8(self.q, K, self.scales, block_rows)
+
+    def get(self):
+        b = self.buf.cpu().numpy()
+        body = b[self.offset:self.offset + self.M * self.ld].reshape(self.M, self.ld)
+        assert (b[:self.offset] == 0x7f).all() and (b[self.offset + body.size:] == 0x7f).all(), "bytes around the matrix were written"
+        assert (body[:, self.K:] == 0x7f).all(), "bytes between the rows were written"
+        return body[:, :self.K], self.scales.cpu().numpy()
+
+
+def floats(shape, dtype, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(*shape, generator=g) * torch.exp(spread * torch.randn(shape[-1], generator=g))
+    return x.to(TORCH[dtype])
+
+
+# ---- the quantiser ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 128), (3, 127), (129, 256), (5, 1000), (200, 129), (300, 640), (1, 8192)])
+def test_quantise(nq, dtype, block_rows, M, K):
+    x = floats((M, K), dtype, M * 1000 + K)
+    c = Codes(nq, M, K, ld=-(-K // 16) * 16, block_rows=block_rows)
+    nq.nq_quantize_fp8(x.cuda(), dt(nq, dtype), K, None, 0, nq.NQ_ACT_NONE, c.desc)
+    q, s = c.get()
+    want_q, want_s = reference_codes(x.float().numpy(), block_rows)
+    assert np.array_equal(s, want_s) and same_codes(q, want_q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("ldx,offset,ldq,qoffset,by_row", [(333, 0, 333, 0, True), (301, 1, 307, 3, False), (304, 8, 304, 8, True),
+                                                           (1000, 4, 512, 16, False)])
+def test_quantise_strides_and_alignment(nq, dtype, block_rows, ldx, offset, ldq, qoffset, by_row):
+    M, K = 140, 300
+    x, u = floats((M, K), dtype, 5), floats((M, K), dtype, 6, 0.3)
+    c = Codes(nq, M, K, ldq, qoffset, block_rows, by_row)
+    nq.nq_quantize_fp8(strided(x, ldx, offset), dt(nq, dtype), ldx, strided(u, K + 4), K + 4, nq.NQ_ACT_RELU, c.desc)
+    q, s = c.get()
+    xf = x.float().numpy()
+    want_q, want_s = reference_codes(np.where(xf < 0, np.float32(0), xf) * u.float().numpy(), block_rows)
+    assert np.array_equal(s, want_s) and same_codes(q, want_q)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantise_special_values(nq, block_rows):
+    """Each block of columns holds one kind: zeros, the smallest and the largest numbers, infinities, NaN, ties."""
+    M, K = 2, 128 * 9
+    x = np.random.default_rng(0).normal(size=(M, K)).astype(np.float32)
+    of = lambda b: np.s_[:, b * 128:(b + 1) * 128]  # noqa: E731
+    x[of(0)] = 0.0
+    x[of(1)] *= np.float32(1e-44)
+    x[of(2)] *= np.float32(1e-37)
+    x[of(3)] *= np.float32(3.4e38) / np.abs(x[of(3)]).max()
+    x[0, 4 * 128 + 5] = np.inf
+    x[1, 5 * 128 + 77] = np.nan
+    x[0, 6 * 128], x[1, 6 * 128 + 1] = np.nan, -np.inf
+    x[of(7)] = -0.0
+    x[of(8)] = np.arange(256).reshape(2, 128) / 16.0      # largest 448 / 2^k: multiples of 1 / 16 are ties
+    x[:, 8 * 128] = 28.0
+    c = Codes(nq, M, K, block_rows=block_rows)
+    nq.nq_quantize_fp8(torch.from_numpy(x).cuda(), nq.NQ_DT_F32, K, None, 0, nq.NQ_ACT_NONE, c.desc)
+    q, s = c.get()
+    want_q, want_s = reference_codes(x, block_rows)
+    assert np.array_equal(s, want_s, equal_nan=True) and same_codes(q, want_q)
+    assert (s[:, 0] == 1).all() and (s[:, 7] == 1).all() and (s[:, 1] == np.float32(2.0 ** -126)).all()
+    assert not np.isfinite(s[0, 4]) and np.isnan(s[-1, 5])
+
+
+def act64(name, v):
+    t = torch.from_numpy(v)
+    f = {"none": lambda t: t, "relu": lambda t: t.clamp(min=0), "silu": lambda t: t * torch.sigmoid(t),
+         "gelu": lambda t: t * 0.5 * torch.erfc(-t * 2.0 ** -0.5),
+         "gelu_tanh": lambda t: t * torch.sigmoid(2 * (2 / torch.pi) ** 0.5 * (t + 0.044715 * t ** 3))}[name]
+    return f(t).numpy()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("mul", [False, True])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantise_activation(nq, act, dtype, mul, block_rows):
+    """The function is good to 16 units of x in fp32 (exponential, 1 +, quotient, products); a code is then off by half the
+    spacing of the codes around it, at most."""
+    M, K = 37, 777
+    x, u = floats((M, K), dtype, 8, 1.5), floats((M, K), dtype, 9, 0.3)
+    x[0, :8] = torch.tensor([30.0, -30.0, 200.0, -200.0, 1e-4, -1e-4, 0.0, -5.5]).to(x.dtype)
+    c = Codes(nq, M, K, block_rows=block_rows)
+    code = {"silu": nq.NQ_ACT_SILU, "gelu": nq.NQ_ACT_GELU, "gelu_tanh": nq.NQ_ACT_GELU_TANH}[act]
+    nq.nq_quantize_fp8(x.cuda(), dt(nq, dtype), K, u.cuda() if mul else None, K, code, c.desc)
+    q, s = c.get()
+    x64, u64 = x.double().numpy(), u.double().numpy() if mul else 1.0
+    v = act64(act, x64) * u64
+    off = 16 * 2.0 ** -23 * np.abs(x64 * u64)
+    scale = s.repeat(block_rows, 0)[:M].repeat(128, 1)[:, :K].astype(np.float64)
+    want = np.abs(v)
+    for rb in range(s.shape[0]):
+        for cb in range(s.shape[1]):
+            at = np.s_[rb * block_rows:(rb + 1) * block_rows, cb * 128:(cb + 1) * 128]
+            assert abs(s[rb, cb] * 448 - want[at].max()) <= 2 * 2.0 ** -23 * want[at].max() + off[at].max()
+    spacing = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(v / scale), 2.0 ** -6))) - 3)
+    # (a value just below a power of two may be rounded from above it, where the spacing is twice as large)
+    assert (np.abs(VALUES[q] * scale - v) <= scale * spacing * 0.5 * (1 + 2.0 ** -20) + 2 * off + scale * 448 * 2.0 ** -22).all()
+
+
+# ---- the matrix product ----------------------------------------------------------------------------------------
+
+class Operand:
+    """Random codes and scales of a matrix, on the GPU with NaN codes everywhere around it and in 64 bits here."""
+
+    def __init__(self, nq, rows, K, block_rows, seed, ld=None, offset=0, by_row=False, exact=False):
+        r = np.random.default_rng(seed)
+        c = Codes(nq, rows, K, ld, offset, block_rows, by_row)
+        if exact:                                            # integers up to 3 and powers of two: every sum is exact
+            self.codes = nearest_codes(r.integers(-3, 4, (rows, K)).astype(np.float32))
+            scale = 2.0 ** r.integers(-1, 2, c.scales.shape)
+        else:
+            self.codes = nearest_codes(np.clip(r.normal(size=(rows, K)) * 130, -448, 448).astype(np.float32))
+            scale = np.exp(r.normal(size=c.scales.shape)) / 130
+        c.q[:, :K] = torch.from_numpy(self.codes).cuda()
+        self.scale = scale.astype(np.float32)
+        c.scales.copy_(torch.from_numpy(self.scale))
+        self.c, self.desc = c, c.desc
+        self.value = VALUES[self.codes] * self.scale.repeat(block_rows, 0)[:rows].repeat(128, 1)[:, :K].astype(np.float64)
+
+
+def check_gemm(nq, M, N, K, out="f32", bias=False, exact=False, seed=0, ldy=None, yoffset=0, x_kw={}, w_kw={}, stream=None):
+    x, w = Operand(nq, M, K, 1, seed, exact=exact, **x_kw), Operand(nq, N, K, 128, seed + 1, exact=exact, **w_kw)
+    b = np.random.default_rng(seed + 2).integers(-8, 9, N).astype(np.float32) if bias else None
+    ldy = ldy or N
+    y = strided(torch.full((M, N), 55, dtype=TORCH[out]), ldy, yoffset)
+    bt = torch.from_numpy(b).cuda() if bias else None
+    torch.cuda.synchronize()
+    nq.nq_gemm_fp8(x.desc, w.desc, bt, y, dt(nq, out), ldy, stream)
+    torch.cuda.synchronize()
+    whole = y._base if y._base is not None else y
+    got = y.double().cpu().numpy()
+    want = x.value @ w.value.T + (b if bias else 0.0)
+    size = np.abs(x.value) @ np.abs(w.value).T + (np.abs(b) if bias else 0.0)
+    if exact:
+        assert np.array_equal(got, torch.from_numpy(want).to(TORCH[out]).double().numpy())
+    else:
+        bound = (min(K, 128) + blocks(K) + 4) * 2.0 ** -23 * size + HALF_UNIT[out] * np.abs(want) + TINY[out]
+        if out != "f32":
+            for b in range(blocks(K)):
+                at = np.s_[:, b * 128:(b + 1) * 128]
+                bound += min(K, 128) * 2.0 ** -14 * np.abs(x.value[at]).max(1)[:, None] * np.abs(w.value[at]).max(1)
+            assert np.linalg.norm(got - want) <= (2.0 ** -14 + HALF_UNIT[out]) * np.linalg.norm(want)
+        assert (np.abs(got - want) <= bound).all()
+    around = whole.reshape(-1).clone()
+    around.as_strided((M, N), (ldy, 1), yoffset).fill_(77)
+    assert bool((around == 77).all()), "elements around the output were written"
+
+
+GEMM_SIZES = [(1, 1, 1), (1, 128, 128), (1, 4096, 512), (2, 17, 100), (3, 130, 129), (7, 64, 4096), (15, 1000, 384), (16, 256, 1024),
+              (17, 48, 2000), (31, 333, 640), (33, 129, 128), (48, 2048, 256), (64, 64, 64), (65, 1024, 1152), (100, 300, 500), (128, 128, 4096),
+              (129, 257, 640), (200, 1000, 2008), (256, 512, 256), (257, 255, 1000), (300, 700, 136), (513, 1030, 392), (700, 320, 512)]
+
+
+@pytest.mark.parametrize("M,N,K", GEMM_SIZES)
+@pytest.mark.parametrize("exact", [False, True])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_gemm(nq, M, N, K, exact, out):
+    ld = dict(ld=-(-K // 16) * 16)
+    check_gemm(nq, M, N, K, out=out, exact=exact, seed=M + N + K, x_kw=ld, w_kw=ld)
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1, 300, 500), (24, 512, 1024), (70, 1000, 300), (260, 520, 768)])
+def test_gemm_types_and_bias(nq, out, M, N, K):
+    ld = dict(ld=-(-K // 16) * 16)
+    check_gemm(nq, M, N, K, out=out, bias=True, seed=3, x_kw=ld, w_kw=ld)
+    check_gemm(nq, M, N, K, out=out, seed=4, x_kw=ld, w_kw=ld)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 200, 300), (5, 129, 1000), (40, 300, 333), (140, 260, 515)])
+@pytest.mark.parametrize("xld,xo,wld,wo", [(0, 0, 0, 0), (1, 1, 3, 2), (16, 16, 16, 32), (7, 0, 16, 0), (16, 0, 5, 3)])
+def test_gemm_strides_and_alignment(nq, M, N, K, xld, xo, wld, wo):
+    """Leading dimensions K, on 16 bytes with room behind, and odd; both orders of the scales; odd outputs."""
+    ld = lambda more: K if more == 0 else -(-K // 16) * 16 + (64 if more == 16 else more)  # noqa: E731
+    for by_row in (False, True):
+        check_gemm(nq, M, N, K, seed=7, bias=by_row, ldy=N + 3, yoffset=1, x_kw=dict(ld=ld(xld), offset=xo, by_row=by_row),
+                   w_kw=dict(ld=ld(wld), offset=wo, by_row=not by_row))
+        check_gemm(nq, M, N, K, out="bf16", seed=8, ldy=-(-N // 8) * 8 + 8, yoffset=8, x_kw=dict(ld=ld(xld), offset=xo, by_row=by_row),
+                   w_kw=dict(ld=ld(wld), offset=wo, by_row=not by_row))
+
+
+def test_gemm_without_columns_or_rows(nq):
+    y = torch.full((3, 5), 9.0, device="cuda")
+    b = torch.arange(5.0, device="cuda")
+    empty = lambda rows, br: nq.make_fp8(torch.empty(rows, 0, dtype=torch.uint8, device="cuda"), 0, torch.empty(-(-rows // br), 0, device="cuda"), br)  # noqa: E731
+    nq.nq_gemm_fp8(empty(3, 1), empty(5, 128), b, y, nq.NQ_DT_F32, 5)
+    assert torch.equal(y, b.expand(3, 5))
+    nq.nq_gemm_fp8(empty(3, 1), empty(5, 128), None, y, nq.NQ_DT_F32, 5)
+    assert not y.any()
+    y.fill_(9.0)
+    nq.nq_gemm_fp8(empty(0, 1), empty(5, 128), b, y, nq.NQ_DT_F32, 5)
+    nq.nq_gemm_fp8(empty(3, 1), empty(0, 128), b, y, nq.NQ_DT_F32, 5)
+    assert (y == 9).all()
+
+
+@pytest.mark.parametrize("M", [1, 20, 100, 300])
+def test_gemm_not_finite(nq, M):
+    """A NaN code, or a scale that is not finite, spoils the outputs of its row or its 128 weight rows and no others."""
+    N, K = 300, 640
+    x, w = Operand(nq, M, K, 1, 1), Operand(nq, N, K, 128, 2)
+    x.c.q[0, 200] = 0x7f
+    w.c.scales[1, 3] = float("nan")
+    y = torch.empty(M, N, device="cuda")
+    nq.nq_gemm_fp8(x.desc, w.desc, None, y, nq.NQ_DT_F32, N)
+    bad = torch.isnan(y).cpu().numpy()
+    want = np.zeros((M, N), bool)
+    want[0], want[:, 128:256] = True, True
+    assert np.array_equal(bad, want)
+
+
+def test_gemm_twice_and_on_another_stream(nq):
+    """Equal calls give equal bits, whatever runs beside them."""
+    M, N, K = 130, 512, 2048
+    x, w = Operand(nq, M, K, 1, 1), Operand(nq, N, K, 128, 2)
+    ys = [torch.empty(M, N, device="cuda") for _ in range(4)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i, y in enumerate(ys):
+        nq.nq_gemm_fp8(x.desc, w.desc, None, y, nq.NQ_DT_F32, N, side if i % 2 else None)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, ys[0]) for y in ys[1:])
+
+
+# ---- norms around a block ----------------------------------------------------------------------------------------
+
+def norm64(kind, v, w, b, eps):
+    if kind == "none":
+        return v
+    m = v.mean(1, keepdims=True) if kind == "layer" else 0.0
+    r = 1 / np.sqrt(((v - m) ** 2).mean(1, keepdims=True) + eps)
+    return (v - m) * r * (w if w is not None else 1.0) + (b if b is not None and kind == "layer" else 0.0)
+
+
+def norm_bound(kind, v, dv, w, b, eps):
+    """How far norm(v) may be off in fp32 when v is off by dv."""
+    if kind == "none":
+        return dv
+    u = 80 * 2.0 ** -23
+    m = v.mean(1, keepdims=True) if kind == "layer" else 0.0
+    if kind == "layer":
+        dv = dv + u * np.abs(v).mean(1, keepdims=True) + 2.0 ** -23 * np.abs(v) + dv.mean(1, keepdims=True)
+    c = v - m
+    var = (c ** 2).mean(1, keepdims=True) + eps
+    r = 1 / np.sqrt(var)
+    dr = r * (u + np.sqrt((dv ** 2).mean(1, keepdims=True)) * r + (dv ** 2).mean(1, keepdims=True) / var)
+    aw = np.abs(w) if w is not None else 1.0
+    return (dv * r + np.abs(c) * dr + 4 * 2.0 ** -23 * np.abs(c) * r) * aw + (2.0 ** -23 * (np.abs(b) + np.abs(c) * r * aw) if b is not None else 0.0)
+
+
+def check_norm(nq, M, D, dtype="bf16", stream="bf16", post="rms", pre="rms", gate=None, out=("x", "q", "h"), vectors=True, branch=True,
+               pad=0, offset=0, in_place=False, seed=0, mean=0.0, rs=0.9, bs=0.7, eps=1e-5):
+    kinds = {"none": nq.NQ_NORM_NONE, "rms": nq.NQ_NORM_RMS, "layer": nq.NQ_NORM_LAYER}
+    h, y = floats((M, D), stream, seed), floats((M, D), dtype, seed + 1)
+    h, y = (h.float() + mean).to(h.dtype), (y.float() + mean).to(y.dtype)
+    g = floats((-(-M // gate), D), dtype, seed + 2, 0.2) if gate else None
+    vec = [torch.randn(D, generator=torch.Generator().manual_seed(seed + 10 + i)) for i in range(4)] if vectors else [None] * 4
+    cu = [v.cuda() if v is not None else None for v in vec]
+    ld = D + pad
+    hd, yd = strided(h, ld, offset), strided(y, ld, offset)
+    gd = strided(g, ld, offset) if gate else None
+    ho = None if "h" not in out else hd if in_place else strided(torch.zeros(M, D, dtype=TORCH[stream]), ld, offset)
+    xo = strided(torch.zeros(M, D, dtype=TORCH[dtype]), ld, offset) if "x" in out else None
+    c = Codes(nq, M, D, ld, offset) if "q" in out else None
+    job = nq.make_block_norm(hd, dt(nq, stream), ld, yd if branch else None, dt(nq, dtype), ld, gd, ld, gate or 0, rs, bs,
+                             nq.make_norm(kinds[post], eps, cu[0], cu[1]), nq.make_norm(kinds[pre], eps, cu[2], cu[3]), ho, ld, xo, ld,
+                             c.desc if c else None)
+    nq.nq_block_norm(job, M, D)
+    torch.cuda.synchronize()
+    n64 = [v.double().numpy() if v is not None else None for v in vec]
+    rs, bs = float(np.float32(rs)), float(np.float32(bs))
+    y64, h64 = y.double().numpy(), h.double().numpy()
+    p = norm64(post, y64, n64[0], n64[1], eps) if branch else np.zeros((M, D))
+    dp = norm_bound(post, y64, np.zeros((M, D)), n64[0], n64[1], eps) if branch else np.zeros((M, D))
+    gg = g.double().numpy()[np.arange(M) // gate] if gate else 1.0
+    hn = rs * h64 + bs * gg * p
+    dh = np.abs(bs * gg) * dp + 4 * 2.0 ** -23 * (np.abs(rs * h64) + np.abs(bs * gg * p))
+    x = norm64(pre, hn, n64[2], n64[3], eps)
+    dx = norm_bound(pre, hn, dh, n64[2], n64[3], eps)
+    if ho is not None:
+        assert (np.abs(ho.double().cpu().numpy() - hn) <= dh + HALF_UNIT[stream] * (np.abs(hn) + dh) + TINY[stream]).all()
+    if xo is not None:
+        assert (np.abs(xo.double().cpu().numpy() - x) <= dx + HALF_UNIT[dtype] * (np.abs(x) + dx) + TINY[dtype]).all()
+    if c is not None:
+        q, s = c.get()
+        for cb in range(blocks(D)):
+            at = np.s_[:, cb * 128:(cb + 1) * 128]
+            a, da = np.abs(x[at]).max(1), dx[at].max(1)
+            sc = s[:, cb].astype(np.float64)
+            assert (np.abs(sc * 448 - a) <= da + 2 * 2.0 ** -23 * a + 448 * 2.0 ** -126).all()
+            v = x[at] / sc[:, None]
+            spacing = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(v) * (1 + 2.0 ** -20), 2.0 ** -6))) - 3)
+            assert (np.abs(VALUES[q[at]] - v) <= spacing * 0.5 * (1 + 2.0 ** -20) + 2 * dx[at] / sc[:, None] + 448 * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("M,D", [(1, 1), (3, 2), (2, 127), (5, 128), (1, 512), (4, 520), (2, 1000), (3, 2048), (1, 2056), (2, 4096), (2, 5003),
+                                 (1, 8192), (2, 8200), (1, 16384), (2, 16392), (1, 20001), (1, 32768)])
+@pytest.mark.parametrize("post,pre", [("rms", "rms"), ("layer", "layer"), ("none", "rms")])
+def test_norm_sizes(nq, M, D, post, pre):
+    check_norm(nq, M, D, post=post, pre=pre, seed=D)
+
+
+@pytest.mark.parametrize("dtype,stream", [("f32", "f32"), ("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("D", [300, 1024])
+def test_norm_types(nq, dtype, stream, D):
+    check_norm(nq, 9, D, dtype, stream, "rms", "layer", gate=2)
+    check_norm(nq, 9, D, dtype, stream, "layer", "rms", gate=9, mean=3.0)
+    check_norm(nq, 9, D, dtype, stream, "layer", "none", gate=1)
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 1), (3, 0), (8, 8), (5, 3), (16, 16)])
+@pytest.mark.parametrize("D", [264, 17000])
+def test_norm_strides_and_alignment(nq, pad, offset, D):
+    check_norm(nq, 5, D, "bf16", "f32", gate=2, pad=pad, offset=offset)
+    check_norm(nq, 5, D, "f16", "f16", "layer", "layer", pad=pad, offset=offset, in_place=True)
+
+
+def test_norm_parts(nq):
+    """Without a branch, without weights, in place, with a single output of each kind, with nothing asked for."""
+    for out in (("x",), ("q",), ("h",), ("h", "q")):
+        check_norm(nq, 7, 640, out=out)
+        check_norm(nq, 7, 640, out=out, branch=False, post="layer", gate=3)
+        check_norm(nq, 7, 640, out=out, vectors=False, in_place=True)
+    check_norm(nq, 7, 17000, branch=False)
+    check_norm(nq, 7, 640, out=())
+    check_norm(nq, 300, 64, gate=1)
+    check_norm(nq, 300, 64, gate=299)
+
+
+@pytest.mark.parametrize("mean", [100.0, 3000.0])
+def test_layer_norm_far_from_zero(nq, mean):
+    """A mean far above the spread: the variance is not the difference of two large sums."""
+    check_norm(nq, 4, 1024, "f32", "f32", "none", "layer", mean=mean, bs=1e-3, out=("x",))
+
+
+def test_norm_not_finite(nq):
+    """A row with a NaN or an infinity is NaN, its neighbours are not touched by it."""
+    D = 1024
+    h, y = torch.randn(4, D, device="cuda"), torch.randn(4, D, device="cuda")
+    h[1, 7], y[2, 1000] = float("nan"), float("inf")
+    x, c = torch.empty(4, D, device="cuda"), Codes(nq, 4, D)
+    norm = nq.make_norm(nq.NQ_NORM_RMS)
+    nq.nq_block_norm(nq.make_block_norm(h, nq.NQ_DT_F32, D, y, nq.NQ_DT_F32, D, None, 0, 0, 1.0, 1.0, norm, norm, None, 0, x, D, c.desc), 4, D)
+    bad = torch.isnan(x).cpu()
+    assert bad[1].all() and bad[2, 1000] and not bad[0].any() and not bad[3].any()
+    q, s = c.get()
+    assert np.isnan(s[1]).all() and np.isfinite(s[0]).all() and np.isfinite(s[3]).all()
+
+
+# ---- all of them, as a layer uses them ------------------------------------------------------------------------
+
+def test_replayed_from_a_graph(nq):
+    """Norm -> product -> quantiser -> product, captured once and replayed beside eager work: every replay as the eager run."""
+    M, D, F = 24, 512, 1536
+    f = lambda *s: torch.randn(*s, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    up, down = nq.Fp8Matrix.from_float(f(F, D) * 0.05), nq.Fp8Matrix.from_float(f(D, F) * 0.03)
+    x, a = nq.Fp8Matrix(M, D), nq.Fp8Matrix(M, F)
+    h, h2, y, z, b = f(M, D), f(M, D), f(M, F), f(M, D), f(M, D)
+    bf, norm = nq.NQ_DT_BF16, nq.make_norm(nq.NQ_NORM_RMS)
+    job = nq.make_block_norm(h, bf, D, b, bf, D, None, 0, 0, 1.0, 1.0, norm, norm, h2, D, None, 0, x.desc)
+
+    def step():
+        nq.nq_block_norm(job, M, D)
+        nq.nq_gemm_fp8(x.desc, up.desc, None, y, bf, F)
+        nq.nq_quantize_fp8(y, bf, F, None, 0, nq.NQ_ACT_SILU, a.desc)
+        nq.nq_gemm_fp8(a.desc, down.desc, None, z, bf, D)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for i in range(4):
+        h.normal_()
+        b.normal_()
+        step()
+        torch.cuda.synchronize()
+        want = (h2.clone(), z.clone())
+        h2.zero_(), y.zero_(), z.zero_(), x.q.zero_(), a.q.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(h2, want[0]) and torch.equal(z, want[1]), i
