@@ -24,6 +24,7 @@ struct Fp8GemmParams {
     int64_t ldx, ldw, ldy, sxr, sxc, swr, swc;
     int M, N, K, KB;                       // KB: column blocks
     int y_vec;                             // four outputs may be stored at once
+    int sx_span;                           // bytes from the first scale of a tile's tokens to past the last (tiled kernel)
 };
 
 __device__ __forceinline__ f8_v8i fp8_frag(f8_v4i lo, f8_v4i hi)

@@ -1,5 +1,6 @@
 // nq_gemm_fp8: the kernels and the choice between them.  nq_fp8_gemm.h has the mathematics.
 #include "nq_fp8_gemm.h"
+#include "nq_fp8_gemm_tile.h"
 
 namespace nq {
 
@@ -76,8 +77,16 @@ __global__ void __launch_bounds__(256) k_fp8_gemm_any(const Fp8GemmParams p)
 }
 
 template <typename T>
-static void launch_gemm(const Fp8GemmParams &p, hipStream_t s)
+static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
+    // rows on 16 bytes, and scales that a buffer descriptor reaches
+    const int64_t span = (255 * p.sxr + (int64_t)std::max(0, p.KB - 1) * p.sxc + 1) * 4;
+    const bool tiled = aligned16(p.x) && aligned16(p.w) && p.ldx % 16 == 0 && p.ldw % 16 == 0 && span < (int64_t(1) << 30) && p.KB > 0;
+    if (tiled) {
+        p.sx_span = (int)span;
+        if constexpr (sizeof(T) == 4) return launch_tile<T, 128, 128, 64, 64, 1, 2, 2>(p, s);
+        else return launch_tile<T, 256, 256, 128, 64, 1, 2, 2>(p, s);
+    }
     k_fp8_gemm_any<T><<<(unsigned)(ceil_div(p.M, 64) * ceil_div(p.N, 64)), 256, 0, s>>>(p);
 }
 

@@ -1,0 +1,192 @@
+// The e4m3 matrix product for more than a few tokens: tiles of BN weight rows x BM tokens through LDS.
+//
+// Both operands travel global -> LDS directly (buffer loads with the LDS bit) into a ring of STAGES stages, each holding G
+// blocks of 128 columns of the tile's rows.  A wave-wide load writes 1024 contiguous bytes, eight rows; a row's eight 16-byte
+// pieces lie exchanged, piece c at c ^ ((row / 2) & 7): two rows are once round the 64 banks, and the same piece of sixteen
+// rows lies in sixteen different places.  Rows past the matrix's end, and pieces past a row's, are requested out of range and
+// arrive as zeros; the bytes past a row's end inside its last piece are cleared in LDS.  The waves are G groups of
+// (BN / WN) x (BM / WM); group g takes the column blocks g, g + G, ..., so that a tile has G times the waves where there are
+// too few tiles to fill the card, and the groups' sums are added in order at the end.
+#pragma once
+#include "nq_fp8_gemm.h"
+
+namespace nq {
+
+constexpr int F8_OOR = 0x7fff0000;                       // beyond every descriptor's range: moves no data
+
+// Tile number -> (tile row, tile column).  Workgroups are dealt to the eight XCDs in turn, and each XCD has an L2 of its own: it
+// gets a contiguous run of tiles, ordered in bands of eight tile rows so that what runs together shares both operands.
+__device__ __forceinline__ void f8_tile_of(int id, int rows, int cols, int &bm, int &bn)
+{
+    const int total = rows * cols, each = total >> 3, more = total & 7, xcd = id & 7, at = id >> 3;
+    const int t = xcd * each + min(xcd, more) + at;
+    const int band = t / (8 * cols), in_band = t - band * 8 * cols, height = min(8, rows - band * 8);
+    bn = in_band / height;
+    bm = band * 8 + in_band - bn * height;
+}
+
+template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC>
+__global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gemm_tile(const Fp8GemmParams p)
+{
+    constexpr bool WIDE = sizeof(T) == 4;
+    constexpr int WAVES_N = BN / WN, WAVES_M = BM / WM, GROUP = WAVES_N * WAVES_M, WAVES = G * GROUP;
+    constexpr int TN = WN / 16, TM = WM / 16;
+    constexpr int SX = (BM < 64 ? 64 : BM) * 4;          // bytes of a block's token scales
+    constexpr int KBYTES = (BN + BM) * 128, STAGE = G * (KBYTES + SX);
+    constexpr int LOADS = (BN + BM) / 8 / GROUP;         // loads of a wave and stage, of its own group's block
+    static_assert((BN / 8) % LOADS == 0 && (BM / 8) % LOADS == 0 && (BN + BM) / 8 % GROUP == 0, "a wave loads one operand");
+    static_assert(WN <= 128 && 128 % WN == 0, "a wave's weights share a scale");
+
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = wave / GROUP, in_group = wave - group * GROUP;
+    const int wn = (in_group % WAVES_N) * WN, wm = (in_group / WAVES_N) * WM;
+    const int r16 = lane & 15, g4 = lane >> 4;
+    int bm, bn;
+    f8_tile_of(blockIdx.x, (p.M + BM - 1) / BM, (p.N + BN - 1) / BN, bm, bn);
+    const int m0 = bm * BM, n0 = bn * BN;
+    const int iters = (p.KB + G - 1) / G;
+
+    // ---- what this wave loads: rows [8 * first, +8 * LOADS) of one operand ---------------------------------------
+    const bool tokens = in_group * LOADS >= BN / 8;
+    const int first = in_group * LOADS - (tokens ? BN / 8 : 0);
+    const int64_t ld = tokens ? p.ldx : p.ldw;
+    const int rows_here = tokens ? min(BM, p.M - m0) : min(BN, p.N - n0);
+    auto uniform_ptr = [](const void *q) {
+        const uint64_t a = reinterpret_cast<uint64_t>(q);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+        return reinterpret_cast<void *>(((uint64_t)hi << 32) | lo);
+    };
+    const __amdgpu_buffer_rsrc_t rows_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        uniform_ptr(tokens ? p.x + m0 * ld : p.w + n0 * ld), 0, __builtin_amdgcn_readfirstlane((int)(rows_here * ld)), 0x00020000);
+    int piece[2], voff[2];                               // rows of even and of odd loads
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        piece[i] = 16 * ((lane & 7) ^ ((4 * ((first + i) & 1) + (lane >> 4)) & 7));
+        voff[i] = (8 * first + (lane >> 3)) * (int)ld + piece[i];
+    }
+    // the token scales of the group's block: every wave asks for 64 of them (several waves for the same ones)
+    const int sx_at = (in_group % (SX / 256)) * 64 + lane;
+    const bool sx_in = sx_at < BM && m0 + sx_at < p.M;
+    const __amdgpu_buffer_rsrc_t sx_rsrc =
+        __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(p.sx + m0 * p.sxr), 0, __builtin_amdgcn_readfirstlane(p.sx_span), 0x00020000);
+    const int sx_off = sx_in ? sx_at * (int)p.sxr * 4 : F8_OOR;
+
+    auto issue = [&](int it, int stage) {
+        const int kb = it * G + group, k0 = kb * 128;
+        uint8_t *dst = lds + stage * STAGE + group * (KBYTES + SX) + (tokens ? BN * 128 : 0) + first * 1024;
+        int v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = k0 + piece[i] < p.K ? voff[i] + k0 : F8_OOR;
+        // (the whole offset in the lane's register: the range check takes the scalar offset from the range, and would wrap where that
+        // alone is past the end)
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows_rsrc, (lds_ptr)(dst + j * 1024), 16, v[j & 1] + j * 8 * (int)ld, 0, 0, 0);
+        uint8_t *sx = lds + stage * STAGE + group * (KBYTES + SX) + KBYTES + (in_group % (SX / 256)) * 256;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)sx, 4, kb < p.KB ? sx_off + kb * (int)p.sxc * 4 : F8_OOR, 0, 0, 0);
+    };
+
+    // ---- the product -----------------------------------------------------------------------------------------
+    f8_f4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f8_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int s8 = (r16 >> 1) & 7;
+    const int at_lo = r16 * 128 + 16 * (g4 ^ s8), at_hi = r16 * 128 + 16 * ((g4 + 4) ^ s8);
+    const float *sw_row = p.sw + (int64_t)((n0 + wn) >> 7) * p.swr;
+    if (n0 + wn >= p.N) sw_row = p.sw;                   // (zeros times any scale: nothing of it is stored)
+
+    for (int s = 0; s < STAGES - 1; ++s) issue(s, s);
+    float sw = sw_row[(int64_t)min(group, p.KB - 1) * p.swc];
+    int stage = 0;
+    for (int it = 0; it < iters; ++it) {
+        // Loads complete in order and every iteration asks for as many (those past the end for nothing), so this many outstanding
+        // means that stage `it` has arrived.
+        constexpr int LEFT = (STAGES - 2) * (LOADS + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt((LEFT & 15) | (7 << 4) | (15 << 8) | ((LEFT >> 4) << 14));
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
+        if (p.K % 16 != 0 && it == iters - 1) {          // the last piece of a row ends before its sixteenth byte
+            const int last = (p.K & 127) >> 4;
+            for (int row = threadIdx.x; row < G * (BN + BM); row += 64 * WAVES) {
+                const int gr = row / (BN + BM), r = row - gr * (BN + BM);
+                if (it * G + gr != p.KB - 1) continue;
+                uint8_t *q = lds + stage * STAGE + gr * (KBYTES + SX) + r * 128 + 16 * (last ^ ((r >> 1) & 7));
+                for (int b = p.K & 15; b < 16; ++b) q[b] = 0;
+            }
+            __syncthreads();
+        }
+        const int ahead = stage == 0 ? STAGES - 1 : stage - 1;
+        issue(it + STAGES - 1, ahead);
+        const float sw_next = sw_row[(int64_t)min((it + 1) * G + group, p.KB - 1) * p.swc];
+
+        const uint8_t *wp = cur + wn * 128, *xp = cur + (BN + wm) * 128;
+        const float *sxp = reinterpret_cast<const float *>(cur + KBYTES) + wm + r16;
+        Fp8Operand<WIDE> x[TM];
+        float s[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            x[i].set(fp8_frag(*reinterpret_cast<const f8_v4i *>(xp + i * 2048 + at_lo), *reinterpret_cast<const f8_v4i *>(xp + i * 2048 + at_hi)));
+            s[i] = sxp[i * 16] * sw;
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            Fp8Operand<WIDE> w;
+            w.set(fp8_frag(*reinterpret_cast<const f8_v4i *>(wp + j * 2048 + at_lo), *reinterpret_cast<const f8_v4i *>(wp + j * 2048 + at_hi)));
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fp8_add(acc[i][j], fp8_mfma(w, x[i]), s[i]);
+        }
+        sw = sw_next;
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+
+    // every load has to have landed before its memory is used for something else
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
+    // ---- the groups' sums, one after the other -------------------------------------------------------------------
+    if constexpr (G > 1) {
+        __syncthreads();
+        f8_f4 *sum = reinterpret_cast<f8_f4 *>(lds);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                if (group > 0) sum[(((group - 1) * GROUP + in_group) * TM * TN + i * TN + j) * 64 + lane] = acc[i][j];
+        __syncthreads();
+        if (group > 0) return;
+        for (int g = 1; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] += sum[(((g - 1) * GROUP + in_group) * TM * TN + i * TN + j) * 64 + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fp8_store<T>(p, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + 4 * g4, acc[i][j]);
+}
+
+template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC>
+static void launch_tile(const Fp8GemmParams &p, hipStream_t s)
+{
+    constexpr int GROUP = (BN / WN) * (BM / WM);
+    constexpr int ring = STAGES * G * ((BN + BM) * 128 + (BM < 64 ? 64 : BM) * 4);
+    constexpr int sums = (G - 1) * GROUP * (WN / 16) * (WM / 16) * 1024;
+    constexpr int lds = ring > sums ? ring : sums;
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    auto k = k_fp8_gemm_tile<T, BN, BM, WN, WM, G, STAGES, OCC>;
+    static bool granted = false;
+    if (!granted) {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        granted = true;
+    }
+    k<<<(unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN)), 64 * G * GROUP, lds, s>>>(p);
+}
+
+}  // namespace nq
