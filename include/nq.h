@@ -425,10 +425,13 @@ nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, const void *d
 
 /* Y[m][n] = sum_b sx[m][b] * sw[n / 128][b] * (sum over the columns k of block b of x[m][k] * w[n][k]) + bias[n],
  * sums in fp32, rounded to `dtype` once.  x: block_rows 1; w: block_rows 128 (NQ_ERR_UNSUPPORTED otherwise);
- * x->cols == w->cols <= NQ_MAX_K, w->rows <= 2^31 (NQ_ERR_SHAPE).  d_bias: device fp32[w->rows] or NULL.
- * d_y: device [x->rows][w->rows] of `dtype`, rows ldy elements apart, aligned to its type.  From one row on: few
- * rows stream the weights, many are tiled; each output is summed in an order that its matrix's sizes alone fix, so
- * equal calls give equal bits.  No columns: Y = bias. */
+ * x->cols == w->cols <= NQ_MAX_K, w->rows <= 2^30 (NQ_ERR_SHAPE).  d_bias: device fp32[w->rows] or NULL.
+ * d_y: device [x->rows][w->rows] of `dtype`, rows ldy elements apart, aligned to its type.  Each output is
+ * summed in an order that the matrices' sizes and alignment alone fix, so equal calls give equal bits.  No columns:
+ * Y = bias.
+ * fp32 outputs are as exact as fp32 sums are.  16-bit outputs are made by the fp8 matrix instructions, which cut a
+ * product off about 14 bits below the largest one added with it: 1.4e-5 of the result (2-norm) on codes of
+ * normally distributed values, against 2e-4 (f16) and 1.7e-3 (bf16) that rounding the outputs costs. */
 nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *d_bias, void *d_y, int dtype, int64_t ldy,
                       void *stream);
 

@@ -24,6 +24,7 @@ struct Fp8GemmParams {
     int64_t ldx, ldw, ldy, sxr, sxc, swr, swc;
     int M, N, K, KB;                       // KB: column blocks
     int y_vec;                             // four outputs may be stored at once
+    int y_16;                              // every row of the outputs starts on 16 bytes
     int sx_span;                           // bytes from the first scale of a tile's tokens to past the last (tiled kernel)
 };
 
@@ -108,6 +109,68 @@ __device__ __forceinline__ void fp8_store(const Fp8GemmParams &p, int m, int n, 
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i < left) from_float(v[i], y + i);
+    }
+}
+
+// A wave's 16 * TM tokens x 16 * TN outputs from token m and output n on.  The matrix core leaves a token's outputs in pieces of
+// four per lane: stored like that a wave's store would touch sixteen rows with 32 bytes each (a tile of 256 x 256 took 12 us).  They go
+// through LDS instead, `mine` being 16 * TM * TN * 16 elements that no other wave uses, and leave as whole rows, 16 bytes per lane.
+// The 16-byte units of a row lie exchanged so that sixteen rows' equal units, which one write covers, lie in different banks.
+template <typename T, int TN, int TM>
+__device__ __forceinline__ void fp8_store_tile(const Fp8GemmParams &p, int m, int n, f8_f4 (&acc)[TM][TN], uint8_t *mine, int lane)
+{
+    const int r16 = lane & 15, g4 = lane >> 4;
+    if (!p.y_16) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fp8_store<T>(p, m + i * 16 + r16, n + j * 16 + 4 * g4, acc[i][j]);
+        return;
+    }
+    constexpr int ROW = TN * 16 * (int)sizeof(T), UNITS = ROW / 16, E = 16 / (int)sizeof(T);
+    constexpr int MASK = UNITS < 16 ? UNITS - 1 : 15, SHARE = UNITS < 16 ? 16 / UNITS : 1;      // rows that lie once round the banks
+    auto place = [](int row, int unit) { return row * ROW + 16 * (unit ^ ((row / SHARE) & MASK)); };
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        f8_f4 b = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.bias) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (n + j * 16 + 4 * g4 + q < p.N) b[q] = p.bias[n + j * 16 + 4 * g4 + q];
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const f8_f4 v = p.bias ? acc[i][j] + b : acc[i][j];
+            if constexpr (sizeof(T) == 4) {
+                *reinterpret_cast<f8_f4 *>(mine + place(i * 16 + r16, j * 4 + g4)) = v;
+            } else {
+                T o[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) from_float(v[q], o + q);
+                *reinterpret_cast<uint2 *>(mine + place(i * 16 + r16, j * 2 + (g4 >> 1)) + 8 * (g4 & 1)) = __builtin_bit_cast(uint2, o);
+            }
+        }
+    }
+    // (the hardware keeps a wave's writes and reads of LDS in order; the compiler, which sees other types in them, has to be told)
+    asm volatile("" ::: "memory");
+    constexpr int AT_ONCE = 64 / UNITS;                    // rows of a store
+    const int unit = lane % UNITS, col = n + unit * E;
+#pragma unroll
+    for (int i = 0; i < (16 * TM + AT_ONCE - 1) / AT_ONCE; ++i) {
+        const int row = i * AT_ONCE + lane / UNITS;
+        if (16 * TM < AT_ONCE && row >= 16 * TM) return;
+        const uint4 v = *reinterpret_cast<const uint4 *>(mine + place(row, unit));
+        if (m + row >= p.M || col >= p.N) continue;
+        T *y = static_cast<T *>(p.y) + (int64_t)(m + row) * p.ldy + col;
+        if (col + E <= p.N) {
+            *reinterpret_cast<uint4 *>(y) = v;
+        } else {
+            T e[E];
+            __builtin_memcpy(e, &v, 16);
+#pragma unroll
+            for (int q = 0; q < E; ++q)
+                if (col + q < p.N) y[q] = e[q];
+        }
     }
 }
 

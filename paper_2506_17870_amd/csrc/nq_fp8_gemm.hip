@@ -1,5 +1,4 @@
 // nq_gemm_fp8: the kernels and the choice between them.  nq_fp8_gemm.h has the mathematics.
-#include "nq_fp8_gemm.h"
 #include "nq_fp8_gemm_tile.h"
 
 namespace nq {
@@ -77,17 +76,77 @@ __global__ void __launch_bounds__(256) k_fp8_gemm_any(const Fp8GemmParams p)
 }
 
 template <typename T>
+static void launch_any(const Fp8GemmParams &p, hipStream_t s)
+{
+    k_fp8_gemm_any<T><<<(unsigned)(ceil_div(p.M, 64) * ceil_div(p.N, 64)), 256, 0, s>>>(p);
+}
+
+// ---- which tile ------------------------------------------------------------------------------------------------
+// What a tile form takes, in microseconds, fitted to launches of 90 (fp32 outputs: 40) random sizes from 1 x 100 x 100 to 8192^3:
+// start + a round of tiles, `occ` to a compute unit, for each 256 * occ of them: per_tile + it * per_step, either with a part
+// that grows with the round's share of occupied units; it: steps of G column blocks.  The form with the least is taken: on those
+// sizes 1.0 % (0.5 %) slower than the fastest of sixteen forms timed for each, 10 % at worst.
+struct Fp8Form {
+    int BN, BM, G, occ;
+    float start, tile, tile_full, step, step_full;
+};
+
+static double form_time(const Fp8Form &f, int M, int N, int KB)
+{
+    const int64_t tiles = ceil_div(M, f.BM) * ceil_div(N, f.BN), slots = 256 * f.occ, rounds = tiles / slots, rest = tiles % slots;
+    const double it = (double)ceil_div(KB, f.G);
+    auto round = [&](double load) { return f.tile + f.tile_full * load + it * (f.step + f.step_full * load); };
+    return f.start + rounds * round(1.0) + (rest ? round((double)rest / slots) : 0.0);
+}
+
+// Few tokens: small tiles with many waves along the columns, two or four tiles to a unit: the weights stream (1 x 8192 x 8192 12.5 us,
+// 5.4 TB/s).  Some hundred: the largest tile of which there are still 256.  Many: tiles of 256 x 256 (16-bit outputs, 8192^3
+// 2.2 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
+// its loads 2.7); fp32 outputs need the registers for their wider operands and stay at 128 x 128.
+static const Fp8Form FORMS_16[] = {
+    {16, 16, 4, 4, 2.12f, 0.00f, 1.03f, 0.311f, 0.465f},   {16, 16, 8, 2, 2.03f, 0.30f, 0.88f, 0.453f, 0.425f},
+    {32, 32, 8, 1, 1.42f, 2.14f, 0.00f, 0.743f, 0.375f},   {64, 32, 4, 1, 1.19f, 2.52f, 0.00f, 0.655f, 0.279f},
+    {64, 64, 2, 2, 0.69f, 2.15f, 1.30f, 0.615f, 0.462f},   {128, 64, 1, 2, 0.00f, 2.93f, 2.01f, 0.557f, 0.300f},
+    {128, 128, 2, 1, 0.00f, 4.38f, 1.74f, 1.011f, 0.477f}, {128, 128, 1, 2, 0.00f, 3.30f, 4.28f, 0.720f, 0.597f},
+    {256, 256, 1, 1, 0.00f, 4.92f, 9.04f, 1.511f, 0.741f}};
+static const Fp8Form FORMS_32[] = {
+    {16, 16, 4, 4, 2.14f, 0.05f, 1.27f, 0.400f, 0.366f},   {16, 16, 8, 2, 1.90f, 0.68f, 0.76f, 0.543f, 0.315f},
+    {32, 32, 8, 1, 1.22f, 2.58f, 0.00f, 0.889f, 0.103f},   {64, 32, 4, 1, 1.28f, 2.56f, 0.54f, 0.858f, 0.002f},
+    {64, 64, 2, 2, 2.99f, 0.00f, 3.09f, 0.814f, 0.327f},   {128, 64, 1, 2, 2.99f, 0.07f, 5.99f, 0.807f, 0.227f},
+    {0, 0, 0, 0, 0, 0, 0, 0, 0},                            {128, 128, 1, 2, 0.00f, 3.53f, 7.30f, 1.268f, 0.457f}};
+
+template <typename T>
 static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
-    // rows on 16 bytes, and scales that a buffer descriptor reaches
-    const int64_t span = (255 * p.sxr + (int64_t)std::max(0, p.KB - 1) * p.sxc + 1) * 4;
-    const bool tiled = aligned16(p.x) && aligned16(p.w) && p.ldx % 16 == 0 && p.ldw % 16 == 0 && span < (int64_t(1) << 30) && p.KB > 0;
-    if (tiled) {
-        p.sx_span = (int)span;
-        if constexpr (sizeof(T) == 4) return launch_tile<T, 128, 128, 64, 64, 1, 2, 2>(p, s);
-        else return launch_tile<T, 256, 256, 128, 64, 1, 2, 2>(p, s);
+    constexpr bool F32 = sizeof(T) == 4;
+    const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
+    const int count = F32 ? 8 : 9;
+    int best = 0;
+    double least = 1e300;
+    for (int i = 0; i < count; ++i) {
+        if (forms[i].BN == 0) continue;
+        const double t = form_time(forms[i], p.M, p.N, p.KB);
+        if (t < least) {
+            least = t;
+            best = i;
+        }
     }
-    k_fp8_gemm_any<T><<<(unsigned)(ceil_div(p.M, 64) * ceil_div(p.N, 64)), 256, 0, s>>>(p);
+    switch (best) {
+    case 0: return launch_tile<T, 16, 16, 16, 16, 4, 2, 1>(p, s);
+    case 1: return launch_tile<T, 16, 16, 16, 16, 8, 2, 2>(p, s);
+    case 2: return launch_tile<T, 32, 32, 32, 16, 8, 2, 4>(p, s);
+    case 3: return launch_tile<T, 64, 32, 32, 16, 4, 3, 4>(p, s);
+    case 4: return launch_tile<T, 64, 64, 32, 32, 2, 2, 2>(p, s);
+    case 5: return launch_tile<T, 128, 64, 64, 32, 1, 3, 2>(p, s);
+    case 7: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2>(p, s);
+    default: break;
+    }
+    if constexpr (!F32) {
+        if (best == 6)
+            launch_tile<T, 128, 128, 64, 32, 2, 2, 4>(p, s);
+        else
+            launch_tile<T, 256, 256, 128, 64, 1, 2, 2>(p, s);
+    }
 }
 
 }  // namespace nq
@@ -101,7 +160,7 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     nq_status st;
     if ((st = check_fp8(x)) != NQ_OK || (st = check_fp8(w)) != NQ_OK) return st;
     if (x->block_rows != 1 || w->block_rows != 128) return NQ_ERR_UNSUPPORTED;
-    if (x->cols != w->cols || w->rows > (int64_t(1) << 31) - 128) return NQ_ERR_SHAPE;
+    if (x->cols != w->cols || w->rows > (int64_t(1) << 30)) return NQ_ERR_SHAPE;
     if (x->rows == 0 || w->rows == 0) return NQ_OK;
     if ((st = check_matrix(d_y, dtype, w->rows, ldy)) != NQ_OK) return st;
     if (!aligned_to(d_bias, 4)) return NQ_ERR_ALIGN;
@@ -122,19 +181,24 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     p.KB = (p.K + 127) / 128;
     const int es = dtype_bytes(dtype);
     p.y_vec = aligned_to(d_y, 4 * es) && ldy % 4 == 0;
-    // at most 2^30 tiles of 64 x 64 to a launch
-    const int64_t step = std::max<int64_t>(1, (int64_t(1) << 30) / ceil_div(p.N, 64)) * 64;
-    for (int64_t m = 0; m < x->rows; m += std::min<int64_t>(step, 1 << 30)) {
-        p.M = (int)std::min<int64_t>(std::min<int64_t>(step, 1 << 30), x->rows - m);
+    p.y_16 = aligned16(d_y) && ldy * es % 16 == 0;
+    // The tiles need rows on 16 bytes and scales that a buffer descriptor reaches from a tile's first token on.
+    const int64_t span = (255 * p.sxr + (int64_t)std::max(0, p.KB - 1) * p.sxc + 1) * 4;
+    const bool tiled = p.KB > 0 && aligned16(x->d_q) && aligned16(w->d_q) && x->ld % 16 == 0 && w->ld % 16 == 0 && span < (int64_t(1) << 30);
+    p.sx_span = tiled ? (int)span : 0;
+    // at most 2^30 tiles of 16 x 16, and 2^24 rows, to a launch (whole tiles of every form)
+    const int64_t step = std::min<int64_t>(1 << 24, std::max<int64_t>(16, (int64_t(1) << 30) / ceil_div(p.N, 16)) * 16);
+    for (int64_t m = 0; m < x->rows; m += step) {
+        p.M = (int)std::min<int64_t>(step, x->rows - m);
         p.x = x->d_q ? x->d_q + m * x->ld : nullptr;
         p.sx = x->d_scale ? x->d_scale + m * x->scale_row_step : nullptr;
         p.y = static_cast<uint8_t *>(d_y) + m * ldy * es;
         if (dtype == NQ_DT_F32)
-            launch_gemm<float>(p, (hipStream_t)stream);
+            tiled ? launch_gemm<float>(p, (hipStream_t)stream) : launch_any<float>(p, (hipStream_t)stream);
         else if (dtype == NQ_DT_F16)
-            launch_gemm<_Float16>(p, (hipStream_t)stream);
+            tiled ? launch_gemm<_Float16>(p, (hipStream_t)stream) : launch_any<_Float16>(p, (hipStream_t)stream);
         else
-            launch_gemm<bf16_t>(p, (hipStream_t)stream);
+            tiled ? launch_gemm<bf16_t>(p, (hipStream_t)stream) : launch_any<bf16_t>(p, (hipStream_t)stream);
         if ((st = launch_status()) != NQ_OK) return st;
     }
     return NQ_OK;

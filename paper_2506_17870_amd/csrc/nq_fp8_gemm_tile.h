@@ -1,4 +1,4 @@
-// The e4m3 matrix product for more than a few tokens: tiles of BN weight rows x BM tokens through LDS.
+// The e4m3 matrix product: tiles of BN weight rows x BM tokens through LDS.
 //
 // Both operands travel global -> LDS directly (buffer loads with the LDS bit) into a ring of STAGES stages, each holding G
 // blocks of 128 columns of the tile's rows.  A wave-wide load writes 1024 contiguous bytes, eight rows; a row's eight 16-byte
@@ -12,7 +12,7 @@
 
 namespace nq {
 
-constexpr int F8_OOR = 0x7fff0000;                       // beyond every descriptor's range: moves no data
+constexpr uint32_t F8_OOR = 0x7fff0000;                  // beyond every descriptor's range: reads as zeros
 
 // Tile number -> (tile row, tile column).  Workgroups are dealt to the eight XCDs in turn, and each XCD has an L2 of its own: it
 // gets a contiguous run of tiles, ordered in bands of eight tile rows so that what runs together shares both operands.
@@ -33,8 +33,8 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     constexpr int TN = WN / 16, TM = WM / 16;
     constexpr int SX = (BM < 64 ? 64 : BM) * 4;          // bytes of a block's token scales
     constexpr int KBYTES = (BN + BM) * 128, STAGE = G * (KBYTES + SX);
-    constexpr int LOADS = (BN + BM) / 8 / GROUP;         // loads of a wave and stage, of its own group's block
-    static_assert((BN / 8) % LOADS == 0 && (BM / 8) % LOADS == 0 && (BN + BM) / 8 % GROUP == 0, "a wave loads one operand");
+    constexpr int LOADS_W = BN / 8 / GROUP, LOADS_X = BM / 8 / GROUP;    // loads of a wave and stage, of its own group's block
+    static_assert(LOADS_W * GROUP * 8 == BN && LOADS_X * GROUP * 8 == BM, "the waves of a group share its loads evenly");
     static_assert(WN <= 128 && 128 % WN == 0, "a wave's weights share a scale");
 
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -49,44 +49,54 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     const int m0 = bm * BM, n0 = bn * BN;
     const int iters = (p.KB + G - 1) / G;
 
-    // ---- what this wave loads: rows [8 * first, +8 * LOADS) of one operand ---------------------------------------
-    const bool tokens = in_group * LOADS >= BN / 8;
-    const int first = in_group * LOADS - (tokens ? BN / 8 : 0);
-    const int64_t ld = tokens ? p.ldx : p.ldw;
-    const int rows_here = tokens ? min(BM, p.M - m0) : min(BN, p.N - n0);
+    // ---- what this wave loads: rows [8 * LOADS_* * in_group, + 8 * LOADS_*) of either operand ---------------------
     auto uniform_ptr = [](const void *q) {
         const uint64_t a = reinterpret_cast<uint64_t>(q);
         const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
         return reinterpret_cast<void *>(((uint64_t)hi << 32) | lo);
     };
-    const __amdgpu_buffer_rsrc_t rows_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-        uniform_ptr(tokens ? p.x + m0 * ld : p.w + n0 * ld), 0, __builtin_amdgcn_readfirstlane((int)(rows_here * ld)), 0x00020000);
-    int piece[2], voff[2];                               // rows of even and of odd loads
+    const int ldw = (int)p.ldw, ldx = (int)p.ldx;
+    const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        uniform_ptr(p.w + n0 * p.ldw), 0, __builtin_amdgcn_readfirstlane(min(BN, p.N - n0) * ldw), 0x00020000);
+    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        uniform_ptr(p.x + m0 * p.ldx), 0, __builtin_amdgcn_readfirstlane(min(BM, p.M - m0) * ldx), 0x00020000);
+    const int first_w = in_group * LOADS_W, first_x = in_group * LOADS_X;
+    int piece_w[2], piece_x[2];                          // even and odd loads
+    uint32_t off_w[2], off_x[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        piece[i] = 16 * ((lane & 7) ^ ((4 * ((first + i) & 1) + (lane >> 4)) & 7));
-        voff[i] = (8 * first + (lane >> 3)) * (int)ld + piece[i];
+        piece_w[i] = 16 * ((lane & 7) ^ ((4 * ((first_w + i) & 1) + (lane >> 4)) & 7));
+        piece_x[i] = 16 * ((lane & 7) ^ ((4 * ((first_x + i) & 1) + (lane >> 4)) & 7));
+        off_w[i] = (8 * first_w + (lane >> 3)) * ldw + piece_w[i];
+        off_x[i] = (8 * first_x + (lane >> 3)) * ldx + piece_x[i];
     }
     // the token scales of the group's block: every wave asks for 64 of them (several waves for the same ones)
     const int sx_at = (in_group % (SX / 256)) * 64 + lane;
     const bool sx_in = sx_at < BM && m0 + sx_at < p.M;
     const __amdgpu_buffer_rsrc_t sx_rsrc =
         __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(p.sx + m0 * p.sxr), 0, __builtin_amdgcn_readfirstlane(p.sx_span), 0x00020000);
-    const int sx_off = sx_in ? sx_at * (int)p.sxr * 4 : F8_OOR;
+    const uint32_t sx_off = sx_in ? (uint32_t)sx_at * (uint32_t)p.sxr * 4u : F8_OOR;
 
+    // (the whole offset in the lane's register: the range check takes the scalar offset from the range, and would wrap where that
+    // alone is past the end)
+    constexpr int PER_STAGE = LOADS_W + LOADS_X + 1;
     auto issue = [&](int it, int stage) {
         const int kb = it * G + group, k0 = kb * 128;
-        uint8_t *dst = lds + stage * STAGE + group * (KBYTES + SX) + (tokens ? BN * 128 : 0) + first * 1024;
-        int v[2];
+        uint8_t *dst = lds + stage * STAGE + group * (KBYTES + SX);
+        uint32_t vw[2], vx[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v[i] = k0 + piece[i] < p.K ? voff[i] + k0 : F8_OOR;
-        // (the whole offset in the lane's register: the range check takes the scalar offset from the range, and would wrap where that
-        // alone is past the end)
+        for (int i = 0; i < 2; ++i) {
+            vw[i] = k0 + piece_w[i] < p.K ? off_w[i] + k0 : F8_OOR;
+            vx[i] = k0 + piece_x[i] < p.K ? off_x[i] + k0 : F8_OOR;
+        }
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows_rsrc, (lds_ptr)(dst + j * 1024), 16, v[j & 1] + j * 8 * (int)ld, 0, 0, 0);
-        uint8_t *sx = lds + stage * STAGE + group * (KBYTES + SX) + KBYTES + (in_group % (SX / 256)) * 256;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)sx, 4, kb < p.KB ? sx_off + kb * (int)p.sxc * 4 : F8_OOR, 0, 0, 0);
+        for (int j = 0; j < LOADS_W; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(dst + (first_w + j) * 1024), 16, (int)(vw[j & 1] + j * 8 * ldw), 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < LOADS_X; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(dst + BN * 128 + (first_x + j) * 1024), 16, (int)(vx[j & 1] + j * 8 * ldx), 0, 0, 0);
+        uint8_t *sx = dst + KBYTES + (in_group % (SX / 256)) * 256;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)sx, 4, (int)(kb < p.KB ? sx_off + (uint32_t)kb * (uint32_t)p.sxc * 4u : F8_OOR), 0, 0, 0);
     };
 
     // ---- the product -----------------------------------------------------------------------------------------
@@ -102,43 +112,44 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
 
     for (int s = 0; s < STAGES - 1; ++s) issue(s, s);
     float sw = sw_row[(int64_t)min(group, p.KB - 1) * p.swc];
+    const int cut_it = p.K % 16 != 0 && (p.KB - 1) % G == group ? (p.KB - 1) / G : -1;
     int stage = 0;
     for (int it = 0; it < iters; ++it) {
         // Loads complete in order and every iteration asks for as many (those past the end for nothing), so this many outstanding
-        // means that stage `it` has arrived.
-        constexpr int LEFT = (STAGES - 2) * (LOADS + 1);
+        // means that this wave's rows of stage `it` have arrived.  Where the last piece of a row ends before its sixteenth byte, the
+        // wave that loaded it clears what is behind.
+        constexpr int LEFT = (STAGES - 2) * PER_STAGE;
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt((LEFT & 15) | (7 << 4) | (15 << 8) | ((LEFT >> 4) << 14));
-        __syncthreads();
-        __builtin_amdgcn_sched_barrier(0);
         uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
-        if (p.K % 16 != 0 && it == iters - 1) {          // the last piece of a row ends before its sixteenth byte
-            const int last = (p.K & 127) >> 4;
-            for (int row = threadIdx.x; row < G * (BN + BM); row += 64 * WAVES) {
-                const int gr = row / (BN + BM), r = row - gr * (BN + BM);
-                if (it * G + gr != p.KB - 1) continue;
-                uint8_t *q = lds + stage * STAGE + gr * (KBYTES + SX) + r * 128 + 16 * (last ^ ((r >> 1) & 7));
+        if (it == cut_it) {
+            for (int i = lane; i < 8 * (LOADS_W + LOADS_X); i += 64) {
+                const int r = i < 8 * LOADS_W ? 8 * first_w + i : BN + 8 * first_x + i - 8 * LOADS_W;
+                uint8_t *q = cur + r * 128 + 16 * (((p.K & 127) >> 4) ^ ((r >> 1) & 7));
                 for (int b = p.K & 15; b < 16; ++b) q[b] = 0;
             }
-            __syncthreads();
         }
-        const int ahead = stage == 0 ? STAGES - 1 : stage - 1;
-        issue(it + STAGES - 1, ahead);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        issue(it + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
         const float sw_next = sw_row[(int64_t)min((it + 1) * G + group, p.KB - 1) * p.swc];
 
         const uint8_t *wp = cur + wn * 128, *xp = cur + (BN + wm) * 128;
         const float *sxp = reinterpret_cast<const float *>(cur + KBYTES) + wm + r16;
+        auto frag = [&](const uint8_t *rows) {
+            return fp8_frag(*reinterpret_cast<const f8_v4i *>(rows + at_lo), *reinterpret_cast<const f8_v4i *>(rows + at_hi));
+        };
         Fp8Operand<WIDE> x[TM];
         float s[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            x[i].set(fp8_frag(*reinterpret_cast<const f8_v4i *>(xp + i * 2048 + at_lo), *reinterpret_cast<const f8_v4i *>(xp + i * 2048 + at_hi)));
+            x[i].set(frag(xp + i * 2048));
             s[i] = sxp[i * 16] * sw;
         }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             Fp8Operand<WIDE> w;
-            w.set(fp8_frag(*reinterpret_cast<const f8_v4i *>(wp + j * 2048 + at_lo), *reinterpret_cast<const f8_v4i *>(wp + j * 2048 + at_hi)));
+            w.set(frag(wp + j * 2048));
 #pragma unroll
             for (int i = 0; i < TM; ++i) fp8_add(acc[i][j], fp8_mfma(w, x[i]), s[i]);
         }
@@ -150,8 +161,9 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
     // ---- the groups' sums, one after the other -------------------------------------------------------------------
+    __syncthreads();
+    constexpr int SUMS = (G - 1) * GROUP * TM * TN * 1024;
     if constexpr (G > 1) {
-        __syncthreads();
         f8_f4 *sum = reinterpret_cast<f8_f4 *>(lds);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -166,10 +178,7 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] += sum[(((g - 1) * GROUP + in_group) * TM * TN + i * TN + j) * 64 + lane];
     }
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) fp8_store<T>(p, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + 4 * g4, acc[i][j]);
+    fp8_store_tile<T, TN, TM>(p, m0 + wm, n0 + wn, acc, lds + SUMS + in_group * (TM * TN * 256 * (int)sizeof(T)), lane);
 }
 
 template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC>
@@ -178,7 +187,8 @@ static void launch_tile(const Fp8GemmParams &p, hipStream_t s)
     constexpr int GROUP = (BN / WN) * (BM / WM);
     constexpr int ring = STAGES * G * ((BN + BM) * 128 + (BM < 64 ? 64 : BM) * 4);
     constexpr int sums = (G - 1) * GROUP * (WN / 16) * (WM / 16) * 1024;
-    constexpr int lds = ring > sums ? ring : sums;
+    constexpr int last = sums + BN * BM * (int)sizeof(T);
+    constexpr int lds = ring > last ? ring : last;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     auto k = k_fp8_gemm_tile<T, BN, BM, WN, WM, G, STAGES, OCC>;
     static bool granted = false;
