@@ -86,29 +86,48 @@ __device__ __forceinline__ void float_to_raw(const float (&v)[8], Raw8<bf16_t> &
     r.a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
-// n (0..8) of eight neighbouring elements, the others as zeros.  VEC: p is 16-byte aligned.
-template <bool VEC, typename T>
-__device__ __forceinline__ Raw8<T> load8(const T *p, int n)
+// Elements c .. c + 7 of a row of D, those past its end as zeros.  The address need not be aligned to more than the type: the memory
+// system takes wide accesses anywhere.  A chunk that the row's end cuts off is read as the row's last eight elements and moved
+// down (one request, where a request per element would hold up the wave), in a row of fewer than eight by elements.
+// FULL: the chunk is known to lie within the row.
+template <bool FULL, typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *row, int c, int D)
 {
+    const int n = D - c;
     Raw8<T> r{};
-    if (VEC && n == 8) {
-        r = *reinterpret_cast<const Raw8<T> *>(p);
-    } else {
+    if (FULL || n >= 8) {
+        __builtin_memcpy(&r, row + c, sizeof r);
+    } else if (n > 0 && D >= 8) {
+        __builtin_memcpy(&r, row + D - 8, sizeof r);
+        constexpr int W = (int)sizeof(r) / 4, PER = W / 8 ? 1 : 2;           // dwords; elements per dword
+        uint32_t d[W];
+        __builtin_memcpy(d, &r, sizeof r);
+        const int down = 8 - n;
+#pragma unroll
+        for (int step = 4; step >= PER; step /= 2)
+#pragma unroll
+            for (int i = 0; i < W; ++i) d[i] = down & step ? (i + step / PER < W ? d[i + step / PER] : 0u) : d[i];
+        if (PER == 2 && (down & 1)) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) d[i] = __builtin_amdgcn_alignbit(i + 1 < W ? d[i + 1] : 0u, d[i], 16);
+        }
+        __builtin_memcpy(&r, d, sizeof r);
+    } else if (n > 0) {
         T e[8] = {};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) e[i] = p[i];
-        r = __builtin_bit_cast(Raw8<T>, e);
+            if (i < n) e[i] = row[c + i];
+        __builtin_memcpy(&r, e, sizeof r);
     }
     return r;
 }
-template <bool VEC, typename T>
+template <typename T>
 __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
 {
-    if (VEC && n == 8) {
+    if (n >= 8) {
         Raw8<T> r;
         float_to_raw(v, r);
-        *reinterpret_cast<Raw8<T> *>(p) = r;
+        __builtin_memcpy(p, &r, sizeof r);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -117,15 +136,22 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
 }
 
 // The scale of a block with largest magnitude a (its bits, so that a NaN, the largest pattern of all, wins every maximum),
-// and the factor of its codes.
+// and the factor of its codes.  Both quotients are the correctly rounded ones: an approximation good to a unit, and a step with the
+// remainder, which a fused multiply-add gives exactly (Markstein 1990); a compiler's division also scales for operands that
+// cannot occur here (s is between 2^-126 and 2^120), and there is one for every eight elements.
 __device__ __forceinline__ float fp8_scale(uint32_t a_bits, float *inverse)
 {
-    const float a = __builtin_bit_cast(float, a_bits);
-    float s = a / 448.0f;
-    s = s < 0x1p-126f ? 0x1p-126f : s;                    // (a NaN stays)
+    const float a = __builtin_bit_cast(float, a_bits), c = 1.0f / 448.0f;
+    float s = a * c;
+    s = fmaf(fmaf(-448.0f, s, a), c, s);
+    s = s < 0x1p-126f ? 0x1p-126f : s;
     s = a_bits == 0 ? 1.0f : s;
-    *inverse = 1.0f / s;
-    return s;
+    float y = __builtin_amdgcn_rcpf(s);
+    y = fmaf(fmaf(-s, y, 1.0f), y, y);
+    y = fmaf(fmaf(-s, y, 1.0f), y, y);
+    const bool finite = a_bits < 0x7f800000u;
+    *inverse = finite ? y : a_bits == 0x7f800000u ? 0.0f : a;             // 1 / infinity, 1 / NaN
+    return finite ? s : a;
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 
@@ -143,12 +169,10 @@ __device__ __forceinline__ uint2 fp8_codes(const float (&v)[8], float inverse)
     }
     return make_uint2(d[0], d[1]);
 }
-// VEC: p is 8-byte aligned
-template <bool VEC>
 __device__ __forceinline__ void store_codes(uint8_t *p, int n, uint2 c)
 {
-    if (VEC && n == 8) {
-        *reinterpret_cast<uint2 *>(p) = c;
+    if (n >= 8) {
+        __builtin_memcpy(p, &c, 8);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -156,12 +180,32 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int n, uint2 c)
     }
 }
 
-// The larger of the lanes' values over each 16 neighbouring lanes.
+// Reductions over sixteen neighbouring lanes by data-parallel moves: neighbours, pairs, halves of eight, halves of sixteen.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __builtin_bit_cast(float, dpp<CTRL>(__builtin_bit_cast(uint32_t, v))); }
+
 __device__ __forceinline__ uint32_t max16(uint32_t v)
 {
-#pragma unroll
-    for (int m = 1; m < 16; m *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, m));
-    return v;
+    v = max(v, dpp<0xB1>(v));
+    v = max(v, dpp<0x4E>(v));
+    v = max(v, dpp<0x141>(v));
+    return max(v, dpp<0x140>(v));
+}
+__device__ __forceinline__ float sum16(float v)
+{
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    return v + dpp<0x140>(v);
+}
+// ... and over the wave's 64, the same value in every lane.
+__device__ __forceinline__ float sum64(float v)
+{
+    const int r = __builtin_bit_cast(int, sum16(v));
+    auto row = [&](int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(r, lane)); };
+    return (row(0) + row(16)) + (row(32) + row(48));
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------

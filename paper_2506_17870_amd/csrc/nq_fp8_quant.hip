@@ -45,7 +45,7 @@ __device__ __forceinline__ uint32_t act_and_max(const Raw8<T> &x, const Raw8<T> 
 }
 
 // A scale for each 1 x 128: eight columns per thread, sixteen threads per block of columns.
-template <typename T, int ACT, bool MUL, bool VEC>
+template <typename T, int ACT, bool MUL>
 __global__ void __launch_bounds__(256) k_fp8_rows(const QuantParams p)
 {
     const uint32_t group = blockIdx.x * 16u + (threadIdx.x >> 4);
@@ -54,18 +54,18 @@ __global__ void __launch_bounds__(256) k_fp8_rows(const QuantParams p)
     const int64_t row = p.row0 + r;
     const int c = (int)b * 128 + (threadIdx.x & 15) * 8;
     const int n = min(8, max(0, p.K - c));
-    const Raw8<T> x = load8<VEC>(static_cast<const T *>(p.x) + row * p.ldx + c, n);
+    const Raw8<T> x = load8<false>(static_cast<const T *>(p.x) + row * p.ldx, c, p.K);
     Raw8<T> m{};
-    if constexpr (MUL) m = load8<VEC>(static_cast<const T *>(p.mul) + row * p.ldmul + c, n);
+    if constexpr (MUL) m = load8<false>(static_cast<const T *>(p.mul) + row * p.ldmul, c, p.K);
     float v[8], inverse;
     const uint32_t a = max16(act_and_max<ACT>(x, MUL ? &m : nullptr, v));
     const float s = fp8_scale(a, &inverse);
-    store_codes<VEC>(p.q + row * p.ldq + c, n, fp8_codes(v, inverse));
+    store_codes(p.q + row * p.ldq + c, n, fp8_codes(v, inverse));
     if ((threadIdx.x & 15) == 0) p.scale[row * p.srow + b * p.scol] = s;
 }
 
 // A scale for each 128 x 128: a workgroup per block, eight columns of each sixteenth row per thread.
-template <typename T, int ACT, bool MUL, bool VEC>
+template <typename T, int ACT, bool MUL>
 __global__ void __launch_bounds__(256) k_fp8_tiles(const QuantParams p)
 {
     __shared__ uint32_t largest[4];
@@ -77,9 +77,9 @@ __global__ void __launch_bounds__(256) k_fp8_tiles(const QuantParams p)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t row = p.row0 + r0 + 16 * i;
-        const int here = r0 + 16 * i < p.rows ? n : 0;
-        x[i] = load8<VEC>(static_cast<const T *>(p.x) + row * p.ldx + c, here);
-        if constexpr (MUL) m[i] = load8<VEC>(static_cast<const T *>(p.mul) + row * p.ldmul + c, here);
+        const int here = r0 + 16 * i < p.rows ? p.K : 0;    // (a row that is not there: no elements)
+        x[i] = load8<false>(static_cast<const T *>(p.x) + row * p.ldx, c, here);
+        if constexpr (MUL) m[i] = load8<false>(static_cast<const T *>(p.mul) + row * p.ldmul, c, here);
     }
     uint32_t a = 0;
     float v[8], inverse;
@@ -96,38 +96,32 @@ __global__ void __launch_bounds__(256) k_fp8_tiles(const QuantParams p)
         const int64_t row = p.row0 + r0 + 16 * i;
         const int here = r0 + 16 * i < p.rows ? n : 0;
         act_and_max<ACT>(x[i], MUL ? &m[i] : nullptr, v);
-        store_codes<VEC>(p.q + row * p.ldq + c, here, fp8_codes(v, inverse));
+        store_codes(p.q + row * p.ldq + c, here, fp8_codes(v, inverse));
     }
     if (threadIdx.x == 0) p.scale[(p.row0 / 128 + rb) * p.srow + b * p.scol] = s;
 }
 
 template <typename T, int ACT, bool MUL>
-static void launch_quant(const QuantParams &p, bool vec, int block_rows, hipStream_t s)
+static void launch_quant(const QuantParams &p, int block_rows, hipStream_t s)
 {
     if (block_rows == 1) {
         const dim3 grid((p.groups + 15) / 16);
-        if (vec)
-            k_fp8_rows<T, ACT, MUL, true><<<grid, 256, 0, s>>>(p);
-        else
-            k_fp8_rows<T, ACT, MUL, false><<<grid, 256, 0, s>>>(p);
+        k_fp8_rows<T, ACT, MUL><<<grid, 256, 0, s>>>(p);
     } else {
         const dim3 grid((p.rows + 127) / 128 * p.by_blocks.d);
-        if (vec)
-            k_fp8_tiles<T, ACT, MUL, true><<<grid, 256, 0, s>>>(p);
-        else
-            k_fp8_tiles<T, ACT, MUL, false><<<grid, 256, 0, s>>>(p);
+        k_fp8_tiles<T, ACT, MUL><<<grid, 256, 0, s>>>(p);
     }
 }
 
 template <typename T>
-static void launch_act(const QuantParams &p, int act, bool vec, int block_rows, hipStream_t s)
+static void launch_act(const QuantParams &p, int act, int block_rows, hipStream_t s)
 {
 #define NQ_QUANT_ACT(A)                                                   \
     case A:                                                               \
         if (p.mul)                                                        \
-            launch_quant<T, A, true>(p, vec, block_rows, s);              \
+            launch_quant<T, A, true>(p, block_rows, s);              \
         else                                                              \
-            launch_quant<T, A, false>(p, vec, block_rows, s);             \
+            launch_quant<T, A, false>(p, block_rows, s);             \
         break;
     switch (act) {
         NQ_QUANT_ACT(NQ_ACT_NONE)
@@ -167,18 +161,17 @@ extern "C" nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, co
     p.K = (int)q->cols;
     const uint32_t blocks = (uint32_t)ceil_div(q->cols, 128);
     p.by_blocks = make_divider(blocks);
-    const bool vec = rows_on_16(d_x, dtype, ldx) && rows_on_16(d_mul, dtype, ldmul) && aligned_to(q->d_q, 8) && q->ld % 8 == 0;
     // at most 2^30 blocks to a launch, whole blocks of 128 rows
     const int64_t step = std::max<int64_t>(128, (int64_t(1) << 30) / blocks / 128 * 128);
     for (p.row0 = 0; p.row0 < q->rows; p.row0 += step) {
         p.rows = (uint32_t)std::min(step, q->rows - p.row0);
         p.groups = p.rows * blocks;
         if (dtype == NQ_DT_F32)
-            launch_act<float>(p, act, vec, q->block_rows, (hipStream_t)stream);
+            launch_act<float>(p, act, q->block_rows, (hipStream_t)stream);
         else if (dtype == NQ_DT_F16)
-            launch_act<_Float16>(p, act, vec, q->block_rows, (hipStream_t)stream);
+            launch_act<_Float16>(p, act, q->block_rows, (hipStream_t)stream);
         else
-            launch_act<bf16_t>(p, act, vec, q->block_rows, (hipStream_t)stream);
+            launch_act<bf16_t>(p, act, q->block_rows, (hipStream_t)stream);
         if ((st = launch_status()) != NQ_OK) return st;
     }
     return NQ_OK;

@@ -485,3 +485,17 @@ def test_replayed_from_a_graph(nq):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(h2, want[0]) and torch.equal(z, want[1]), i
+
+
+# ragged sizes at which the library's choice is each of its tile forms
+FORM_SIZES = [(1, 23, 318), (1, 21, 376), (1, 23, 1596), (1, 20, 1653), (4083, 54, 532), (49, 3665, 553), (66, 4878, 305), (98, 3021, 313),
+              (49, 5471, 330), (2883, 132, 301), (3721, 341, 318), (2996, 688, 301), (325, 5668, 1961), (2307, 1700, 334), (2572, 1286, 316),
+              (2999, 2930, 40), (3999, 4001, 415)]
+
+
+@pytest.mark.parametrize("M,N,K", FORM_SIZES)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_gemm_every_tile_form(nq, M, N, K, out):
+    ld = dict(ld=-(-K // 16) * 16)
+    check_gemm(nq, M, N, K, out=out, exact=True, seed=K, x_kw=ld, w_kw=ld)
+    check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
