@@ -2,7 +2,7 @@
 benchmark).  Every kernel time is the begin/end time stamp of the dispatch itself; buffers are rotated so that
 activations and outputs come from HBM, not from the Infinity Cache.
 
-    python bench_configs.py [c1] [c2] [c3] [c4] [c5] [pack] [page] [sweep] [words] [dw] [lib] [cpu]
+    python bench_configs.py [c1] [c2] [c3] [c4] [c5] [pack] [page] [sweep] [words] [dw] [lib] [fp8] [cpu]
 """
 from __future__ import annotations
 
@@ -709,9 +709,31 @@ def words():
     conv("7x7 s2 224x224 3->64 word pages", 8, 224, 224, 3, 64, 7, 2, 3, 2, sets=2, layout=nq.NQ_LAYOUT_PAPER_U64)
 
 
+def fp8():
+    """The MLP blocks of a transformer on the fp8 operators: four blocks of D = 4096, gated, F = 8192."""
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    D, F, n = 4096, 8192, 4
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    mlp = Fp8Mlp([dict(up=rand(2 * F, D) * D ** -0.5, down=rand(D, F) * F ** -0.5, pre=1 + 0.1 * rand(D), post=1 + 0.1 * rand(D))
+                  for _ in range(n)], h_dtype=torch.float32)
+    print(f"\n### fp8 MLP blocks, D = {D}, gated, F = {F}, norm before and after, {n} blocks per pass (back-to-back passes, HIP graph)\n")
+    print("| tokens | us per block | TFLOP/s | weights GB/s |")
+    print("|---|---|---|---|")
+    for tokens in (1, 16, 64, 256, 1024, 4096):
+        mlp.allocate(tokens).h.normal_()
+        mlp.run()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            mlp.run()
+        us = wall_us(graph.replay, 50) / n
+        print(f"| {tokens} | {us:.1f} | {6.0 * tokens * D * F / us / 1e6:.0f} | {3 * D * F / us / 1e3:.0f} |")
+
+
 if __name__ == "__main__":
     torch.cuda.set_device(0)
-    which = sys.argv[1:] or ["c1", "c2", "c3", "c4", "c5", "pack", "page", "sweep", "words", "dw", "lib", "cpu"]
+    which = sys.argv[1:] or ["c1", "c2", "c3", "c4", "c5", "pack", "page", "sweep", "words", "dw", "lib", "fp8", "cpu"]
     for name in which:
-        {"c1": c1, "c2": c2, "c3": c3, "c4": c4, "c5": c5, "pack": pack, "page": page, "sweep": sweep, "dw": dw, "lib": lib, "cpu": cpu,
+        {"c1": c1, "c2": c2, "c3": c3, "c4": c4, "c5": c5, "pack": pack, "page": page, "sweep": sweep, "dw": dw, "lib": lib, "fp8": fp8, "cpu": cpu,
          "words": words}[name]()

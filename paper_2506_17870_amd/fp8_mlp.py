@@ -1,0 +1,88 @@
+"""The MLP blocks of a transformer on the fp8 operators, from one token to a long prompt; calls only the C ABI.
+
+A block is norm -> first layer -> activation -> second layer, and its output is the branch that the next norm adds to the
+residual stream.  Between two matrix products stands one launch each: nq_block_norm (norm of the last branch, gate, residual sum,
+norm, e4m3 codes) before the first layer, nq_quantize_fp8 (activation, product with the gated half, codes) before the second.
+Everything a forward pass writes is allocated by allocate(), so that it can be captured into a HIP graph.
+"""
+from __future__ import annotations
+
+import torch
+
+import paper_2506_17870_amd as nq
+
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}       # nq_dtype
+
+
+class Fp8Mlp:
+    """layers: sequence of dicts of float tensors on the device,
+        up      [F][D], or [2 F][D]: the rows that go through the activation first, then those it is multiplied with
+        down    [D][F]
+        pre     fp32 [D], weight of the RMS norm before the block
+        post    fp32 [D] or absent, weight of the RMS norm after it
+        gate    dtype [D] or absent, factors of the branch per channel
+    dtype: of branches and activations (the residual stream has h_dtype)."""
+
+    def __init__(self, layers, act=nq.NQ_ACT_SILU, dtype=torch.bfloat16, h_dtype=None, eps=1e-5, residual_scale=1.0, branch_scale=1.0):
+        self.act, self.dtype, self.h_dtype, self.eps = act, dtype, h_dtype or dtype, eps
+        self.residual_scale, self.branch_scale = residual_scale, branch_scale
+        self.layers = []
+        for L in layers:
+            D, F = L["down"].shape
+            if L["up"].shape[1] != D or L["up"].shape[0] not in (F, 2 * F):
+                raise ValueError(f"up {tuple(L['up'].shape)} does not fit down {tuple(L['down'].shape)}")
+            self.layers.append(dict(D=D, F=F, gated=L["up"].shape[0] == 2 * F, up=nq.Fp8Matrix.from_float(L["up"].contiguous()),
+                                    down=nq.Fp8Matrix.from_float(L["down"].contiguous()), pre=L["pre"], post=L.get("post"), gate=L.get("gate")))
+        if len({L["D"] for L in self.layers}) > 1:
+            raise ValueError("the layers differ in width")
+        self.tokens = None
+
+    def allocate(self, tokens: int):
+        """Buffers and descriptors for `tokens` tokens."""
+        self.tokens, self.D = tokens, self.layers[0]["D"]
+        dev = self.layers[0]["up"].q.device
+        self.x = nq.Fp8Matrix(tokens, self.D, device=dev)
+        self.h = torch.empty(tokens, self.D, dtype=self.h_dtype, device=dev)
+        self.branch = torch.empty(tokens, self.D, dtype=self.dtype, device=dev)
+        most = max(L["up"].rows for L in self.layers)
+        self.mid = torch.empty(tokens * most, dtype=self.dtype, device=dev)
+        self.a = {F: nq.Fp8Matrix(tokens, F, device=dev) for F in {L["F"] for L in self.layers}}
+        dt, hdt = _DTYPES[self.dtype], _DTYPES[self.h_dtype]
+        none = nq.make_norm(nq.NQ_NORM_NONE)
+        # norm i stands before layer i: it ends what layer i - 1 began
+        self.norms = []
+        for i, L in enumerate(self.layers + [None]):
+            last = self.layers[i - 1] if i else None
+            post = nq.make_norm(nq.NQ_NORM_RMS, self.eps, last["post"]) if last and last["post"] is not None else none
+            pre = nq.make_norm(nq.NQ_NORM_RMS, self.eps, L["pre"]) if L else none
+            gate = last["gate"] if last else None
+            self.norms.append(nq.make_block_norm(
+                self.h, hdt, self.D, self.branch if last else None, dt, self.D, gate, self.D, tokens if gate is not None else 0,
+                self.residual_scale if last else 1.0, self.branch_scale, post, pre, self.h if last else None, self.D, None, 0,
+                self.x.desc if L else None))
+        return self
+
+    def forward(self, h, stream=None):
+        """h: [tokens][D] of h_dtype.  Returns the stream behind the last block (a buffer of this object: the next forward
+        overwrites it)."""
+        if self.tokens != h.shape[0]:
+            self.allocate(h.shape[0])
+        if stream is None:
+            self.h.copy_(h)
+        else:
+            with torch.cuda.stream(stream):
+                self.h.copy_(h)
+        return self.run(stream)
+
+    def run(self, stream=None):
+        """The same on the stream that lies in self.h already."""
+        dt, es = _DTYPES[self.dtype], self.mid.element_size()
+        for L, norm in zip(self.layers, self.norms):
+            F, rows, a = L["F"], L["up"].rows, self.a[L["F"]]
+            nq.nq_block_norm(norm, self.tokens, self.D, stream)
+            nq.nq_gemm_fp8(self.x.desc, L["up"].desc, None, self.mid, dt, rows, stream)
+            mul = self.mid.data_ptr() + F * es if L["gated"] else None
+            nq.nq_quantize_fp8(self.mid, dt, rows, mul, rows, self.act, a.desc, stream)
+            nq.nq_gemm_fp8(a.desc, L["down"].desc, None, self.branch, dt, self.D, stream)
+        nq.nq_block_norm(self.norms[-1], self.tokens, self.D, stream)
+        return self.h
