@@ -82,10 +82,11 @@ static void launch_any(const Fp8GemmParams &p, hipStream_t s)
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
-// What a tile form takes, in microseconds, fitted to launches of 90 (fp32 outputs: 40) random sizes from 1 x 100 x 100 to 8192^3:
+// What a tile form takes, in microseconds, fitted to launches of 126 (fp32 outputs: 59) random sizes from 1 x 100 x 100 to 8192^3:
 // start + a round of tiles, `occ` to a compute unit, for each 256 * occ of them: per_tile + it * per_step, either with a part
 // that grows with the round's share of occupied units; it: steps of G column blocks.  The form with the least is taken: on those
-// sizes 1.0 % (0.5 %) slower than the fastest of sixteen forms timed for each, 10 % at worst.
+// sizes 1.0 % (0.7 %) slower than the fastest of fifteen forms timed for each, 17 % at worst (584 x 2560 x 128, 4 us), 12 % where
+// K is longer.
 struct Fp8Form {
     int BN, BM, G, occ;
     float start, tile, tile_full, step, step_full;
@@ -104,23 +105,24 @@ static double form_time(const Fp8Form &f, int M, int N, int KB)
 // 2.2 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
 // its loads 2.7); fp32 outputs need the registers for their wider operands and stay at 128 x 128.
 static const Fp8Form FORMS_16[] = {
-    {16, 16, 4, 4, 2.12f, 0.00f, 1.03f, 0.311f, 0.465f},   {16, 16, 8, 2, 2.03f, 0.30f, 0.88f, 0.453f, 0.425f},
-    {32, 32, 8, 1, 1.42f, 2.14f, 0.00f, 0.743f, 0.375f},   {64, 32, 4, 1, 1.19f, 2.52f, 0.00f, 0.655f, 0.279f},
-    {64, 64, 2, 2, 0.69f, 2.15f, 1.30f, 0.615f, 0.462f},   {128, 64, 1, 2, 0.00f, 2.93f, 2.01f, 0.557f, 0.300f},
-    {128, 128, 2, 1, 0.00f, 4.38f, 1.74f, 1.011f, 0.477f}, {128, 128, 1, 2, 0.00f, 3.30f, 4.28f, 0.720f, 0.597f},
-    {256, 256, 1, 1, 0.00f, 4.92f, 9.04f, 1.511f, 0.741f}};
+    {16, 16, 4, 4, 2.21f, 0.00f, 1.18f, 0.303f, 0.429f},   {16, 16, 8, 2, 2.23f, 0.26f, 1.03f, 0.403f, 0.415f},
+    {32, 32, 8, 1, 1.43f, 2.06f, 0.10f, 0.728f, 0.267f},   {64, 32, 4, 1, 1.44f, 2.20f, 0.43f, 0.601f, 0.106f},
+    {64, 64, 2, 2, 1.15f, 1.82f, 1.45f, 0.582f, 0.355f},   {128, 64, 2, 1, 0.00f, 3.79f, 0.99f, 0.736f, 0.044f},
+    {128, 128, 1, 1, 0.00f, 3.43f, 2.88f, 0.533f, 0.046f}, {128, 128, 1, 2, 0.00f, 3.46f, 6.49f, 0.635f, 0.455f},
+    {256, 128, 1, 1, 0.00f, 4.15f, 6.65f, 0.810f, 0.113f}, {256, 256, 1, 1, 0.00f, 5.19f, 13.49f, 1.282f, 0.304f}};
 static const Fp8Form FORMS_32[] = {
-    {16, 16, 4, 4, 2.14f, 0.05f, 1.27f, 0.400f, 0.366f},   {16, 16, 8, 2, 1.90f, 0.68f, 0.76f, 0.543f, 0.315f},
-    {32, 32, 8, 1, 1.22f, 2.58f, 0.00f, 0.889f, 0.103f},   {64, 32, 4, 1, 1.28f, 2.56f, 0.54f, 0.858f, 0.002f},
-    {64, 64, 2, 2, 2.99f, 0.00f, 3.09f, 0.814f, 0.327f},   {128, 64, 1, 2, 2.99f, 0.07f, 5.99f, 0.807f, 0.227f},
-    {0, 0, 0, 0, 0, 0, 0, 0, 0},                            {128, 128, 1, 2, 0.00f, 3.53f, 7.30f, 1.268f, 0.457f}};
+    {16, 16, 4, 4, 2.17f, 0.00f, 1.30f, 0.370f, 0.383f},   {16, 16, 8, 2, 1.94f, 0.61f, 0.85f, 0.480f, 0.341f},
+    {32, 32, 8, 1, 1.11f, 2.63f, 0.00f, 0.945f, 0.058f},   {64, 32, 4, 1, 1.49f, 2.29f, 0.66f, 0.885f, 0.028f},
+    {64, 64, 2, 2, 3.15f, 0.00f, 2.65f, 0.782f, 0.461f},   {0, 0, 0, 0, 0, 0, 0, 0, 0},
+    {128, 128, 1, 1, 2.24f, 1.35f, 4.58f, 0.977f, 0.016f}, {128, 128, 1, 2, 0.00f, 4.03f, 7.55f, 0.992f, 0.675f},
+    {256, 128, 1, 1, 0.00f, 4.67f, 7.70f, 1.512f, 0.063f}};
 
 template <typename T>
 static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
-    const int count = F32 ? 8 : 9;
+    const int count = F32 ? 9 : 10;
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < count; ++i) {
@@ -132,20 +134,21 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
         }
     }
     switch (best) {
-    case 0: return launch_tile<T, 16, 16, 16, 16, 4, 2, 1>(p, s);
-    case 1: return launch_tile<T, 16, 16, 16, 16, 8, 2, 2>(p, s);
-    case 2: return launch_tile<T, 32, 32, 32, 16, 8, 2, 4>(p, s);
-    case 3: return launch_tile<T, 64, 32, 32, 16, 4, 3, 4>(p, s);
-    case 4: return launch_tile<T, 64, 64, 32, 32, 2, 2, 2>(p, s);
-    case 5: return launch_tile<T, 128, 64, 64, 32, 1, 3, 2>(p, s);
-    case 7: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2>(p, s);
+    case 0: return launch_tile<T, 16, 16, 16, 16, 4, 2, 1, false>(p, s);
+    case 1: return launch_tile<T, 16, 16, 16, 16, 8, 2, 2, false>(p, s);
+    case 2: return launch_tile<T, 32, 32, 32, 16, 8, 2, 4, false>(p, s);
+    case 3: return launch_tile<T, 64, 32, 32, 16, 4, 3, 4, false>(p, s);
+    case 4: return launch_tile<T, 64, 64, 32, 32, 2, 2, 2, false>(p, s);
+    case 6: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
+    case 7: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2, true>(p, s);
+    case 8: return launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
     default: break;
     }
     if constexpr (!F32) {
-        if (best == 6)
-            launch_tile<T, 128, 128, 64, 32, 2, 2, 4>(p, s);
+        if (best == 5)
+            launch_tile<T, 128, 64, 32, 32, 2, 3, 2, false>(p, s);
         else
-            launch_tile<T, 256, 256, 128, 64, 1, 2, 2>(p, s);
+            launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
     }
 }
 

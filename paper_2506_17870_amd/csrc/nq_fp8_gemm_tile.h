@@ -7,6 +7,13 @@
 // arrive as zeros; the bytes past a row's end inside its last piece are cleared in LDS.  The waves are G groups of
 // (BN / WN) x (BM / WM); group g takes the column blocks g, g + G, ..., so that a tile has G times the waves where there are
 // too few tiles to fill the card, and the groups' sums are added in order at the end.
+//
+// AHEAD, for the large tiles: a step does not begin with its barrier but has it before its last fragment of weights, so that the
+// next step's first fragments are read while the matrix cores still work; the loads of the stage to come are issued one at a time
+// between the products (a burst of them holds the wave at the address unit); and four products are in flight, each one's multiply-adds
+// standing behind the third product after it.  8192^3 507 -> 483 us, 1024 x 8192 x 8192 89 -> 72 (its tile then 256 x 128, in
+// three stages), 2048^3 15.4 -> 14.7.  Small tiles have more waves and fewer products to a step, and are faster without: 64 x 64
+// at 256 x 4096 x 4096 13.6 against 17.3 us.
 #pragma once
 #include "nq_fp8_gemm.h"
 
@@ -25,7 +32,7 @@ __device__ __forceinline__ void f8_tile_of(int id, int rows, int cols, int &bm, 
     bm = band * 8 + in_band - bn * height;
 }
 
-template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC>
+template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC, bool AHEAD>
 __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gemm_tile(const Fp8GemmParams p)
 {
     constexpr bool WIDE = sizeof(T) == 4;
@@ -61,15 +68,15 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
         uniform_ptr(p.x + m0 * p.ldx), 0, __builtin_amdgcn_readfirstlane(min(BM, p.M - m0) * ldx), 0x00020000);
     const int first_w = in_group * LOADS_W, first_x = in_group * LOADS_X;
-    int piece_w[2], piece_x[2];                          // even and odd loads
-    uint32_t off_w[2], off_x[2];
+    // (where the loads come in pairs, those of either operand begin with an even one and share the exchange of pieces)
+    constexpr bool PAIRS = LOADS_W % 2 == 0 && LOADS_X % 2 == 0;
+    int piece_w[2], piece_x[2];                          // of the rows of even and of odd loads
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        piece_w[i] = 16 * ((lane & 7) ^ ((4 * ((first_w + i) & 1) + (lane >> 4)) & 7));
-        piece_x[i] = 16 * ((lane & 7) ^ ((4 * ((first_x + i) & 1) + (lane >> 4)) & 7));
-        off_w[i] = (8 * first_w + (lane >> 3)) * ldw + piece_w[i];
-        off_x[i] = (8 * first_x + (lane >> 3)) * ldx + piece_x[i];
+        piece_w[i] = 16 * ((lane & 7) ^ ((4 * ((PAIRS ? i : first_w + i) & 1) + (lane >> 4)) & 7));
+        piece_x[i] = PAIRS ? piece_w[i] : 16 * ((lane & 7) ^ ((4 * ((first_x + i) & 1) + (lane >> 4)) & 7));
     }
+    const uint32_t row_w = (8 * first_w + (lane >> 3)) * ldw, row_x = (8 * first_x + (lane >> 3)) * ldx;
     // the token scales of the group's block: every wave asks for 64 of them (several waves for the same ones)
     const int sx_at = (in_group % (SX / 256)) * 64 + lane;
     const bool sx_in = sx_at < BM && m0 + sx_at < p.M;
@@ -77,26 +84,28 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
         __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(p.sx + m0 * p.sxr), 0, __builtin_amdgcn_readfirstlane(p.sx_span), 0x00020000);
     const uint32_t sx_off = sx_in ? (uint32_t)sx_at * (uint32_t)p.sxr * 4u : F8_OOR;
 
-    // (the whole offset in the lane's register: the range check takes the scalar offset from the range, and would wrap where that
-    // alone is past the end)
+    // Loads [from, to) of stage `it`.  (The whole offset in the lane's register: the range check takes the scalar offset from the
+    // range, and would wrap where that alone is past the end.)
     constexpr int PER_STAGE = LOADS_W + LOADS_X + 1;
-    auto issue = [&](int it, int stage) {
+    auto issue = [&](int it, int stage, int from, int to) {
         const int kb = it * G + group, k0 = kb * 128;
         uint8_t *dst = lds + stage * STAGE + group * (KBYTES + SX);
-        uint32_t vw[2], vx[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            vw[i] = k0 + piece_w[i] < p.K ? off_w[i] + k0 : F8_OOR;
-            vx[i] = k0 + piece_x[i] < p.K ? off_x[i] + k0 : F8_OOR;
+        for (int l = 0; l < PER_STAGE; ++l) {
+            if (l < from || l >= to) continue;
+            if (l < LOADS_W) {
+                const uint32_t v = k0 + piece_w[l & 1] < p.K ? row_w + piece_w[l & 1] + k0 + l * 8 * ldw : F8_OOR;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(dst + (first_w + l) * 1024), 16, (int)v, 0, 0, 0);
+            } else if (l < LOADS_W + LOADS_X) {
+                const int j = l - LOADS_W;
+                const uint32_t v = k0 + piece_x[j & 1] < p.K ? row_x + piece_x[j & 1] + k0 + j * 8 * ldx : F8_OOR;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(dst + BN * 128 + (first_x + j) * 1024), 16, (int)v, 0, 0, 0);
+            } else {
+                uint8_t *sx = dst + KBYTES + (in_group % (SX / 256)) * 256;
+                const uint32_t v = kb < p.KB ? sx_off + (uint32_t)kb * (uint32_t)p.sxc * 4u : F8_OOR;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)sx, 4, (int)v, 0, 0, 0);
+            }
         }
-#pragma unroll
-        for (int j = 0; j < LOADS_W; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(dst + (first_w + j) * 1024), 16, (int)(vw[j & 1] + j * 8 * ldw), 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < LOADS_X; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(dst + BN * 128 + (first_x + j) * 1024), 16, (int)(vx[j & 1] + j * 8 * ldx), 0, 0, 0);
-        uint8_t *sx = dst + KBYTES + (in_group % (SX / 256)) * 256;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)sx, 4, (int)(kb < p.KB ? sx_off + (uint32_t)kb * (uint32_t)p.sxc * 4u : F8_OOR), 0, 0, 0);
     };
 
     // ---- the product -----------------------------------------------------------------------------------------
@@ -110,51 +119,117 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     const float *sw_row = p.sw + (int64_t)((n0 + wn) >> 7) * p.swr;
     if (n0 + wn >= p.N) sw_row = p.sw;                   // (zeros times any scale: nothing of it is stored)
 
-    for (int s = 0; s < STAGES - 1; ++s) issue(s, s);
-    float sw = sw_row[(int64_t)min(group, p.KB - 1) * p.swc];
+    auto sw_of = [&](int it) { return sw_row[(int64_t)min(it * G + group, p.KB - 1) * p.swc]; };
+    auto frag = [&](const uint8_t *rows) {
+        return fp8_frag(*reinterpret_cast<const f8_v4i *>(rows + at_lo), *reinterpret_cast<const f8_v4i *>(rows + at_hi));
+    };
+    // Stage `it` for everybody.  Loads complete in order and every step asks for as many (those past the end for nothing), so this many
+    // outstanding means that this wave's rows have arrived.  Where the last piece of a row ends before its sixteenth byte, the wave that
+    // loaded it clears what is behind.
     const int cut_it = p.K % 16 != 0 && (p.KB - 1) % G == group ? (p.KB - 1) / G : -1;
-    int stage = 0;
-    for (int it = 0; it < iters; ++it) {
-        // Loads complete in order and every iteration asks for as many (those past the end for nothing), so this many outstanding
-        // means that this wave's rows of stage `it` have arrived.  Where the last piece of a row ends before its sixteenth byte, the
-        // wave that loaded it clears what is behind.
+    auto arrived = [&](int it, int stage) {
         constexpr int LEFT = (STAGES - 2) * PER_STAGE;
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt((LEFT & 15) | (7 << 4) | (15 << 8) | ((LEFT >> 4) << 14));
-        uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
+        __builtin_amdgcn_s_waitcnt((LEFT & 15) | (7 << 4) | (0 << 8) | ((LEFT >> 4) << 14));
         if (it == cut_it) {
             for (int i = lane; i < 8 * (LOADS_W + LOADS_X); i += 64) {
                 const int r = i < 8 * LOADS_W ? 8 * first_w + i : BN + 8 * first_x + i - 8 * LOADS_W;
-                uint8_t *q = cur + r * 128 + 16 * (((p.K & 127) >> 4) ^ ((r >> 1) & 7));
+                uint8_t *q = lds + stage * STAGE + group * (KBYTES + SX) + r * 128 + 16 * (((p.K & 127) >> 4) ^ ((r >> 1) & 7));
                 for (int b = p.K & 15; b < 16; ++b) q[b] = 0;
             }
+            __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
         }
-        __syncthreads();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();                    // (alone: __syncthreads() would wait for the stages on their way as well)
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        issue(it + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-        const float sw_next = sw_row[(int64_t)min((it + 1) * G + group, p.KB - 1) * p.swc];
+    };
+    auto after = [&](int stage) { return stage == STAGES - 1 ? 0 : stage + 1; };
+    auto before = [&](int stage) { return stage == 0 ? STAGES - 1 : stage - 1; };
 
-        const uint8_t *wp = cur + wn * 128, *xp = cur + (BN + wm) * 128;
-        const float *sxp = reinterpret_cast<const float *>(cur + KBYTES) + wm + r16;
-        auto frag = [&](const uint8_t *rows) {
-            return fp8_frag(*reinterpret_cast<const f8_v4i *>(rows + at_lo), *reinterpret_cast<const f8_v4i *>(rows + at_hi));
+    for (int s = 0; s < STAGES - 1; ++s) issue(s, s, 0, PER_STAGE);
+    if constexpr (!AHEAD) {
+        float sw = sw_of(0);
+        for (int it = 0, stage = 0; it < iters; ++it, stage = after(stage)) {
+            arrived(it, stage);
+            issue(it + STAGES - 1, before(stage), 0, PER_STAGE);
+            const float sw_next = sw_of(it + 1);
+            const uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
+            const float *sxp = reinterpret_cast<const float *>(cur + KBYTES) + wm + r16;
+            Fp8Operand<WIDE> x[TM];
+            float s[TM];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                x[i].set(frag(cur + (BN + wm + 16 * i) * 128));
+                s[i] = sxp[i * 16] * sw;
+            }
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                Fp8Operand<WIDE> w;
+                w.set(frag(cur + (wn + 16 * j) * 128));
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fp8_add(acc[i][j], fp8_mfma(w, x[i]), s[i]);
+            }
+            sw = sw_next;
+        }
+    } else {
+        // Product k of a step is weight fragment k / TM with token fragment k % TM.  A fragment of tokens is read again, for the next
+        // step, as soon as its last product is under way, and a product's multiply-adds stand DEPTH products after it, those of a step's last
+        // ones in the next step.
+        constexpr int COUNT = TN * TM, DEPTH = 3, SPREAD = COUNT / 4;
+        static_assert(TN % 2 == 0 && COUNT % (DEPTH + 1) == 0, "fragments and products have the same places in every step");
+        static_assert(COUNT - TM > DEPTH, "a step's scales are taken before the next one's are read");
+        f8_v8i wf[2], xf[TM];
+        Fp8Operand<WIDE> w, x[TM];
+        f8_f4 prod[DEPTH + 1];
+        float s[TM], sx[TM];
+        auto tokens = [&](int i, int stage) {
+            const uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
+            xf[i] = frag(cur + (BN + wm + 16 * i) * 128);
+            sx[i] = reinterpret_cast<const float *>(cur + KBYTES)[wm + r16 + 16 * i];
         };
-        Fp8Operand<WIDE> x[TM];
-        float s[TM];
+        auto weights = [&](int j, int stage) { wf[j & 1] = frag(lds + stage * STAGE + group * (KBYTES + SX) + (wn + 16 * j) * 128); };
+        auto add = [&](int k) {
+            fp8_add(acc[k % TM][k / TM], prod[k % (DEPTH + 1)], s[k % TM]);
+            asm volatile("" : "+v"(acc[k % TM][k / TM]));       // (here: not sunk to the loop's end, with its product kept until then)
+        };
+        float sw = sw_of(0);
+        arrived(0, 0);
+        weights(0, 0);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            x[i].set(frag(xp + i * 2048));
-            s[i] = sxp[i * 16] * sw;
+        for (int i = 0; i < TM; ++i) tokens(i, 0);
+#pragma unroll
+        for (int i = 0; i <= DEPTH; ++i) prod[i] = f8_f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < TM; ++i) s[i] = 0.0f;
+        for (int it = 0, stage = 0; it < iters; ++it, stage = after(stage)) {
+            const float sw_next = sw_of(it + 1);
+#pragma unroll
+            for (int k = 0; k < COUNT; ++k) {
+                const int j = k / TM, i = k % TM;
+                if (i == 0) {
+                    if (j + 1 < TN) weights(j + 1, stage);
+                    w.set(wf[j & 1]);
+                    if (j == TN - 1) {                   // all of this stage is in registers
+                        arrived(it + 1, after(stage));
+                        weights(0, after(stage));
+                    }
+                }
+                if (j == 0) x[i].set(xf[i]);
+                prod[k % (DEPTH + 1)] = fp8_mfma(w, x[i]);
+                if (j == TN - 1) tokens(i, after(stage));
+                if (k < SPREAD) issue(it + STAGES - 1, before(stage), k * PER_STAGE / SPREAD, (k + 1) * PER_STAGE / SPREAD);
+                if (k == DEPTH) {
+#pragma unroll
+                    for (int m = 0; m < TM; ++m) s[m] = sx[m] * sw;
+                }
+                add((k + COUNT - DEPTH) % COUNT);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            sw = sw_next;
         }
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            Fp8Operand<WIDE> w;
-            w.set(frag(wp + j * 2048));
-#pragma unroll
-            for (int i = 0; i < TM; ++i) fp8_add(acc[i][j], fp8_mfma(w, x[i]), s[i]);
-        }
-        sw = sw_next;
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        for (int k = COUNT - DEPTH; k < COUNT; ++k) add(k);
     }
 
     // every load has to have landed before its memory is used for something else
@@ -181,7 +256,7 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     fp8_store_tile<T, TN, TM>(p, m0 + wm, n0 + wn, acc, lds + SUMS + in_group * (TM * TN * 256 * (int)sizeof(T)), lane);
 }
 
-template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC>
+template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC, bool AHEAD>
 static void launch_tile(const Fp8GemmParams &p, hipStream_t s)
 {
     constexpr int GROUP = (BN / WN) * (BM / WM);
@@ -190,7 +265,7 @@ static void launch_tile(const Fp8GemmParams &p, hipStream_t s)
     constexpr int last = sums + BN * BM * (int)sizeof(T);
     constexpr int lds = ring > last ? ring : last;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    auto k = k_fp8_gemm_tile<T, BN, BM, WN, WM, G, STAGES, OCC>;
+    auto k = k_fp8_gemm_tile<T, BN, BM, WN, WM, G, STAGES, OCC, AHEAD>;
     static bool granted = false;
     if (!granted) {
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);

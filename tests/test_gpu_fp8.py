@@ -487,7 +487,7 @@ def test_replayed_from_a_graph(nq):
         assert torch.equal(h2, want[0]) and torch.equal(z, want[1]), i
 
 
-# ragged sizes at which the library's choice is each of its tile forms
+# ragged sizes over the range in which the library chooses between its tile forms
 FORM_SIZES = [(1, 23, 318), (1, 21, 376), (1, 23, 1596), (1, 20, 1653), (4083, 54, 532), (49, 3665, 553), (66, 4878, 305), (98, 3021, 313),
               (49, 5471, 330), (2883, 132, 301), (3721, 341, 318), (2996, 688, 301), (325, 5668, 1961), (2307, 1700, 334), (2572, 1286, 316),
               (2999, 2930, 40), (3999, 4001, 415)]
@@ -496,6 +496,20 @@ FORM_SIZES = [(1, 23, 318), (1, 21, 376), (1, 23, 1596), (1, 20, 1653), (4083, 5
 @pytest.mark.parametrize("M,N,K", FORM_SIZES)
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_gemm_every_tile_form(nq, M, N, K, out):
+    ld = dict(ld=-(-K // 16) * 16)
+    check_gemm(nq, M, N, K, out=out, exact=True, seed=K, x_kw=ld, w_kw=ld)
+    check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
+
+
+# one to nine steps in each form of tile whose next step is read ahead, and in the one for some hundred tokens
+STEP_SIZES = [(407, 4846, 17), (336, 4465, 17), (5620, 333, 135), (324, 5490, 273), (4153, 458, 385), (331, 5773, 648), (5133, 786, 17),
+              (2617, 1422, 17), (645, 5554, 134), (791, 4621, 257), (5192, 769, 386), (5379, 709, 655), (5063, 1421, 651), (1996, 4033, 1117),
+              (3875, 2061, 17), (2461, 3211, 133), (1545, 5030, 270), (2385, 3329, 654), (5196, 330, 533), (327, 5174, 657)]
+
+
+@pytest.mark.parametrize("M,N,K", STEP_SIZES)
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_gemm_step_counts(nq, M, N, K, out):
     ld = dict(ld=-(-K // 16) * 16)
     check_gemm(nq, M, N, K, out=out, exact=True, seed=K, x_kw=ld, w_kw=ld)
     check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
