@@ -82,11 +82,10 @@ static void launch_any(const Fp8GemmParams &p, hipStream_t s)
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
-// What a tile form takes, in microseconds, fitted to launches of 126 (fp32 outputs: 59) random sizes from 1 x 100 x 100 to 8192^3:
+// What a tile form takes, in microseconds, fitted to launches of 130 (fp32 outputs: 60) random sizes from 1 x 100 x 100 to 8192^3:
 // start + a round of tiles, `occ` to a compute unit, for each 256 * occ of them: per_tile + it * per_step, either with a part
 // that grows with the round's share of occupied units; it: steps of G column blocks.  The form with the least is taken: on those
-// sizes 1.0 % (0.7 %) slower than the fastest of fifteen forms timed for each, 17 % at worst (584 x 2560 x 128, 4 us), 12 % where
-// K is longer.
+// sizes 0.7 % (0.4 %) slower than the fastest of thirteen forms timed for each, 11 % (8 %) at worst.
 struct Fp8Form {
     int BN, BM, G, occ;
     float start, tile, tile_full, step, step_full;
@@ -100,33 +99,31 @@ static double form_time(const Fp8Form &f, int M, int N, int KB)
     return f.start + rounds * round(1.0) + (rest ? round((double)rest / slots) : 0.0);
 }
 
-// Few tokens: small tiles with many waves along the columns, two or four tiles to a unit: the weights stream (1 x 8192 x 8192 12.5 us,
+// Few tokens: small tiles with many waves along the columns, two or four tiles to a unit: the weights stream (24 x 8192 x 8192 12.6 us,
 // 5.4 TB/s).  Some hundred: the largest tile of which there are still 256.  Many: tiles of 256 x 256 (16-bit outputs, 8192^3
-// 2.2 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
+// 2.3 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
 // its loads 2.7); fp32 outputs need the registers for their wider operands and stay at 128 x 128.
 static const Fp8Form FORMS_16[] = {
-    {16, 16, 4, 4, 2.21f, 0.00f, 1.18f, 0.303f, 0.429f},   {16, 16, 8, 2, 2.23f, 0.26f, 1.03f, 0.403f, 0.415f},
-    {32, 32, 8, 1, 1.43f, 2.06f, 0.10f, 0.728f, 0.267f},   {64, 32, 4, 1, 1.44f, 2.20f, 0.43f, 0.601f, 0.106f},
-    {64, 64, 2, 2, 1.15f, 1.82f, 1.45f, 0.582f, 0.355f},   {128, 64, 2, 1, 0.00f, 3.79f, 0.99f, 0.736f, 0.044f},
-    {128, 128, 1, 1, 0.00f, 3.43f, 2.88f, 0.533f, 0.046f}, {128, 128, 1, 2, 0.00f, 3.46f, 6.49f, 0.635f, 0.455f},
-    {256, 128, 1, 1, 0.00f, 4.15f, 6.65f, 0.810f, 0.113f}, {256, 256, 1, 1, 0.00f, 5.19f, 13.49f, 1.282f, 0.304f}};
+    {16, 16, 4, 4, 2.20f, 0.00f, 1.13f, 0.300f, 0.431f},   {16, 16, 8, 2, 2.13f, 0.27f, 0.97f, 0.401f, 0.415f},
+    {64, 16, 4, 1, 1.37f, 1.50f, 0.22f, 0.473f, 0.074f},   {64, 32, 4, 1, 1.51f, 2.07f, 0.32f, 0.609f, 0.103f},
+    {64, 64, 2, 2, 2.23f, 0.46f, 1.54f, 0.560f, 0.361f},   {128, 128, 1, 1, 1.63f, 1.76f, 1.48f, 0.521f, 0.079f},
+    {128, 128, 1, 2, 3.38f, 0.00f, 3.46f, 0.630f, 0.490f}, {128, 64, 2, 1, 1.55f, 2.17f, 0.83f, 0.711f, 0.092f},
+    {256, 128, 1, 1, 2.88f, 1.23f, 3.39f, 0.801f, 0.197f}, {256, 256, 1, 1, 3.09f, 2.39f, 5.40f, 1.258f, 0.467f}};
 static const Fp8Form FORMS_32[] = {
-    {16, 16, 4, 4, 2.17f, 0.00f, 1.30f, 0.370f, 0.383f},   {16, 16, 8, 2, 1.94f, 0.61f, 0.85f, 0.480f, 0.341f},
-    {32, 32, 8, 1, 1.11f, 2.63f, 0.00f, 0.945f, 0.058f},   {64, 32, 4, 1, 1.49f, 2.29f, 0.66f, 0.885f, 0.028f},
-    {64, 64, 2, 2, 3.15f, 0.00f, 2.65f, 0.782f, 0.461f},   {0, 0, 0, 0, 0, 0, 0, 0, 0},
-    {128, 128, 1, 1, 2.24f, 1.35f, 4.58f, 0.977f, 0.016f}, {128, 128, 1, 2, 0.00f, 4.03f, 7.55f, 0.992f, 0.675f},
-    {256, 128, 1, 1, 0.00f, 4.67f, 7.70f, 1.512f, 0.063f}};
+    {16, 16, 4, 4, 2.12f, 0.02f, 1.25f, 0.367f, 0.379f},   {16, 16, 8, 2, 1.84f, 0.62f, 0.76f, 0.485f, 0.332f},
+    {64, 16, 4, 1, 1.29f, 1.59f, 0.29f, 0.640f, 0.030f},   {64, 32, 4, 1, 1.58f, 2.01f, 0.66f, 0.869f, 0.009f},
+    {64, 64, 2, 2, 2.90f, 0.00f, 2.08f, 0.765f, 0.448f},   {128, 128, 1, 1, 2.99f, 0.49f, 3.34f, 0.960f, 0.032f},
+    {128, 128, 1, 2, 4.06f, 0.00f, 3.68f, 0.973f, 0.779f}};
 
 template <typename T>
 static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
-    const int count = F32 ? 9 : 10;
+    const int count = F32 ? 7 : 10;
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < count; ++i) {
-        if (forms[i].BN == 0) continue;
         const double t = form_time(forms[i], p.M, p.N, p.KB);
         if (t < least) {
             least = t;
@@ -136,17 +133,18 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
     switch (best) {
     case 0: return launch_tile<T, 16, 16, 16, 16, 4, 2, 1, false>(p, s);
     case 1: return launch_tile<T, 16, 16, 16, 16, 8, 2, 2, false>(p, s);
-    case 2: return launch_tile<T, 32, 32, 32, 16, 8, 2, 4, false>(p, s);
+    case 2: return launch_tile<T, 64, 16, 32, 16, 4, 3, 2, false>(p, s);
     case 3: return launch_tile<T, 64, 32, 32, 16, 4, 3, 4, false>(p, s);
     case 4: return launch_tile<T, 64, 64, 32, 32, 2, 2, 2, false>(p, s);
-    case 6: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
-    case 7: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2, true>(p, s);
-    case 8: return launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
+    case 5: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
+    case 6: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2, true>(p, s);
     default: break;
     }
     if constexpr (!F32) {
-        if (best == 5)
+        if (best == 7)
             launch_tile<T, 128, 64, 32, 32, 2, 3, 2, false>(p, s);
+        else if (best == 8)
+            launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
         else
             launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
     }
@@ -184,7 +182,6 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     p.KB = (p.K + 127) / 128;
     const int es = dtype_bytes(dtype);
     p.y_vec = aligned_to(d_y, 4 * es) && ldy % 4 == 0;
-    p.y_16 = aligned16(d_y) && ldy * es % 16 == 0;
     // The tiles need rows on 16 bytes and scales that a buffer descriptor reaches from a tile's first token on.
     const int64_t span = (255 * p.sxr + (int64_t)std::max(0, p.KB - 1) * p.sxc + 1) * 4;
     const bool tiled = p.KB > 0 && aligned16(x->d_q) && aligned16(w->d_q) && x->ld % 16 == 0 && w->ld % 16 == 0 && span < (int64_t(1) << 30);

@@ -501,10 +501,11 @@ def test_gemm_every_tile_form(nq, M, N, K, out):
     check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
 
 
-# one to nine steps in each form of tile whose next step is read ahead, and in the one for some hundred tokens
+# one to nine steps in the tiles whose next step is read ahead, and the forms that the sizes above do not reach
 STEP_SIZES = [(407, 4846, 17), (336, 4465, 17), (5620, 333, 135), (324, 5490, 273), (4153, 458, 385), (331, 5773, 648), (5133, 786, 17),
               (2617, 1422, 17), (645, 5554, 134), (791, 4621, 257), (5192, 769, 386), (5379, 709, 655), (5063, 1421, 651), (1996, 4033, 1117),
-              (3875, 2061, 17), (2461, 3211, 133), (1545, 5030, 270), (2385, 3329, 654), (5196, 330, 533), (327, 5174, 657)]
+              (3875, 2061, 17), (2461, 3211, 133), (1545, 5030, 270), (2385, 3329, 654), (5196, 330, 533), (327, 5174, 657), (33, 5745, 822), (261, 6427, 570),
+              (7605, 206, 807), (2338, 3229, 700), (7924, 1678, 131), (5015, 2251, 257), (1166, 7607, 395), (5555, 1497, 518), (1162, 6646, 705)]
 
 
 @pytest.mark.parametrize("M,N,K", STEP_SIZES)
