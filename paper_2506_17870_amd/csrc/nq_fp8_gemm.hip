@@ -85,7 +85,7 @@ static void launch_any(const Fp8GemmParams &p, hipStream_t s)
 // What a tile form takes, in microseconds, fitted to launches of 130 (fp32 outputs: 60) random sizes from 1 x 100 x 100 to 8192^3:
 // start + a round of tiles, `occ` to a compute unit, for each 256 * occ of them: per_tile + it * per_step, either with a part
 // that grows with the round's share of occupied units; it: steps of G column blocks.  The form with the least is taken: on those
-// sizes 0.7 % (0.4 %) slower than the fastest of thirteen forms timed for each, 11 % (8 %) at worst.
+// sizes 0.9 % (0.5 %) slower than the fastest of 22 forms timed for each, 14 % (12 %) at worst.
 struct Fp8Form {
     int BN, BM, G, occ;
     float start, tile, tile_full, step, step_full;
@@ -96,31 +96,33 @@ static double form_time(const Fp8Form &f, int M, int N, int KB)
     const int64_t tiles = ceil_div(M, f.BM) * ceil_div(N, f.BN), slots = 256 * f.occ, rounds = tiles / slots, rest = tiles % slots;
     const double it = (double)ceil_div(KB, f.G);
     auto round = [&](double load) { return f.tile + f.tile_full * load + it * (f.step + f.step_full * load); };
-    return f.start + rounds * round(1.0) + (rest ? round((double)rest / slots) : 0.0);
+    // (the last round's load: half of it what the tiles share over the card, half what the fullest compute unit has)
+    const double load = 0.5 * ((double)rest / slots + (double)ceil_div(rest, 256) / f.occ);
+    return f.start + rounds * round(1.0) + (rest ? round(load) : 0.0);
 }
 
-// Few tokens: small tiles with many waves along the columns, two or four tiles to a unit: the weights stream (24 x 8192 x 8192 12.6 us,
-// 5.4 TB/s).  Some hundred: the largest tile of which there are still 256.  Many: tiles of 256 x 256 (16-bit outputs, 8192^3
-// 2.3 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
+// Few tokens: small tiles with many waves along the columns, two or four tiles to a unit: the weights stream (24 x 8192 x 8192 12.7 us,
+// 5.3 TB/s).  Some hundred: the largest tile of which there are still 256.  Many: tiles of 256 x 256 (16-bit outputs, 8192^3
+// 2.36 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
 // its loads 2.7); fp32 outputs need the registers for their wider operands and stay at 128 x 128.
 static const Fp8Form FORMS_16[] = {
-    {16, 16, 4, 4, 2.20f, 0.00f, 1.13f, 0.300f, 0.431f},   {16, 16, 8, 2, 2.13f, 0.27f, 0.97f, 0.401f, 0.415f},
-    {64, 16, 4, 1, 1.37f, 1.50f, 0.22f, 0.473f, 0.074f},   {64, 32, 4, 1, 1.51f, 2.07f, 0.32f, 0.609f, 0.103f},
-    {64, 64, 2, 2, 2.23f, 0.46f, 1.54f, 0.560f, 0.361f},   {128, 128, 1, 1, 1.63f, 1.76f, 1.48f, 0.521f, 0.079f},
-    {128, 128, 1, 2, 3.38f, 0.00f, 3.46f, 0.630f, 0.490f}, {128, 64, 2, 1, 1.55f, 2.17f, 0.83f, 0.711f, 0.092f},
-    {256, 128, 1, 1, 2.88f, 1.23f, 3.39f, 0.801f, 0.197f}, {256, 256, 1, 1, 3.09f, 2.39f, 5.40f, 1.258f, 0.467f}};
+    {16, 16, 4, 4, 2.16f, 0.00f, 1.37f, 0.225f, 0.396f},   {16, 16, 8, 2, 2.15f, 0.03f, 1.43f, 0.290f, 0.432f},
+    {64, 16, 4, 1, 1.47f, 1.28f, 0.59f, 0.387f, 0.120f},   {64, 32, 4, 1, 1.44f, 2.12f, 0.59f, 0.468f, 0.158f},
+    {64, 64, 2, 2, 2.33f, 0.00f, 2.14f, 0.398f, 0.439f},   {128, 128, 1, 2, 2.91f, 0.00f, 4.22f, 0.400f, 0.628f},
+    {64, 64, 2, 1, 1.43f, 1.14f, 1.01f, 0.443f, 0.051f},   {128, 128, 1, 1, 1.72f, 0.82f, 2.69f, 0.353f, 0.220f},
+    {256, 128, 1, 1, 2.18f, 0.00f, 5.50f, 0.492f, 0.459f}, {256, 256, 1, 1, 1.77f, 0.00f, 8.95f, 0.832f, 0.851f}};
 static const Fp8Form FORMS_32[] = {
-    {16, 16, 4, 4, 2.12f, 0.02f, 1.25f, 0.367f, 0.379f},   {16, 16, 8, 2, 1.84f, 0.62f, 0.76f, 0.485f, 0.332f},
-    {64, 16, 4, 1, 1.29f, 1.59f, 0.29f, 0.640f, 0.030f},   {64, 32, 4, 1, 1.58f, 2.01f, 0.66f, 0.869f, 0.009f},
-    {64, 64, 2, 2, 2.90f, 0.00f, 2.08f, 0.765f, 0.448f},   {128, 128, 1, 1, 2.99f, 0.49f, 3.34f, 0.960f, 0.032f},
-    {128, 128, 1, 2, 4.06f, 0.00f, 3.68f, 0.973f, 0.779f}};
+    {16, 16, 4, 4, 2.13f, 0.00f, 1.49f, 0.301f, 0.303f},   {16, 16, 8, 2, 1.93f, 0.37f, 1.24f, 0.350f, 0.337f},
+    {64, 16, 4, 1, 1.32f, 1.52f, 0.52f, 0.543f, 0.042f},   {64, 32, 4, 1, 1.56f, 1.83f, 1.07f, 0.729f, 0.057f},
+    {64, 64, 2, 2, 2.50f, 0.00f, 2.41f, 0.553f, 0.631f},   {128, 128, 1, 2, 3.23f, 0.00f, 4.93f, 0.632f, 1.082f},
+    {64, 64, 4, 1, 1.69f, 1.40f, 1.85f, 1.101f, 0.122f},   {128, 128, 2, 1, 2.70f, 0.00f, 5.79f, 1.402f, 0.299f}};
 
 template <typename T>
 static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
-    const int count = F32 ? 7 : 10;
+    const int count = F32 ? 8 : 10;
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < count; ++i) {
@@ -136,17 +138,21 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
     case 2: return launch_tile<T, 64, 16, 32, 16, 4, 3, 2, false>(p, s);
     case 3: return launch_tile<T, 64, 32, 32, 16, 4, 3, 4, false>(p, s);
     case 4: return launch_tile<T, 64, 64, 32, 32, 2, 2, 2, false>(p, s);
-    case 5: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
-    case 6: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2, true>(p, s);
+    case 5: return launch_tile<T, 128, 128, 64, 64, 1, 2, 2, true>(p, s);
     default: break;
     }
-    if constexpr (!F32) {
-        if (best == 7)
-            launch_tile<T, 128, 64, 32, 32, 2, 3, 2, false>(p, s);
-        else if (best == 8)
-            launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
+    if constexpr (F32) {
+        if (best == 6)
+            launch_tile<T, 64, 64, 32, 32, 4, 2, 4, false>(p, s);
         else
-            launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
+            launch_tile<T, 128, 128, 64, 64, 2, 2, 2, true>(p, s);
+    } else {
+        switch (best) {
+        case 6: return launch_tile<T, 64, 64, 32, 32, 2, 3, 2, false>(p, s);
+        case 7: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
+        case 8: return launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
+        default: return launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
+        }
     }
 }
 

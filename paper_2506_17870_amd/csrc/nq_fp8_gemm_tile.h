@@ -8,12 +8,11 @@
 // (BN / WN) x (BM / WM); group g takes the column blocks g, g + G, ..., so that a tile has G times the waves where there are
 // too few tiles to fill the card, and the groups' sums are added in order at the end.
 //
-// AHEAD, for the large tiles: a step does not begin with its barrier but has it before its last fragment of weights, so that the
+// AHEAD, for the large tiles: a step does not begin with its barrier but has it as soon as all its weights are in registers, so that the
 // next step's first fragments are read while the matrix cores still work; the loads of the stage to come are issued one at a time
 // between the products (a burst of them holds the wave at the address unit); and four products are in flight, each one's multiply-adds
-// standing behind the third product after it.  8192^3 507 -> 483 us, 1024 x 8192 x 8192 89 -> 72 (its tile then 256 x 128, in
-// three stages), 2048^3 15.4 -> 14.7.  Small tiles have more waves and fewer products to a step, and are faster without: 64 x 64
-// at 256 x 4096 x 4096 13.6 against 17.3 us.
+// standing behind the third product after it.  8192^3 507 -> 475 us, 1024 x 8192 x 8192 89 -> 68 (its tile then 256 x 128, in
+// three stages), 512 x 8192 x 4096 24.8 -> 22.7.  Tiles of a few products to a step have more waves instead.
 #pragma once
 #include "nq_fp8_gemm.h"
 
@@ -76,35 +75,52 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
         piece_w[i] = 16 * ((lane & 7) ^ ((4 * ((PAIRS ? i : first_w + i) & 1) + (lane >> 4)) & 7));
         piece_x[i] = PAIRS ? piece_w[i] : 16 * ((lane & 7) ^ ((4 * ((first_x + i) & 1) + (lane >> 4)) & 7));
     }
-    const uint32_t row_w = (8 * first_w + (lane >> 3)) * ldw, row_x = (8 * first_x + (lane >> 3)) * ldx;
     // the token scales of the group's block: every wave asks for 64 of them (several waves for the same ones)
     const int sx_at = (in_group % (SX / 256)) * 64 + lane;
     const bool sx_in = sx_at < BM && m0 + sx_at < p.M;
     const __amdgpu_buffer_rsrc_t sx_rsrc =
         __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(p.sx + m0 * p.sxr), 0, __builtin_amdgcn_readfirstlane(p.sx_span), 0x00020000);
-    const uint32_t sx_off = sx_in ? (uint32_t)sx_at * (uint32_t)p.sxr * 4u : F8_OOR;
 
-    // Loads [from, to) of stage `it`.  (The whole offset in the lane's register: the range check takes the scalar offset from the
-    // range, and would wrap where that alone is past the end.)
+    // A lane's offsets stay the same from block to block, whose own offset is the scalar one: a step costs no vector instruction for
+    // its addresses.  From a row's last block on the pieces past its end, and then all of them, are asked for out of range.  (The
+    // range check takes the scalar offset from the range and would wrap, were that past the end: it stays at the last block.)
     constexpr int PER_STAGE = LOADS_W + LOADS_X + 1;
-    auto issue = [&](int it, int stage, int from, int to) {
-        const int kb = it * G + group, k0 = kb * 128;
-        uint8_t *dst = lds + stage * STAGE + group * (KBYTES + SX);
+    uint32_t off[PER_STAGE];
+#pragma unroll
+    for (int l = 0; l < LOADS_W; ++l) off[l] = (8 * (first_w + l) + (lane >> 3)) * ldw + piece_w[l & 1];
+#pragma unroll
+    for (int l = 0; l < LOADS_X; ++l) off[LOADS_W + l] = (8 * (first_x + l) + (lane >> 3)) * ldx + piece_x[l & 1];
+    off[PER_STAGE - 1] = sx_in ? (uint32_t)sx_at * (uint32_t)p.sxr * 4u : F8_OOR;
+    uint8_t *const mine = lds + group * (KBYTES + SX);
+    const int last_kb = p.KB - 1, sx_step = G * (int)p.sxc * 4;
+    int kb = group - G, k_at = min(group, last_kb) * 128 - G * 128, sx_from = min(group, last_kb) * (int)p.sxc * 4 - sx_step;
+    auto next_block = [&] {
+        kb += G;
+        if (kb <= last_kb) {
+            k_at += G * 128;
+            sx_from += sx_step;
+        }
+        if (kb >= last_kb) {
+            const int here = kb == last_kb ? p.K - last_kb * 128 : 0;
+#pragma unroll
+            for (int l = 0; l < PER_STAGE; ++l) {
+                const int piece = l < LOADS_W ? piece_w[l & 1] : l < LOADS_W + LOADS_X ? piece_x[(l - LOADS_W) & 1] : 0;
+                off[l] = piece < here ? off[l] : F8_OOR;
+            }
+        }
+    };
+    // loads [from, to) of the block into the stage at `at`
+    auto issue = [&](int at, int from, int to) {
+        uint8_t *dst = mine + at;
 #pragma unroll
         for (int l = 0; l < PER_STAGE; ++l) {
             if (l < from || l >= to) continue;
-            if (l < LOADS_W) {
-                const uint32_t v = k0 + piece_w[l & 1] < p.K ? row_w + piece_w[l & 1] + k0 + l * 8 * ldw : F8_OOR;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(dst + (first_w + l) * 1024), 16, (int)v, 0, 0, 0);
-            } else if (l < LOADS_W + LOADS_X) {
-                const int j = l - LOADS_W;
-                const uint32_t v = k0 + piece_x[j & 1] < p.K ? row_x + piece_x[j & 1] + k0 + j * 8 * ldx : F8_OOR;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(dst + BN * 128 + (first_x + j) * 1024), 16, (int)v, 0, 0, 0);
-            } else {
-                uint8_t *sx = dst + KBYTES + (in_group % (SX / 256)) * 256;
-                const uint32_t v = kb < p.KB ? sx_off + (uint32_t)kb * (uint32_t)p.sxc * 4u : F8_OOR;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)sx, 4, (int)v, 0, 0, 0);
-            }
+            if (l < LOADS_W)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(dst + (first_w + l) * 1024), 16, (int)off[l], k_at, 0, 0);
+            else if (l < LOADS_W + LOADS_X)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(dst + BN * 128 + (first_x + l - LOADS_W) * 1024), 16, (int)off[l], k_at, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)(dst + KBYTES + (in_group % (SX / 256)) * 256), 4, (int)off[l], sx_from, 0, 0);
         }
     };
 
@@ -119,7 +135,16 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     const float *sw_row = p.sw + (int64_t)((n0 + wn) >> 7) * p.swr;
     if (n0 + wn >= p.N) sw_row = p.sw;                   // (zeros times any scale: nothing of it is stored)
 
-    auto sw_of = [&](int it) { return sw_row[(int64_t)min(it * G + group, p.KB - 1) * p.swc]; };
+    // (a group without a block in the last step adds zeros times a scale of zero)
+    const float *sw_at = sw_row + (int64_t)min(group, last_kb) * p.swc;
+    const int64_t sw_step = G * p.swc;
+    int sw_kb = group;
+    auto scale_at = [&] { return G == 1 || sw_kb <= last_kb ? *sw_at : 0.0f; };
+    auto next_scale = [&] {
+        sw_kb += G;
+        if (sw_kb <= last_kb) sw_at += sw_step;
+        return scale_at();
+    };
     auto frag = [&](const uint8_t *rows) {
         return fp8_frag(*reinterpret_cast<const f8_v4i *>(rows + at_lo), *reinterpret_cast<const f8_v4i *>(rows + at_hi));
     };
@@ -127,14 +152,17 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     // outstanding means that this wave's rows have arrived.  Where the last piece of a row ends before its sixteenth byte, the wave that
     // loaded it clears what is behind.
     const int cut_it = p.K % 16 != 0 && (p.KB - 1) % G == group ? (p.KB - 1) / G : -1;
-    auto arrived = [&](int it, int stage) {
-        constexpr int LEFT = (STAGES - 2) * PER_STAGE;
+    auto arrived = [&](int it, int at, bool first = false) {
+        constexpr int LEFT = (STAGES - 2) * PER_STAGE, FIRST = (STAGES - 1) * PER_STAGE;
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt((LEFT & 15) | (7 << 4) | (0 << 8) | ((LEFT >> 4) << 14));
+        if (first)                                       // (before the loop, with every stage asked for)
+            __builtin_amdgcn_s_waitcnt((FIRST & 15) | (7 << 4) | (0 << 8) | ((FIRST >> 4) << 14));
+        else
+            __builtin_amdgcn_s_waitcnt((LEFT & 15) | (7 << 4) | (0 << 8) | ((LEFT >> 4) << 14));
         if (it == cut_it) {
             for (int i = lane; i < 8 * (LOADS_W + LOADS_X); i += 64) {
                 const int r = i < 8 * LOADS_W ? 8 * first_w + i : BN + 8 * first_x + i - 8 * LOADS_W;
-                uint8_t *q = lds + stage * STAGE + group * (KBYTES + SX) + r * 128 + 16 * (((p.K & 127) >> 4) ^ ((r >> 1) & 7));
+                uint8_t *q = mine + at + r * 128 + 16 * (((p.K & 127) >> 4) ^ ((r >> 1) & 7));
                 for (int b = p.K & 15; b < 16; ++b) q[b] = 0;
             }
             __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
@@ -144,17 +172,22 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto after = [&](int stage) { return stage == STAGES - 1 ? 0 : stage + 1; };
-    auto before = [&](int stage) { return stage == 0 ? STAGES - 1 : stage - 1; };
+    // stages by where they begin
+    auto after = [&](int at) { return at == (STAGES - 1) * STAGE ? 0 : at + STAGE; };
+    auto before = [&](int at) { return at == 0 ? (STAGES - 1) * STAGE : at - STAGE; };
 
-    for (int s = 0; s < STAGES - 1; ++s) issue(s, s, 0, PER_STAGE);
+    for (int s = 0; s < STAGES - 1; ++s) {
+        next_block();
+        issue(s * STAGE, 0, PER_STAGE);
+    }
+    float sw = scale_at();
     if constexpr (!AHEAD) {
-        float sw = sw_of(0);
-        for (int it = 0, stage = 0; it < iters; ++it, stage = after(stage)) {
-            arrived(it, stage);
-            issue(it + STAGES - 1, before(stage), 0, PER_STAGE);
-            const float sw_next = sw_of(it + 1);
-            const uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
+        for (int it = 0, at = 0; it < iters; ++it, at = after(at)) {
+            arrived(it, at);
+            const float sw_next = next_scale();          // (before the stage's loads: complete when they are waited for)
+            next_block();
+            issue(before(at), 0, PER_STAGE);
+            const uint8_t *cur = mine + at;
             const float *sxp = reinterpret_cast<const float *>(cur + KBYTES) + wm + r16;
             Fp8Operand<WIDE> x[TM];
             float s[TM];
@@ -173,52 +206,59 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
             sw = sw_next;
         }
     } else {
-        // Product k of a step is weight fragment k / TM with token fragment k % TM.  A fragment of tokens is read again, for the next
-        // step, as soon as its last product is under way, and a product's multiply-adds stand DEPTH products after it, those of a step's last
-        // ones in the next step.
-        constexpr int COUNT = TN * TM, DEPTH = 3, SPREAD = COUNT / 4;
-        static_assert(TN % 2 == 0 && COUNT % (DEPTH + 1) == 0, "fragments and products have the same places in every step");
+        // Product k of a step is weight fragment k / TM with token fragment k % TM.  The weights go round a ring, RING - 1 fragments ahead;
+        // from fragment TURN on, when all of a stage's are in registers, they are the next stage's, and its own place is filled again.  A
+        // fragment of tokens is read for the next step as soon as its last product is under way, and a product's multiply-adds
+        // stand DEPTH products after it, those of a step's last ones in the next step.
+        constexpr int COUNT = TN * TM, DEPTH = 3, RING = TN % 4 == 0 ? 4 : 2, TURN = TN - RING + 1;
+        constexpr int SPREAD = COUNT / 4 < COUNT - TURN * TM ? COUNT / 4 : COUNT - TURN * TM;
+        static_assert(TN % RING == 0 && COUNT % (DEPTH + 1) == 0, "fragments and products have the same places in every step");
         static_assert(COUNT - TM > DEPTH, "a step's scales are taken before the next one's are read");
-        f8_v8i wf[2], xf[TM];
+        f8_v8i wf[RING], xf[TM];
         Fp8Operand<WIDE> w, x[TM];
         f8_f4 prod[DEPTH + 1];
         float s[TM], sx[TM];
-        auto tokens = [&](int i, int stage) {
-            const uint8_t *cur = lds + stage * STAGE + group * (KBYTES + SX);
-            xf[i] = frag(cur + (BN + wm + 16 * i) * 128);
-            sx[i] = reinterpret_cast<const float *>(cur + KBYTES)[wm + r16 + 16 * i];
+        auto tokens = [&](int i, int at) {
+            xf[i] = frag(mine + at + (BN + wm + 16 * i) * 128);
+            sx[i] = reinterpret_cast<const float *>(mine + at + KBYTES)[wm + r16 + 16 * i];
         };
-        auto weights = [&](int j, int stage) { wf[j & 1] = frag(lds + stage * STAGE + group * (KBYTES + SX) + (wn + 16 * j) * 128); };
+        auto weights = [&](int j, int at) { wf[j % RING] = frag(mine + at + (wn + 16 * j) * 128); };
         auto add = [&](int k) {
             fp8_add(acc[k % TM][k / TM], prod[k % (DEPTH + 1)], s[k % TM]);
             asm volatile("" : "+v"(acc[k % TM][k / TM]));       // (here: not sunk to the loop's end, with its product kept until then)
         };
-        float sw = sw_of(0);
-        arrived(0, 0);
-        weights(0, 0);
+        float sw_then = next_scale();
+        next_block();
+        issue((STAGES - 1) * STAGE, 0, PER_STAGE);
+        arrived(0, 0, true);
+#pragma unroll
+        for (int j = 0; j < RING - 1; ++j) weights(j, 0);
 #pragma unroll
         for (int i = 0; i < TM; ++i) tokens(i, 0);
 #pragma unroll
         for (int i = 0; i <= DEPTH; ++i) prod[i] = f8_f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < TM; ++i) s[i] = 0.0f;
-        for (int it = 0, stage = 0; it < iters; ++it, stage = after(stage)) {
-            const float sw_next = sw_of(it + 1);
+        for (int it = 0, at = 0; it < iters; ++it, at = after(at)) {
+            float sw_next = 0.0f;
 #pragma unroll
             for (int k = 0; k < COUNT; ++k) {
                 const int j = k / TM, i = k % TM;
                 if (i == 0) {
-                    if (j + 1 < TN) weights(j + 1, stage);
-                    w.set(wf[j & 1]);
-                    if (j == TN - 1) {                   // all of this stage is in registers
-                        arrived(it + 1, after(stage));
-                        weights(0, after(stage));
+                    if (j == TURN) {                     // all weights of this stage are in registers
+                        arrived(it + 1, after(at));
+                        sw_next = next_scale();
+                        next_block();
                     }
+                    w.set(wf[j % RING]);
+                    if (j + RING - 1 < TN) weights(j + RING - 1, at);
+                    else weights(j + RING - 1 - TN, after(at));
                 }
                 if (j == 0) x[i].set(xf[i]);
                 prod[k % (DEPTH + 1)] = fp8_mfma(w, x[i]);
-                if (j == TN - 1) tokens(i, after(stage));
-                if (k < SPREAD) issue(it + STAGES - 1, before(stage), k * PER_STAGE / SPREAD, (k + 1) * PER_STAGE / SPREAD);
+                if (j == TN - 1) tokens(i, after(at));
+                if (k >= TURN * TM && k < TURN * TM + SPREAD)
+                    issue(at, (k - TURN * TM) * PER_STAGE / SPREAD, (k - TURN * TM + 1) * PER_STAGE / SPREAD);
                 if (k == DEPTH) {
 #pragma unroll
                     for (int m = 0; m < TM; ++m) s[m] = sx[m] * sw;
@@ -226,7 +266,8 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
                 add((k + COUNT - DEPTH) % COUNT);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            sw = sw_next;
+            sw = sw_then;
+            sw_then = sw_next;
         }
 #pragma unroll
         for (int k = COUNT - DEPTH; k < COUNT; ++k) add(k);

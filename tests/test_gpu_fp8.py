@@ -505,7 +505,9 @@ def test_gemm_every_tile_form(nq, M, N, K, out):
 STEP_SIZES = [(407, 4846, 17), (336, 4465, 17), (5620, 333, 135), (324, 5490, 273), (4153, 458, 385), (331, 5773, 648), (5133, 786, 17),
               (2617, 1422, 17), (645, 5554, 134), (791, 4621, 257), (5192, 769, 386), (5379, 709, 655), (5063, 1421, 651), (1996, 4033, 1117),
               (3875, 2061, 17), (2461, 3211, 133), (1545, 5030, 270), (2385, 3329, 654), (5196, 330, 533), (327, 5174, 657), (33, 5745, 822), (261, 6427, 570),
-              (7605, 206, 807), (2338, 3229, 700), (7924, 1678, 131), (5015, 2251, 257), (1166, 7607, 395), (5555, 1497, 518), (1162, 6646, 705)]
+              (7605, 206, 807), (2338, 3229, 700), (7924, 1678, 131), (5015, 2251, 257), (1166, 7607, 395), (5555, 1497, 518), (1162, 6646, 705),
+              (5691, 33, 1372), (67, 5541, 385), (5371, 33, 753), (5654, 709, 791), (5652, 641, 901), (33, 5522, 1034), (5779, 67, 1283),
+              (5609, 331, 1559), (300, 4224, 128), (600, 2048, 1152), (2304, 4096, 512), (768, 5120, 384)]
 
 
 @pytest.mark.parametrize("M,N,K", STEP_SIZES)
