@@ -16,15 +16,19 @@ struct NormParams {
     int post, pre, D;
 };
 
-// Sum over the workgroup, the same in every thread and every run: within the waves first, then the waves' sums in order.  The
+// Sum over the TH threads of a row, the same in every one and every run: within the waves first, then the waves' sums in order.  The
 // sums of a row alternate between two sets of memory, so that one barrier each is enough: a wave that writes a set again has
 // passed the barrier of the sum between, and with it every wave that still had to read it.
 template <int TH>
 struct BlockSum {
-    float (*part)[TH / 64];
+    float (*part)[TH < 64 ? 1 : TH / 64];
     int set;
     __device__ __forceinline__ float operator()(float v)
     {
+        if constexpr (TH < 64) {
+            v = sum16(v);
+            return TH == 16 ? v : v + __shfl_xor(v, 16);
+        }
         v = sum64(v);
         if constexpr (TH > 64) {
             if ((threadIdx.x & 63) == 0) part[set][threadIdx.x >> 6] = v;
@@ -46,24 +50,33 @@ __device__ __forceinline__ float inverse_root(float x)
     return small ? r * 0x1p40f : r;
 }
 
-// The weights and biases of a norm for a thread's columns, in registers for all its rows.
-template <bool FULL>
+// The weights and biases of a norm for a thread's columns: in registers for all its rows where it has eight columns, else read for
+// every row (they stay in the caches).
+template <int FIT, int CH>
 struct NormVectors {
     const float *w, *b;
-    float wv[8], bv[8];
-    __device__ __forceinline__ void init(const float *w_, const float *b_, int D, float b_scale)
+    int D;
+    float b_scale, wv[8], bv[8];
+    __device__ __forceinline__ void read(int c)
     {
-        w = w_;
-        b = b_;
-        if (w) raw_to_float(load8<FULL>(w, threadIdx.x * 8, D), wv);
+        if (w) raw_to_float(load8<FIT>(w, c, D), wv);
         if (b) {
-            raw_to_float(load8<FULL>(b, threadIdx.x * 8, D), bv);
+            raw_to_float(load8<FIT>(b, c, D), bv);
 #pragma unroll
             for (int i = 0; i < 8; ++i) bv[i] *= b_scale;
         }
     }
-    __device__ __forceinline__ void apply(float r, float (&v)[8])
+    __device__ __forceinline__ void init(const float *w_, const float *b_, int c, int D_, float b_scale_)
     {
+        w = w_;
+        b = b_;
+        D = D_;
+        b_scale = b_scale_;
+        if constexpr (CH == 1) read(c);
+    }
+    __device__ __forceinline__ void apply(float r, int c, float (&v)[8])
+    {
+        if constexpr (CH > 1) read(c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= r;
         if (w) {
@@ -79,92 +92,141 @@ struct NormVectors {
 
 // v -> norm(v) * scale (the biases have it already).  The variance is that of the differences from the mean (two sums over registers),
 // not a difference of two large sums.
-template <int TH, bool FULL>
-__device__ __forceinline__ void norm_row(int kind, float eps, float scale, NormVectors<FULL> &vec, int n, float per_column, float (&v)[8],
-                                         BlockSum<TH> &sum)
+template <int TH, int FIT, int CH>
+__device__ __forceinline__ void norm_row(int kind, float eps, float scale, NormVectors<FIT, CH> &vec, int c, int D, float per_column,
+                                         float (&v)[CH][8], BlockSum<TH> &sum)
 {
     float r = 1.0f;
     if (kind != NQ_NORM_NONE) {
         if (kind == NQ_NORM_LAYER) {
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[i];
+            for (int i = 0; i < 8 * CH; ++i) s += v[i / 8][i % 8];
             const float mean = sum(s) * per_column;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = FULL || i < n ? v[i] - mean : 0.0f;
+            for (int i = 0; i < 8 * CH; ++i) {
+                float &x = v[i / 8][i % 8];
+                x = FIT == FULL || c + i / 8 * TH * 8 + (FIT == WHOLE ? 0 : i % 8) < D ? x - mean : 0.0f;
+            }
         }
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
+        for (int i = 0; i < 8 * CH; ++i) s = fmaf(v[i / 8][i % 8], v[i / 8][i % 8], s);
         r = inverse_root(fmaf(sum(s), per_column, eps));
     }
-    vec.apply(r * scale, v);
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        vec.apply(r * scale, c + k * TH * 8, v[k]);
+        if (CH > 1) __builtin_amdgcn_sched_barrier(0);       // (one chunk's vectors at a time: registers)
+    }
 }
 
-// A row to a workgroup of TH threads, eight columns to a thread; FULL: D is exactly 8 * TH.  A workgroup takes rows blockIdx.x,
+// A row to TH threads, CH times eight columns to a thread.  A workgroup takes rows blockIdx.x,
 // + gridDim.x, ...: the norms' vectors stay in its registers, and the next row is on its way while one is worked on.  (Columns past D
 // read as zeros and stay zeros, so only the differences from a mean are masked.)  With eight columns to a thread the vector unit and
 // the memory take about as long: every division, every mask and every conversion twice over that was taken out of the loop
-// showed (16384 x 4096 bf16 to codes 123 -> 92 us, 5.1 TB/s, what a copy reaches).
-template <typename T, typename H, int TH, bool FULL>
-__global__ void __launch_bounds__(TH) k_block_norm(const NormParams p)
+// showed (16384 x 4096 bf16 to codes 123 -> 86 us, 5.4 TB/s, what a copy reaches).  Rows of 256 columns at most share the waves of a
+// workgroup of 256 threads (16054 x 128 f16 to codes 11.5 -> 5.1 us).  Rows that do not fit 1024 threads have sixteen columns to
+// one; the next row is asked for when the stream's new row is formed, with 1024 threads at the end, when its registers are free
+// (4096 x 16384 bf16 to codes 156 -> 98 us against the row in LDS).
+constexpr int norm_rows(int th) { return th < 64 ? 256 / th : 1; }       // rows that a workgroup has at once
+
+template <typename T, typename H, int TH, int CH, int FIT>
+__global__ void __launch_bounds__(TH * norm_rows(TH)) k_block_norm(const NormParams p)
 {
-    __shared__ float part[2][TH / 64];
+    constexpr int ROWS = norm_rows(TH);
+    __shared__ float part[2][TH < 64 ? 1 : TH / 64];
     BlockSum<TH> sum{part, 0};
-    const int c = threadIdx.x * 8, n = FULL ? 8 : p.D - c;
+    const int c = (ROWS == 1 ? threadIdx.x : threadIdx.x % TH) * 8;
+    const int64_t first = (int64_t)blockIdx.x * ROWS + (ROWS == 1 ? 0 : threadIdx.x / TH), step = (int64_t)gridDim.x * ROWS;
+    if (ROWS > 1 && first >= p.M) return;
     const float per_column = 1.0f / (float)p.D;
+    auto left = [&](int k) {
+        const int n = p.D - (c + k * TH * 8);
+        return FIT == CUT ? n : FIT == FULL || n > 0 ? 8 : 0;
+    };
 
     struct Row {
-        Raw8<T> y, g;
-        Raw8<H> h;
+        Raw8<T> y[CH], g[CH];
+        Raw8<H> h[CH];
     };
     auto load = [&](Row &r, int64_t row) {
-        if (p.y) r.y = load8<FULL>(static_cast<const T *>(p.y) + row * p.ldy, c, p.D);
-        r.h = load8<FULL>(static_cast<const H *>(p.h) + row * p.ldh, c, p.D);
-        if (p.gate) r.g = load8<FULL>(static_cast<const T *>(p.gate) + row / p.gate_rows * p.ldgate, c, p.D);
+        const T *y = static_cast<const T *>(p.y) + row * p.ldy;
+        const H *h = static_cast<const H *>(p.h) + row * p.ldh;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if (p.y) r.y[k] = fetch8<FIT>(y, c + k * TH * 8, p.D);
+            r.h[k] = fetch8<FIT>(h, c + k * TH * 8, p.D);
+        }
+        if (p.gate) {
+            const T *gate = static_cast<const T *>(p.gate) + row / p.gate_rows * p.ldgate;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) r.g[k] = fetch8<FIT>(gate, c + k * TH * 8, p.D);
+        }
     };
     Row now;
-    load(now, blockIdx.x);
-    NormVectors<FULL> post, pre;
-    post.init(p.post_w, p.post_b, p.D, p.branch_scale);
-    pre.init(p.pre_w, p.pre_b, p.D, 1.0f);
+    load(now, first);
+    NormVectors<FIT, CH> post, pre;
+    post.init(p.post_w, p.post_b, c, p.D, p.branch_scale);
+    pre.init(p.pre_w, p.pre_b, c, p.D, 1.0f);
 
-    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
+    for (int64_t row = first; row < p.M; row += step) {
         Row next;
-        if (row + gridDim.x < p.M) load(next, row + gridDim.x);
-        float v[8] = {}, h[8];
+        if (CH == 1 && row + step < p.M) load(next, row + step);
+        float v[CH][8] = {}, h[8];
         if (p.y) {
-            raw_to_float(now.y, v);
-            norm_row<TH, FULL>(p.post, p.post_eps, p.branch_scale, post, n, per_column, v, sum);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                settle8<FIT>(now.y[k], c + k * TH * 8, p.D);
+                raw_to_float(now.y[k], v[k]);
+            }
+            norm_row<TH, FIT, CH>(p.post, p.post_eps, p.branch_scale, post, c, p.D, per_column, v, sum);
             if (p.gate) {
-                float g[8];
-                raw_to_float(now.g, g);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= g[i];
+                for (int k = 0; k < CH; ++k) {
+                    float g[8];
+                    settle8<FIT>(now.g[k], c + k * TH * 8, p.D);
+                    raw_to_float(now.g[k], g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[k][i] *= g[i];
+                }
             }
         }
-        raw_to_float(now.h, h);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(p.residual_scale, h[i], v[i]);
-        if (p.h_out) store8(static_cast<H *>(p.h_out) + row * p.ldh_out + c, n, v);
+        for (int k = 0; k < CH; ++k) {
+            settle8<FIT>(now.h[k], c + k * TH * 8, p.D);
+            raw_to_float(now.h[k], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = fmaf(p.residual_scale, h[i], v[k][i]);
+        }
+        if (CH > 1 && TH < 1024 && row + step < p.M) load(next, row + step);
+        if (p.h_out) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) store8(static_cast<H *>(p.h_out) + row * p.ldh_out + c + k * TH * 8, left(k), v[k]);
+        }
         if (p.x || p.q) {
-            norm_row<TH, FULL>(p.pre, p.pre_eps, 1.0f, pre, n, per_column, v, sum);
-            if (p.x) store8(static_cast<T *>(p.x) + row * p.ldx + c, n, v);
-            if (p.q) {
-                uint32_t a = 0;
+            norm_row<TH, FIT, CH>(p.pre, p.pre_eps, 1.0f, pre, c, p.D, per_column, v, sum);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a = max(a, abs_bits(v[i]));
-                float inverse;
-                const float s = fp8_scale(max16(a), &inverse);
-                store_codes(p.q + row * p.ldq + c, n, fp8_codes(v, inverse));
-                if ((threadIdx.x & 15) == 0 && n > 0) p.scale[row * p.srow + (c >> 7) * p.scol] = s;
+            for (int k = 0; k < CH; ++k) {
+                const int at = c + k * TH * 8;
+                if (p.x) store8(static_cast<T *>(p.x) + row * p.ldx + at, left(k), v[k]);
+                if (p.q) {
+                    uint32_t a = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a = max(a, abs_bits(v[k][i]));
+                    float inverse;
+                    const float s = fp8_scale(max16(a), &inverse);
+                    store_codes(p.q + row * p.ldq + at, left(k), fp8_codes(v[k], inverse));
+                    if ((threadIdx.x & 15) == 0 && left(k) > 0) p.scale[row * p.srow + (at >> 7) * p.scol] = s;
+                }
             }
         }
+        if (CH > 1 && TH == 1024 && row + step < p.M) load(next, row + step);
         now = next;
     }
 }
 
-// Rows too long for the registers (D > 8192): the fp32 row lies in LDS, where a thread reads back only what it wrote itself.
+// Rows too long for the registers: the fp32 row lies in LDS, where a thread reads back only what it wrote itself.
 constexpr int LONG_TH = 512;
 
 template <typename F>
@@ -204,8 +266,8 @@ __device__ __forceinline__ void norm_long_row(const NormParams &p, f8_f4 *row, i
     const float r = inverse_root(sum(s) / count + eps);
     long_row(p, row, [&](int c, int n, float (&v)[8]) {
         float wv[8], bv[8];
-        if (w) raw_to_float(load8<false>(w, c, p.D), wv);
-        if (b) raw_to_float(load8<false>(b, c, p.D), bv);
+        if (w) raw_to_float(load8<CUT>(w, c, p.D), wv);
+        if (b) raw_to_float(load8<CUT>(b, c, p.D), bv);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             v[i] *= r;
@@ -224,13 +286,13 @@ __global__ void __launch_bounds__(LONG_TH) k_block_norm_long(const NormParams p)
     for (int64_t r = blockIdx.x; r < p.M; r += gridDim.x) {
         const T *gate = static_cast<const T *>(p.gate) + r / p.gate_rows * p.ldgate;
         if (p.y) {
-            long_row(p, lds, [&](int c, int, float (&v)[8]) { raw_to_float(load8<false>(static_cast<const T *>(p.y) + r * p.ldy, c, p.D), v); });
+            long_row(p, lds, [&](int c, int, float (&v)[8]) { raw_to_float(load8<CUT>(static_cast<const T *>(p.y) + r * p.ldy, c, p.D), v); });
             norm_long_row(p, lds, p.post, p.post_eps, p.post_w, p.post_b, sum);
         }
         long_row(p, lds, [&](int c, int n, float (&v)[8]) {
             float h[8], g[8];
-            raw_to_float(load8<false>(static_cast<const H *>(p.h) + r * p.ldh, c, p.D), h);
-            if (p.gate) raw_to_float(load8<false>(gate, c, p.D), g);
+            raw_to_float(load8<CUT>(static_cast<const H *>(p.h) + r * p.ldh, c, p.D), h);
+            if (p.gate) raw_to_float(load8<CUT>(gate, c, p.D), g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float d = 0.0f;
@@ -262,26 +324,51 @@ __global__ void __launch_bounds__(LONG_TH) k_block_norm_long(const NormParams p)
     }
 }
 
-template <typename T, typename H, int TH>
+template <typename T, typename H, int TH, int CH = 1>
 static void launch_norm(const NormParams &p, hipStream_t s)
 {
-    // up to sixteen waves to a compute unit (8: 126 us, 24: 103 us on the rows above)
-    const dim3 grid((unsigned)std::min<int64_t>(p.M, 256 * (1024 / TH)));
-    if (p.D == TH * 8)
-        k_block_norm<T, H, TH, true><<<grid, TH, 0, s>>>(p);
-    else
-        k_block_norm<T, H, TH, false><<<grid, TH, 0, s>>>(p);
+    // up to sixteen waves to a compute unit (16384 x 4096 bf16 90 us; 8: 126, 24: 103)
+    constexpr int ROWS = norm_rows(TH), WG = TH * ROWS;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(p.M, ROWS), 256 * (1024 / WG)));
+    if constexpr (CH > 1) {
+        k_block_norm<T, H, TH, CH, WHOLE><<<grid, WG, 0, s>>>(p);
+    } else if (p.D == TH * 8) {
+        k_block_norm<T, H, TH, CH, FULL><<<grid, WG, 0, s>>>(p);
+    } else if (p.D % 8 == 0) {
+        k_block_norm<T, H, TH, CH, WHOLE><<<grid, WG, 0, s>>>(p);
+    } else {
+        k_block_norm<T, H, TH, CH, CUT><<<grid, WG, 0, s>>>(p);
+    }
 }
 
 template <typename T, typename H>
 static void norm_by_size(const NormParams &p, hipStream_t s)
 {
+    constexpr bool WIDE = sizeof(H) == 4;                   // the stream takes half of the registers
     const int chunks = (p.D + 7) / 8;
+    if (p.M > 1024) {                                       // (few rows are faster with a wave each: 10 x 205 3.7 against 4.7 us)
+        if (chunks <= 16) return launch_norm<T, H, 16>(p, s);
+        if (chunks <= 32) return launch_norm<T, H, 32>(p, s);
+    }
     if (chunks <= 64) return launch_norm<T, H, 64>(p, s);
     if (chunks <= 128) return launch_norm<T, H, 128>(p, s);
     if (chunks <= 256) return launch_norm<T, H, 256>(p, s);
     if (chunks <= 384) return launch_norm<T, H, 384>(p, s);
     if (chunks <= 512) return launch_norm<T, H, 512>(p, s);
+    if (chunks <= 640) return launch_norm<T, H, 640>(p, s);
+    // Sixteen columns to a thread make two workgroups to a unit of the one, 16384 x 8192 bf16 203 -> 184 us; with an fp32 stream
+    // (8192 x 8192 fp32 195 -> 211 us) and with a cut-off chunk (16384 x 8190 bf16 215 -> 290) they cost more than that.
+    if (p.D % 8 == 0) {
+        if constexpr (!WIDE) {
+            if (chunks <= 768) return launch_norm<T, H, 384, 2>(p, s);
+            if (chunks <= 896) return launch_norm<T, H, 448, 2>(p, s);
+            if (chunks <= 1024) return launch_norm<T, H, 512, 2>(p, s);
+        }
+        if (chunks > 1024 && chunks <= 1536) return launch_norm<T, H, 768, 2>(p, s);
+        if constexpr (!WIDE) {
+            if (chunks > 1536 && chunks <= 2048) return launch_norm<T, H, 1024, 2>(p, s);
+        }
+    }
     if (chunks <= 768) return launch_norm<T, H, 768>(p, s);
     if (chunks <= 1024) return launch_norm<T, H, 1024>(p, s);
     const int lds = chunks * 32;

@@ -86,39 +86,52 @@ __device__ __forceinline__ void float_to_raw(const float (&v)[8], Raw8<bf16_t> &
     r.a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
-// Elements c .. c + 7 of a row of D, those past its end as zeros.  The address need not be aligned to more than the type: the memory
-// system takes wide accesses anywhere.  A chunk that the row's end cuts off is read as the row's last eight elements and moved
-// down (one request, where a request per element would hold up the wave), in a row of fewer than eight by elements.
-// FULL: the chunk is known to lie within the row.
-template <bool FULL, typename T>
-__device__ __forceinline__ Raw8<T> load8(const T *row, int c, int D)
+// Elements c .. c + 7 of a row of D, those past its end as zeros: fetch8() asks for them and settle8() puts them in their places, so
+// that nothing waits before they are used.  The address need not be aligned to more than the type: the memory system takes wide
+// accesses anywhere.  A chunk that the row's end cuts off is read as the row's last eight elements and moved down (one request,
+// where a request per element would hold up the wave), in a row of fewer than eight by elements.
+// FIT: CUT, any D; WHOLE, a multiple of eight, so that no chunk is cut off; FULL, every chunk is known to lie within the row.
+enum Fit { CUT, WHOLE, FULL };
+template <int FIT, typename T>
+__device__ __forceinline__ Raw8<T> fetch8(const T *row, int c, int D)
 {
-    const int n = D - c;
     Raw8<T> r{};
-    if (FULL || n >= 8) {
-        __builtin_memcpy(&r, row + c, sizeof r);
-    } else if (n > 0 && D >= 8) {
-        __builtin_memcpy(&r, row + D - 8, sizeof r);
-        constexpr int W = (int)sizeof(r) / 4, PER = W / 8 ? 1 : 2;           // dwords; elements per dword
-        uint32_t d[W];
-        __builtin_memcpy(d, &r, sizeof r);
-        const int down = 8 - n;
-#pragma unroll
-        for (int step = 4; step >= PER; step /= 2)
-#pragma unroll
-            for (int i = 0; i < W; ++i) d[i] = down & step ? (i + step / PER < W ? d[i + step / PER] : 0u) : d[i];
-        if (PER == 2 && (down & 1)) {
-#pragma unroll
-            for (int i = 0; i < W; ++i) d[i] = __builtin_amdgcn_alignbit(i + 1 < W ? d[i + 1] : 0u, d[i], 16);
-        }
-        __builtin_memcpy(&r, d, sizeof r);
-    } else if (n > 0) {
+    if (FIT != CUT) {
+        if (FIT == FULL || c < D) __builtin_memcpy(&r, row + c, sizeof r);
+    } else if (D >= 8) {
+        if (c < D) __builtin_memcpy(&r, row + min(c, D - 8), sizeof r);
+    } else if (c < D) {
         T e[8] = {};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) e[i] = row[c + i];
+            if (c + i < D) e[i] = row[c + i];
         __builtin_memcpy(&r, e, sizeof r);
     }
+    return r;
+}
+template <int FIT, typename T>
+__device__ __forceinline__ void settle8(Raw8<T> &r, int c, int D)
+{
+    const int down = 8 - (D - c);
+    if (FIT != CUT || down <= 0 || down >= 8 || D < 8) return;
+    constexpr int W = (int)sizeof(r) / 4, PER = W / 8 ? 1 : 2;               // dwords; elements per dword
+    uint32_t d[W];
+    __builtin_memcpy(d, &r, sizeof r);
+#pragma unroll
+    for (int step = 4; step >= PER; step /= 2)
+#pragma unroll
+        for (int i = 0; i < W; ++i) d[i] = down & step ? (i + step / PER < W ? d[i + step / PER] : 0u) : d[i];
+    if (PER == 2 && (down & 1)) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) d[i] = __builtin_amdgcn_alignbit(i + 1 < W ? d[i + 1] : 0u, d[i], 16);
+    }
+    __builtin_memcpy(&r, d, sizeof r);
+}
+template <int FIT, typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *row, int c, int D)
+{
+    Raw8<T> r = fetch8<FIT>(row, c, D);
+    settle8<FIT>(r, c, D);
     return r;
 }
 template <typename T>

@@ -70,9 +70,9 @@ __global__ void __launch_bounds__(256) k_fp8_rows(const QuantParams p)
     const int64_t row = p.row0 + r;
     const int c = (int)b * 128 + (threadIdx.x & 15) * 8;
     const int n = min(8, max(0, p.K - c));
-    const Raw8<T> x = load8<false>(static_cast<const T *>(p.x) + row * p.ldx, c, p.K);
+    const Raw8<T> x = load8<CUT>(static_cast<const T *>(p.x) + row * p.ldx, c, p.K);
     Raw8<T> m{};
-    if constexpr (MUL) m = load8<false>(static_cast<const T *>(p.mul) + row * p.ldmul, c, p.K);
+    if constexpr (MUL) m = load8<CUT>(static_cast<const T *>(p.mul) + row * p.ldmul, c, p.K);
     float v[8], inverse;
     const uint32_t a = max16(act_and_max<ACT>(x, MUL ? &m : nullptr, v));
     const float s = fp8_scale(a, &inverse);
@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(256) k_fp8_tiles(const QuantParams p)
     for (int i = 0; i < 8; ++i) {
         const int64_t row = p.row0 + r0 + 16 * i;
         const int here = r0 + 16 * i < p.rows ? p.K : 0;    // (a row that is not there: no elements)
-        x[i] = load8<false>(static_cast<const T *>(p.x) + row * p.ldx, c, here);
-        if constexpr (MUL) m[i] = load8<false>(static_cast<const T *>(p.mul) + row * p.ldmul, c, here);
+        x[i] = load8<CUT>(static_cast<const T *>(p.x) + row * p.ldx, c, here);
+        if constexpr (MUL) m[i] = load8<CUT>(static_cast<const T *>(p.mul) + row * p.ldmul, c, here);
     }
     uint32_t a = 0;
     float v[8], inverse;

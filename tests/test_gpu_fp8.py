@@ -420,6 +420,16 @@ def test_norm_strides_and_alignment(nq, pad, offset, D):
     check_norm(nq, 5, D, "f16", "f16", "layer", "layer", pad=pad, offset=offset, in_place=True)
 
 
+@pytest.mark.parametrize("M,D", [(1100, 64), (1030, 128), (4200, 40), (2050, 200), (1025, 256), (3001, 77), (1111, 7), (20000, 24), (9, 4600), (300, 5120),
+                                 (257, 4611), (520, 5640), (515, 7168), (513, 8192), (3, 6000), (2, 7169), (260, 12288), (258, 10000), (270, 12800),
+                                 (3, 16376)])
+@pytest.mark.parametrize("dtype,stream", [("f16", "f16"), ("bf16", "f32"), ("f32", "f32")])
+def test_norm_rows_to_threads(nq, M, D, dtype, stream):
+    """Rows that share a wave, rows of one and of two chunks to a thread, more rows than workgroups."""
+    check_norm(nq, M, D, dtype, stream, "layer", "rms", gate=3, seed=D)
+    check_norm(nq, M, D, dtype, stream, "rms", "layer", seed=D + 1, in_place=True)
+
+
 def test_norm_parts(nq):
     """Without a branch, without weights, in place, with a single output of each kind, with nothing asked for."""
     for out in (("x",), ("q",), ("h",), ("h", "q")):
