@@ -92,13 +92,17 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     for (int l = 0; l < LOADS_X; ++l) off[LOADS_W + l] = (8 * (first_x + l) + (lane >> 3)) * ldx + piece_x[l & 1];
     off[PER_STAGE - 1] = sx_in ? (uint32_t)sx_at * (uint32_t)p.sxr * 4u : F8_OOR;
     uint8_t *const mine = lds + group * (KBYTES + SX);
-    const int last_kb = p.KB - 1, sx_step = G * (int)p.sxc * 4;
-    int kb = group - G, k_at = min(group, last_kb) * 128 - G * 128, sx_from = min(group, last_kb) * (int)p.sxc * 4 - sx_step;
-    auto next_block = [&] {
-        kb += G;
-        if (kb <= last_kb) {
-            k_at += G * 128;
-            sx_from += sx_step;
+    const int last_kb = p.KB - 1;
+    const uint32_t sx_col = (uint32_t)p.sxc * 4u;
+    int kb = group, k_at = min(group, last_kb) * 128;
+    uint32_t sx_from = (uint32_t)min(group, last_kb) * sx_col;
+    auto next_block = [&](bool first = false) {
+        if (!first) {
+            kb += G;
+            if (kb <= last_kb) {
+                k_at += G * 128;
+                sx_from += G * sx_col;
+            }
         }
         if (kb >= last_kb) {
             const int here = kb == last_kb ? p.K - last_kb * 128 : 0;
@@ -120,7 +124,7 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
             else if (l < LOADS_W + LOADS_X)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(dst + BN * 128 + (first_x + l - LOADS_W) * 1024), 16, (int)off[l], k_at, 0, 0);
             else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)(dst + KBYTES + (in_group % (SX / 256)) * 256), 4, (int)off[l], sx_from, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(sx_rsrc, (lds_ptr)(dst + KBYTES + (in_group % (SX / 256)) * 256), 4, (int)off[l], (int)sx_from, 0, 0);
         }
     };
 
@@ -176,8 +180,9 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
     auto after = [&](int at) { return at == (STAGES - 1) * STAGE ? 0 : at + STAGE; };
     auto before = [&](int at) { return at == 0 ? (STAGES - 1) * STAGE : at - STAGE; };
 
+#pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) {
-        next_block();
+        next_block(s == 0);
         issue(s * STAGE, 0, PER_STAGE);
     }
     float sw = scale_at();

@@ -526,3 +526,69 @@ def test_gemm_step_counts(nq, M, N, K, out):
     ld = dict(ld=-(-K // 16) * 16)
     check_gemm(nq, M, N, K, out=out, exact=True, seed=K, x_kw=ld, w_kw=ld)
     check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
+
+
+# ---- offsets past 32 bits ----------------------------------------------------------------------------------------
+
+def slices(M):
+    """Rows at both ends and around the middle of a long matrix, whole blocks of 128."""
+    return [slice(0, 256), slice(M // 256 * 128, M // 256 * 128 + 256), slice((M - 300) // 128 * 128, M)]
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantise_past_32_bits(nq, block_rows):
+    M, K = 264197, 16390
+    assert M * K > 2 ** 32
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda").normal_()
+    c = Codes(nq, M, K, block_rows=block_rows)
+    nq.nq_quantize_fp8(x, nq.NQ_DT_BF16, K, None, 0, nq.NQ_ACT_NONE, c.desc)
+    torch.cuda.synchronize()
+    for at in slices(M):
+        part = Codes(nq, at.stop - at.start, K, block_rows=block_rows)
+        nq.nq_quantize_fp8(x[at].contiguous(), nq.NQ_DT_BF16, K, None, 0, nq.NQ_ACT_NONE, part.desc)
+        torch.cuda.synchronize()
+        assert torch.equal(c.q[at, :K], part.q[:, :K])
+        assert torch.equal(c.scales[at.start // block_rows:-(-at.stop // block_rows)], part.scales)
+
+
+def test_norm_past_32_bits(nq):
+    M, D, bf = 530001, 8120, nq.NQ_DT_BF16
+    assert M * D > 2 ** 32
+    h, y = (torch.empty(M, D, dtype=torch.bfloat16, device="cuda").normal_() for _ in range(2))
+    ho, c, norm = torch.empty_like(h), Codes(nq, M, D), nq.make_norm(nq.NQ_NORM_RMS)
+
+    def call(h, y, ho, c, M):
+        nq.nq_block_norm(nq.make_block_norm(h, bf, D, y, bf, D, None, 0, 0, 1.0, 0.7, norm, norm, ho, D, None, 0, c.desc), M, D)
+        torch.cuda.synchronize()
+
+    call(h, y, ho, c, M)
+    for at in slices(M):
+        m = at.stop - at.start
+        part, pc = torch.empty(m, D, dtype=torch.bfloat16, device="cuda"), Codes(nq, m, D)
+        call(h[at].contiguous(), y[at].contiguous(), part, pc, m)
+        assert torch.equal(ho[at], part) and torch.equal(c.q[at, :D], pc.q[:, :D]) and torch.equal(c.scales[at], pc.scales)
+
+
+@pytest.mark.parametrize("K", [130, 100])
+def test_gemm_past_32_bits(nq, K):
+    """More rows than one launch has, scales of a column of blocks far apart, tokens and outputs past 32 bits."""
+    M, N, ld, f16 = 2 ** 25 + 37, 70, 144, nq.NQ_DT_F16
+    q = torch.randint(0, 120, (M, ld), dtype=torch.uint8, device="cuda")
+    xs = torch.rand(blocks(K), M, device="cuda") + 0.5
+    wq = torch.randint(0, 120, (N, ld), dtype=torch.uint8, device="cuda")
+    ws = torch.rand(1, blocks(K), device="cuda") * 2.0 ** -12
+    w = nq.make_fp8(wq, K, ws, 128)
+    y = torch.empty(M, N, dtype=torch.float16, device="cuda")
+    assert M * ld > 2 ** 32 and M * N * 2 > 2 ** 32
+    nq.nq_gemm_fp8(nq.make_fp8(q, K, xs.t()), w, None, y, f16, N)
+    torch.cuda.synchronize()
+    for at in slices(M) + [slice(2 ** 24 - 128, 2 ** 24 + 128)]:
+        m = at.stop - at.start
+        part = torch.empty(m, N, dtype=torch.float16, device="cuda")
+        nq.nq_gemm_fp8(nq.make_fp8(q[at].contiguous(), K, xs[:, at].contiguous().t()), w, None, part, f16, N)
+        torch.cuda.synchronize()
+        value = VALUES[q[at, :K].cpu().numpy()] * xs[:, at].t().double().cpu().numpy().repeat(128, 1)[:, :K]
+        want = value @ (VALUES[wq[:, :K].cpu().numpy()] * ws.double().cpu().numpy().repeat(128, 1)[:, :K]).T
+        got = y[at].double().cpu().numpy()
+        assert np.isfinite(want).all() and (np.abs(got - want) <= 2.0 ** -9 * np.abs(want)).all()       # (every term is positive)
+        assert (np.abs(part.double().cpu().numpy() - want) <= 2.0 ** -9 * np.abs(want)).all()
