@@ -82,10 +82,10 @@ static void launch_any(const Fp8GemmParams &p, hipStream_t s)
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
-// What a tile form takes, in microseconds, fitted to launches of 130 (fp32 outputs: 60) random sizes from 1 x 100 x 100 to 8192^3:
+// What a tile form takes, in microseconds, fitted to launches of 165 (fp32 outputs: 71) random sizes from 1 x 100 x 100 to 8192^3:
 // start + a round of tiles, `occ` to a compute unit, for each 256 * occ of them: per_tile + it * per_step, either with a part
 // that grows with the round's share of occupied units; it: steps of G column blocks.  The form with the least is taken: on those
-// sizes 0.9 % (0.5 %) slower than the fastest of 22 forms timed for each, 14 % (12 %) at worst.
+// sizes 0.4 % (0.3 %) slower than the fastest of 17 forms timed for each, 9 % (8 %) at worst.
 struct Fp8Form {
     int BN, BM, G, occ;
     float start, tile, tile_full, step, step_full;
@@ -101,28 +101,29 @@ static double form_time(const Fp8Form &f, int M, int N, int KB)
     return f.start + rounds * round(1.0) + (rest ? round(load) : 0.0);
 }
 
-// Few tokens: small tiles with many waves along the columns, two or four tiles to a unit: the weights stream (24 x 8192 x 8192 12.7 us,
-// 5.3 TB/s).  Some hundred: the largest tile of which there are still 256.  Many: tiles of 256 x 256 (16-bit outputs, 8192^3
+// Few tokens: small tiles with many waves along the columns: the weights stream (24 x 8192 x 8192 12.6 us, 5.4 TB/s), and up to 256 tiles
+// three stages have a unit's weights on their way at once (1 x 4096 x 4096 5.0 us, with two stages 5.8).  Some hundred: the largest tile of which there are still 256.  Many: tiles of 256 x 256 (16-bit outputs, 8192^3
 // 2.36 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
 // its loads 2.7); fp32 outputs need the registers for their wider operands and stay at 128 x 128.
 static const Fp8Form FORMS_16[] = {
-    {16, 16, 4, 4, 2.16f, 0.00f, 1.37f, 0.225f, 0.396f},   {16, 16, 8, 2, 2.15f, 0.03f, 1.43f, 0.290f, 0.432f},
-    {64, 16, 4, 1, 1.47f, 1.28f, 0.59f, 0.387f, 0.120f},   {64, 32, 4, 1, 1.44f, 2.12f, 0.59f, 0.468f, 0.158f},
-    {64, 64, 2, 2, 2.33f, 0.00f, 2.14f, 0.398f, 0.439f},   {128, 128, 1, 2, 2.91f, 0.00f, 4.22f, 0.400f, 0.628f},
-    {64, 64, 2, 1, 1.43f, 1.14f, 1.01f, 0.443f, 0.051f},   {128, 128, 1, 1, 1.72f, 0.82f, 2.69f, 0.353f, 0.220f},
-    {256, 128, 1, 1, 2.18f, 0.00f, 5.50f, 0.492f, 0.459f}, {256, 256, 1, 1, 1.77f, 0.00f, 8.95f, 0.832f, 0.851f}};
+    {16, 16, 4, 4, 2.10f, 0.00f, 1.30f, 0.240f, 0.407f},   {16, 16, 8, 1, 1.50f, 0.83f, 0.75f, 0.305f, 0.083f},
+    {64, 16, 4, 1, 1.50f, 1.20f, 0.63f, 0.369f, 0.142f},   {64, 32, 4, 1, 1.50f, 1.89f, 0.73f, 0.485f, 0.156f},
+    {64, 64, 2, 2, 2.21f, 0.00f, 2.10f, 0.439f, 0.410f},   {128, 128, 1, 2, 2.68f, 0.00f, 4.31f, 0.397f, 0.640f},
+    {64, 64, 2, 1, 1.38f, 1.19f, 0.99f, 0.446f, 0.043f},   {128, 128, 1, 1, 1.53f, 0.86f, 2.67f, 0.353f, 0.224f},
+    {256, 128, 1, 1, 2.02f, 0.00f, 5.47f, 0.478f, 0.497f}, {256, 256, 1, 1, 1.08f, 0.00f, 9.78f, 0.809f, 0.837f},
+    {32, 16, 4, 2, 2.35f, 0.00f, 1.79f, 0.244f, 0.266f}};
 static const Fp8Form FORMS_32[] = {
-    {16, 16, 4, 4, 2.13f, 0.00f, 1.49f, 0.301f, 0.303f},   {16, 16, 8, 2, 1.93f, 0.37f, 1.24f, 0.350f, 0.337f},
-    {64, 16, 4, 1, 1.32f, 1.52f, 0.52f, 0.543f, 0.042f},   {64, 32, 4, 1, 1.56f, 1.83f, 1.07f, 0.729f, 0.057f},
-    {64, 64, 2, 2, 2.50f, 0.00f, 2.41f, 0.553f, 0.631f},   {128, 128, 1, 2, 3.23f, 0.00f, 4.93f, 0.632f, 1.082f},
-    {64, 64, 4, 1, 1.69f, 1.40f, 1.85f, 1.101f, 0.122f},   {128, 128, 2, 1, 2.70f, 0.00f, 5.79f, 1.402f, 0.299f}};
+    {16, 16, 4, 4, 2.12f, 0.00f, 1.47f, 0.306f, 0.312f},   {16, 16, 8, 2, 2.12f, 0.09f, 1.45f, 0.353f, 0.353f},
+    {64, 16, 4, 1, 1.42f, 1.24f, 0.74f, 0.556f, 0.025f},   {64, 32, 4, 1, 1.53f, 1.75f, 1.10f, 0.779f, 0.011f},
+    {64, 64, 2, 2, 2.45f, 0.00f, 2.35f, 0.592f, 0.600f},   {128, 128, 1, 2, 3.17f, 0.00f, 4.67f, 0.639f, 1.089f},
+    {64, 64, 4, 1, 1.66f, 1.44f, 1.71f, 1.097f, 0.145f},   {128, 128, 2, 1, 2.62f, 0.00f, 5.60f, 1.278f, 0.454f}};
 
 template <typename T>
 static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
-    const int count = F32 ? 8 : 10;
+    const int count = F32 ? 8 : 11;
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < count; ++i) {
@@ -134,7 +135,7 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
     }
     switch (best) {
     case 0: return launch_tile<T, 16, 16, 16, 16, 4, 2, 1, false>(p, s);
-    case 1: return launch_tile<T, 16, 16, 16, 16, 8, 2, 2, false>(p, s);
+    case 1: return launch_tile<T, 16, 16, 16, 16, 8, F32 ? 2 : 3, 2, false>(p, s);
     case 2: return launch_tile<T, 64, 16, 32, 16, 4, 3, 2, false>(p, s);
     case 3: return launch_tile<T, 64, 32, 32, 16, 4, 3, 4, false>(p, s);
     case 4: return launch_tile<T, 64, 64, 32, 32, 2, 2, 2, false>(p, s);
@@ -151,7 +152,8 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
         case 6: return launch_tile<T, 64, 64, 32, 32, 2, 3, 2, false>(p, s);
         case 7: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
         case 8: return launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
-        default: return launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
+        case 9: return launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
+        default: return launch_tile<T, 32, 16, 16, 16, 4, 3, 2, false>(p, s);
         }
     }
 }

@@ -26,6 +26,11 @@ __device__ __forceinline__ void f8_tile_of(int id, int rows, int cols, int &bm, 
 {
     const int total = rows * cols, each = total >> 3, more = total & 7, xcd = id & 7, at = id >> 3;
     const int t = xcd * each + min(xcd, more) + at;
+    if (rows == 1) {                                     // (few tokens: no divisions)
+        bm = 0;
+        bn = t;
+        return;
+    }
     const int band = t / (8 * cols), in_band = t - band * 8 * cols, height = min(8, rows - band * 8);
     bn = in_band / height;
     bm = band * 8 + in_band - bn * height;

@@ -528,6 +528,20 @@ def test_gemm_step_counts(nq, M, N, K, out):
     check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
 
 
+# few tokens: rings of three stages, with fewer steps than stages and with groups of waves that have no block in the last step
+FEW_SIZES = [(1, 33, 1573), (3, 35, 2567), (1, 33, 3109), (16, 33, 3785), (1, 4096, 4096), (2, 1024, 2048), (405, 605, 2578), (17, 3285, 3642),
+             (1, 4146, 4105), (13, 4157, 4266), (35, 4329, 266), (33, 4146, 472), (34, 4126, 571), (33, 4233, 674), (49, 3223, 827),
+             (33, 4251, 897), (65, 3349, 1297), (33, 5654, 1516), (140, 5249, 294), (141, 5307, 417), (36, 5565, 778), (32, 4096, 4224)]
+
+
+@pytest.mark.parametrize("M,N,K", FEW_SIZES)
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_gemm_few_tokens(nq, M, N, K, out):
+    ld = dict(ld=-(-K // 16) * 16)
+    check_gemm(nq, M, N, K, out=out, exact=True, seed=K, x_kw=ld, w_kw=ld)
+    check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
+
+
 # ---- offsets past 32 bits ----------------------------------------------------------------------------------------
 
 def slices(M):
