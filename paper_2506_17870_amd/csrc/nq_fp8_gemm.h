@@ -111,13 +111,34 @@ __device__ __forceinline__ void fp8_store(const Fp8GemmParams &p, int m, int n, 
     }
 }
 
+// The biases of a lane's outputs n + 16 j + 4 (lane / 16) + 0 .. 3.
+template <int TN>
+__device__ __forceinline__ void fp8_bias(const Fp8GemmParams &p, int n, int lane, f8_f4 (&b)[TN])
+{
+    if (!p.bias) return;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int at = n + j * 16 + 4 * (lane >> 4);
+        b[j] = f8_f4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (at + 4 <= p.N) {
+            __builtin_memcpy(&b[j], p.bias + at, 16);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (at + q < p.N) b[j][q] = p.bias[at + q];
+        }
+    }
+}
+
 // A wave's 16 * TM tokens x 16 * TN outputs from token m and output n on.  The matrix core leaves a token's outputs in pieces of
 // four per lane: stored like that a wave's store would touch sixteen rows with 32 bytes each (a tile of 256 x 256 took 12 us).  They go
 // through LDS instead, `mine` being 16 * TM * TN * 16 elements that no other wave uses, and leave as whole rows, 16 bytes per lane at
 // any alignment (2773 x 2474 x 554, whose rows start on four bytes, 12.1 us; element by element 21.4).
 // The 16-byte units of a row lie exchanged so that sixteen rows' equal units, which one write covers, lie in different banks.
+// `bias`: those of the lane's outputs, from fp8_bias().
 template <typename T, int TN, int TM>
-__device__ __forceinline__ void fp8_store_tile(const Fp8GemmParams &p, int m, int n, f8_f4 (&acc)[TM][TN], uint8_t *mine, int lane)
+__device__ __forceinline__ void fp8_store_tile(const Fp8GemmParams &p, int m, int n, f8_f4 (&acc)[TM][TN], const f8_f4 (&bias)[TN], uint8_t *mine,
+                                               int lane)
 {
     const int r16 = lane & 15, g4 = lane >> 4;
     constexpr int ROW = TN * 16 * (int)sizeof(T), UNITS = ROW / 16, E = 16 / (int)sizeof(T);
@@ -125,15 +146,9 @@ __device__ __forceinline__ void fp8_store_tile(const Fp8GemmParams &p, int m, in
     auto place = [](int row, int unit) { return row * ROW + 16 * (unit ^ ((row / SHARE) & MASK)); };
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-        f8_f4 b = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (p.bias) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (n + j * 16 + 4 * g4 + q < p.N) b[q] = p.bias[n + j * 16 + 4 * g4 + q];
-        }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const f8_f4 v = p.bias ? acc[i][j] + b : acc[i][j];
+            const f8_f4 v = p.bias ? acc[i][j] + bias[j] : acc[i][j];
             if constexpr (sizeof(T) == 4) {
                 *reinterpret_cast<f8_f4 *>(mine + place(i * 16 + r16, j * 4 + g4)) = v;
             } else {

@@ -133,6 +133,10 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
         }
     };
 
+    // (small tiles: the biases are there when the sums are)
+    f8_f4 bias[TN];
+    if (TN <= 2 && group == 0) fp8_bias(p, n0 + wn, lane, bias);
+
     // ---- the product -----------------------------------------------------------------------------------------
     f8_f4 acc[TM][TN];
 #pragma unroll
@@ -304,7 +308,8 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] += sum[(((g - 1) * GROUP + in_group) * TM * TN + i * TN + j) * 64 + lane];
     }
-    fp8_store_tile<T, TN, TM>(p, m0 + wm, n0 + wn, acc, lds + SUMS + in_group * (TM * TN * 256 * (int)sizeof(T)), lane);
+    if (TN > 2) fp8_bias(p, n0 + wn, lane, bias);
+    fp8_store_tile<T, TN, TM>(p, m0 + wm, n0 + wn, acc, bias, lds + SUMS + in_group * (TM * TN * 256 * (int)sizeof(T)), lane);
 }
 
 template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC, bool AHEAD>
