@@ -82,10 +82,10 @@ static void launch_any(const Fp8GemmParams &p, hipStream_t s)
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
-// What a tile form takes, in microseconds, fitted to launches of 165 (fp32 outputs: 71) random sizes from 1 x 100 x 100 to 8192^3:
+// What a tile form takes, in microseconds, fitted to launches of 193 (fp32 outputs: 77) random sizes from 1 x 100 x 100 to 8192^3:
 // start + a round of tiles, `occ` to a compute unit, for each 256 * occ of them: per_tile + it * per_step, either with a part
 // that grows with the round's share of occupied units; it: steps of G column blocks.  The form with the least is taken: on those
-// sizes 0.4 % (0.3 %) slower than the fastest of 17 forms timed for each, 9 % (8 %) at worst.
+// sizes 0.8 % (0.4 %) slower than the fastest of 17 forms timed for each, 9 % at worst.
 struct Fp8Form {
     int BN, BM, G, occ;
     float start, tile, tile_full, step, step_full;
@@ -106,24 +106,24 @@ static double form_time(const Fp8Form &f, int M, int N, int KB)
 // 2.36 PFLOP/s; the register-only stream of these instructions and multiply-adds reaches 3.5 on such data, the same kernel without
 // its loads 2.7); fp32 outputs need the registers for their wider operands and stay at 128 x 128.
 static const Fp8Form FORMS_16[] = {
-    {16, 16, 4, 4, 2.10f, 0.00f, 1.30f, 0.240f, 0.407f},   {16, 16, 8, 1, 1.50f, 0.83f, 0.75f, 0.305f, 0.083f},
-    {64, 16, 4, 1, 1.50f, 1.20f, 0.63f, 0.369f, 0.142f},   {64, 32, 4, 1, 1.50f, 1.89f, 0.73f, 0.485f, 0.156f},
-    {64, 64, 2, 2, 2.21f, 0.00f, 2.10f, 0.439f, 0.410f},   {128, 128, 1, 2, 2.68f, 0.00f, 4.31f, 0.397f, 0.640f},
-    {64, 64, 2, 1, 1.38f, 1.19f, 0.99f, 0.446f, 0.043f},   {128, 128, 1, 1, 1.53f, 0.86f, 2.67f, 0.353f, 0.224f},
-    {256, 128, 1, 1, 2.02f, 0.00f, 5.47f, 0.478f, 0.497f}, {256, 256, 1, 1, 1.08f, 0.00f, 9.78f, 0.809f, 0.837f},
-    {32, 16, 4, 2, 2.35f, 0.00f, 1.79f, 0.244f, 0.266f}};
+    {16, 16, 4, 4, 2.15f, 0.00f, 1.33f, 0.218f, 0.439f},   {16, 16, 8, 1, 1.51f, 0.53f, 1.16f, 0.312f, 0.073f},
+    {64, 16, 4, 1, 1.58f, 0.68f, 1.16f, 0.414f, 0.102f},   {64, 32, 4, 1, 1.64f, 0.97f, 1.70f, 0.492f, 0.137f},
+    {64, 64, 2, 2, 2.01f, 0.00f, 2.15f, 0.408f, 0.461f},   {128, 128, 1, 2, 2.52f, 0.00f, 4.27f, 0.394f, 0.669f},
+    {64, 64, 2, 1, 1.43f, 0.79f, 1.36f, 0.396f, 0.081f},   {128, 128, 1, 1, 1.34f, 0.88f, 2.73f, 0.348f, 0.236f},
+    {256, 128, 1, 1, 1.88f, 0.00f, 5.52f, 0.450f, 0.539f}, {256, 256, 1, 1, 0.86f, 0.00f, 9.81f, 0.818f, 0.831f},
+    {32, 16, 4, 2, 2.27f, 0.00f, 1.87f, 0.236f, 0.278f},   {128, 64, 2, 1, 1.41f, 1.79f, 1.81f, 0.394f, 0.309f}};
 static const Fp8Form FORMS_32[] = {
-    {16, 16, 4, 4, 2.12f, 0.00f, 1.47f, 0.306f, 0.312f},   {16, 16, 8, 2, 2.12f, 0.09f, 1.45f, 0.353f, 0.353f},
-    {64, 16, 4, 1, 1.42f, 1.24f, 0.74f, 0.556f, 0.025f},   {64, 32, 4, 1, 1.53f, 1.75f, 1.10f, 0.779f, 0.011f},
-    {64, 64, 2, 2, 2.45f, 0.00f, 2.35f, 0.592f, 0.600f},   {128, 128, 1, 2, 3.17f, 0.00f, 4.67f, 0.639f, 1.089f},
-    {64, 64, 4, 1, 1.66f, 1.44f, 1.71f, 1.097f, 0.145f},   {128, 128, 2, 1, 2.62f, 0.00f, 5.60f, 1.278f, 0.454f}};
+    {16, 16, 4, 4, 2.14f, 0.00f, 1.45f, 0.280f, 0.365f},   {16, 16, 8, 2, 2.06f, 0.08f, 1.57f, 0.352f, 0.354f},
+    {64, 16, 4, 1, 1.43f, 1.08f, 0.96f, 0.539f, 0.063f},   {64, 32, 4, 1, 1.72f, 0.87f, 2.03f, 0.763f, 0.055f},
+    {64, 64, 2, 2, 2.39f, 0.00f, 2.47f, 0.563f, 0.643f},   {128, 128, 1, 2, 2.92f, 0.00f, 5.26f, 0.628f, 1.111f},
+    {64, 64, 4, 1, 1.74f, 0.81f, 2.38f, 1.051f, 0.252f},   {128, 128, 2, 1, 2.43f, 0.00f, 5.55f, 1.261f, 0.514f}};
 
 template <typename T>
 static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
-    const int count = F32 ? 8 : 11;
+    const int count = F32 ? 8 : 12;
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < count; ++i) {
@@ -153,7 +153,8 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
         case 7: return launch_tile<T, 128, 128, 64, 32, 1, 3, 2, true>(p, s);
         case 8: return launch_tile<T, 256, 128, 64, 64, 1, 3, 2, true>(p, s);
         case 9: return launch_tile<T, 256, 256, 128, 64, 1, 2, 2, true>(p, s);
-        default: return launch_tile<T, 32, 16, 16, 16, 4, 3, 2, false>(p, s);
+        case 10: return launch_tile<T, 32, 16, 16, 16, 4, 3, 2, false>(p, s);
+        default: return launch_tile<T, 128, 64, 64, 32, 2, 3, 2, true>(p, s);
         }
     }
 }

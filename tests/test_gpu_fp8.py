@@ -531,7 +531,8 @@ def test_gemm_step_counts(nq, M, N, K, out):
 # few tokens: rings of three stages, with fewer steps than stages and with groups of waves that have no block in the last step
 FEW_SIZES = [(1, 33, 1573), (3, 35, 2567), (1, 33, 3109), (16, 33, 3785), (1, 4096, 4096), (2, 1024, 2048), (405, 605, 2578), (17, 3285, 3642),
              (1, 4146, 4105), (13, 4157, 4266), (35, 4329, 266), (33, 4146, 472), (34, 4126, 571), (33, 4233, 674), (49, 3223, 827),
-             (33, 4251, 897), (65, 3349, 1297), (33, 5654, 1516), (140, 5249, 294), (141, 5307, 417), (36, 5565, 778), (32, 4096, 4224)]
+             (33, 4251, 897), (65, 3349, 1297), (33, 5654, 1516), (140, 5249, 294), (141, 5307, 417), (36, 5565, 778), (32, 4096, 4224),
+              (201, 6503, 1313), (130, 5563, 1970), (711, 5594, 1042), (256, 4096, 2048)]
 
 
 @pytest.mark.parametrize("M,N,K", FEW_SIZES)
