@@ -23,7 +23,6 @@ struct Fp8GemmParams {
     void *y;
     int64_t ldx, ldw, ldy, sxr, sxc, swr, swc;
     int M, N, K, KB;                       // KB: column blocks
-    int y_vec;                             // four outputs may be stored at once
     int sx_span;                           // bytes from the first scale of a tile's tokens to past the last (tiled kernel)
 };
 
@@ -81,34 +80,6 @@ __device__ __forceinline__ void fp8_add(f8_f4 &acc, f8_f4 p, float s)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(p[i], s, acc[i]);
-}
-
-// Outputs n .. n + 3 of token m.
-template <typename T>
-__device__ __forceinline__ void fp8_store(const Fp8GemmParams &p, int m, int n, f8_f4 v)
-{
-    if (m >= p.M || n >= p.N) return;
-    T *y = static_cast<T *>(p.y) + (int64_t)m * p.ldy + n;
-    const int left = p.N - n;
-    if (p.bias) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) v[i] += p.bias[n + i];
-    }
-    if (p.y_vec && left >= 4) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<f8_f4 *>(y) = v;
-        } else {
-            T o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) from_float(v[i], o + i);
-            *reinterpret_cast<uint2 *>(y) = __builtin_bit_cast(uint2, o);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) from_float(v[i], y + i);
-    }
 }
 
 // The biases of a lane's outputs n + 16 j + 4 (lane / 16) + 0 .. 3.

@@ -4,81 +4,129 @@
 namespace nq {
 
 // ---- any alignment ---------------------------------------------------------------------------------------------
-// Rows that start on any byte: a piece of 16 bytes is put together from the aligned dwords around it, of which only those
-// are read that hold a byte of the row.
-__device__ __forceinline__ f8_v4i fp8_piece(const uint8_t *p, int n)
+// Rows that start on any byte: the direct loads of the tiles want them on 16, ordinary ones do not.  A piece of 16 bytes that the row's
+// end cuts off is read as the row's last 16 and moved down by any_settle(); rows of fewer than 16 bytes go by bytes.
+__device__ __forceinline__ f8_v4i any_fetch(const uint8_t *row, int k, int K)
 {
     f8_v4i r = {0, 0, 0, 0};
-    if (n <= 0) return r;
-    const int a = (int)(reinterpret_cast<uintptr_t>(p) & 3);
-    const uint32_t *q = reinterpret_cast<const uint32_t *>(p - a);
-    uint32_t d[5];
+    if (k >= K) return r;
+    if (K >= 16) {
+        __builtin_memcpy(&r, row + min(k, K - 16), 16);
+    } else {
+        uint32_t d[4] = {};
 #pragma unroll
-    for (int i = 0; i < 5; ++i) d[i] = 4 * i - a < n && (i < 4 || a != 0) ? q[i] : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t v = __builtin_amdgcn_alignbyte(d[i + 1], d[i], a);
-        const int left = n - 4 * i;                        // bytes of this dword that belong to the row
-        v = left >= 4 ? v : left <= 0 ? 0u : v & ((1u << (8 * left)) - 1u);
-        r[i] = (int)v;
+        for (int i = 0; i < 16; ++i)
+            if (i < K) d[i >> 2] |= (uint32_t)row[i] << (8 * (i & 3));
+        __builtin_memcpy(&r, d, 16);
     }
     return r;
 }
-
-// Tile of 64 weight rows x 64 tokens, four waves of 32 x 32, one column block at a time through LDS.  A row's eight 16-byte
-// pieces lie exchanged, piece c at c ^ ((row / 2) & 7): two rows are once round the 64 banks, and sixteen rows' pieces c in
-// sixteen different places.
-template <typename T>
-__global__ void __launch_bounds__(256) k_fp8_gemm_any(const Fp8GemmParams p)
+__device__ __forceinline__ void any_settle(f8_v4i &r, int k, int K)
 {
-    __shared__ f8_v4i panel[2][64 * 8];                    // weights, tokens
+    const int down = 16 - (K - k);                         // bytes
+    if (down <= 0 || down >= 16 || K < 16) return;
+    uint32_t d[4];
+    __builtin_memcpy(d, &r, 16);
+#pragma unroll
+    for (int step = 2; step >= 1; step /= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = (down >> 2) & step ? (i + step < 4 ? d[i + step] : 0u) : d[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = __builtin_amdgcn_alignbyte(i + 1 < 4 ? d[i + 1] : 0u, d[i], down & 3);
+    __builtin_memcpy(&r, d, 16);
+}
+
+// Tile of 64 weight rows x 64 tokens, G groups of four waves of 32 x 32; group g takes the column blocks g, g + G, ... through LDS
+// of its own, the next block's pieces on their way in registers while one is worked on, and the groups' sums are added in order.
+// A row's eight 16-byte pieces lie exchanged, piece c at c ^ ((row / 2) & 7): two rows are once round the 64 banks, and sixteen rows'
+// pieces c in sixteen different places.  Bound by the loads' latency
+// and by placing what they bring: 16 x 4096 x 4096 17 us, 1024 x 4096 x 4096 68, 4096^3 186, where rows on 16 bytes take 5, 24 and
+// 62; put together from aligned dwords, without the next block ahead and in one group these took 51, 142 and 417.
+template <typename T, int G>
+__global__ void __launch_bounds__(256 * G) k_fp8_gemm_any(const Fp8GemmParams p)
+{
+    __shared__ f8_v4i lds[G][2][64 * 8];                   // weights, tokens
+    const int group = G == 1 ? 0 : threadIdx.x >> 8, id0 = threadIdx.x & 255;
     const int nblocks = (p.N + 63) / 64;
     const int bm = blockIdx.x / nblocks, bn = blockIdx.x - bm * nblocks;
     const int m0 = bm * 64, n0 = bn * 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = id0 >> 6;
     const int wn = (wave & 1) * 32, wm = (wave >> 1) * 32;
     const int r16 = lane & 15, g = lane >> 4;
+    auto &panel = lds[group];
+    const float *sw = p.sw + (int64_t)(min(n0 + wn, p.N - 1) >> 7) * p.swr;
+
+    f8_v4i piece[4];                                       // two of the weights, two of the tokens
+    float scale[3];                                        // of the lane's tokens and of the weights
+    auto fetch = [&](int kb) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int id = (i & 1) * 256 + id0, row = id >> 3, k = kb * 128 + (id & 7) * 16;
+            const int at = (i >= 2 ? m0 : n0) + row;
+            const bool there = kb < p.KB && at < (i >= 2 ? p.M : p.N);
+            piece[i] = any_fetch(i >= 2 ? p.x + (int64_t)at * p.ldx : p.w + (int64_t)at * p.ldw, there ? k : p.K, p.K);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + wm + i * 16 + r16;
+            scale[i] = kb < p.KB && m < p.M ? p.sx[(int64_t)m * p.sxr + (int64_t)kb * p.sxc] : 0.0f;
+        }
+        scale[2] = kb < p.KB ? sw[(int64_t)kb * p.swc] : 0.0f;
+    };
     f8_f4 acc[2][2] = {};
-    for (int kb = 0; kb < p.KB; ++kb) {
+    fetch(group);
+    for (int kb = group; kb - group < p.KB; kb += G) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int id = (i & 1) * 256 + threadIdx.x, row = id >> 3, c = id & 7, k = kb * 128 + c * 16;
-            const bool tokens = i >= 2;
-            const int at = (tokens ? m0 : n0) + row;
-            const int n = at < (tokens ? p.M : p.N) ? min(16, p.K - k) : 0;
-            const uint8_t *src = (tokens ? p.x + (int64_t)at * p.ldx : p.w + (int64_t)at * p.ldw) + k;
-            panel[tokens][row * 8 + (c ^ ((row >> 1) & 7))] = fp8_piece(src, n);
+            const int id = (i & 1) * 256 + id0, row = id >> 3, c = id & 7;
+            any_settle(piece[i], kb * 128 + c * 16, p.K);
+            panel[i >> 1][row * 8 + (c ^ ((row >> 1) & 7))] = piece[i];
         }
+        const float s[2] = {scale[0] * scale[2], scale[1] * scale[2]};
         __syncthreads();
-        const float sw = p.sw[(int64_t)((n0 + wn) >> 7) * p.swr + (int64_t)kb * p.swc];
+        fetch(kb + G);
         auto frag = [&](int which, int row) {
             const f8_v4i *q = panel[which] + row * 8;
-            const int s = (row >> 1) & 7;
+            const int e = (row >> 1) & 7;
             Fp8Operand<sizeof(T) == 4> o;
-            o.set(fp8_frag(q[g ^ s], q[(g + 4) ^ s]));
+            o.set(fp8_frag(q[g ^ e], q[(g + 4) ^ e]));
             return o;
         };
         const auto w0 = frag(0, wn + r16), w1 = frag(0, wn + 16 + r16);
 #pragma unroll
         for (int tm = 0; tm < 2; ++tm) {
-            const int m = m0 + wm + tm * 16 + r16;
-            const float s = m < p.M ? p.sx[(int64_t)m * p.sxr + (int64_t)kb * p.sxc] * sw : 0.0f;
             const auto x = frag(1, wm + tm * 16 + r16);
-            fp8_add(acc[tm][0], fp8_mfma(w0, x), s);
-            fp8_add(acc[tm][1], fp8_mfma(w1, x), s);
+            fp8_add(acc[tm][0], fp8_mfma(w0, x), s[tm]);
+            fp8_add(acc[tm][1], fp8_mfma(w1, x), s[tm]);
         }
     }
+    __syncthreads();
+    if constexpr (G > 1) {
+        f8_f4 *sum = reinterpret_cast<f8_f4 *>(lds);
+        if (group > 0)
 #pragma unroll
-    for (int tm = 0; tm < 2; ++tm)
+            for (int i = 0; i < 4; ++i) sum[((group - 1) * 4 + i) * 256 + id0] = acc[i >> 1][i & 1];
+        __syncthreads();
+        if (group > 0) return;
+        for (int h = 1; h < G; ++h)
 #pragma unroll
-        for (int tn = 0; tn < 2; ++tn) fp8_store<T>(p, m0 + wm + tm * 16 + r16, n0 + wn + tn * 16 + 4 * g, acc[tm][tn]);
+            for (int i = 0; i < 4; ++i) acc[i >> 1][i & 1] += sum[((h - 1) * 4 + i) * 256 + id0];
+    }
+    f8_f4 bias[2];
+    fp8_bias(p, n0 + wn, lane, bias);
+    // (the last group's part of the memory holds no sums)
+    fp8_store_tile<T, 2, 2>(p, m0 + wm, n0 + wn, acc, bias, reinterpret_cast<uint8_t *>(lds[G - 1]) + wave * (32 * 32 * (int)sizeof(T)), lane);
 }
 
 template <typename T>
 static void launch_any(const Fp8GemmParams &p, hipStream_t s)
 {
-    k_fp8_gemm_any<T><<<(unsigned)(ceil_div(p.M, 64) * ceil_div(p.N, 64)), 256, 0, s>>>(p);
+    const int64_t tiles = ceil_div(p.M, 64) * ceil_div(p.N, 64);
+    if (tiles <= 512)                                      // two to a compute unit
+        k_fp8_gemm_any<T, 4><<<(unsigned)tiles, 1024, 0, s>>>(p);
+    else
+        k_fp8_gemm_any<T, 1><<<(unsigned)tiles, 256, 0, s>>>(p);
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
@@ -190,7 +238,6 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     p.K = (int)w->cols;
     p.KB = (p.K + 127) / 128;
     const int es = dtype_bytes(dtype);
-    p.y_vec = aligned_to(d_y, 4 * es) && ldy % 4 == 0;
     // The tiles need rows on 16 bytes and scales that a buffer descriptor reaches from a tile's first token on.
     const int64_t span = (255 * p.sxr + (int64_t)std::max(0, p.KB - 1) * p.sxc + 1) * 4;
     const bool tiled = p.KB > 0 && aligned16(x->d_q) && aligned16(w->d_q) && x->ld % 16 == 0 && w->ld % 16 == 0 && span < (int64_t(1) << 30);

@@ -543,6 +543,14 @@ def test_gemm_few_tokens(nq, M, N, K, out):
     check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, x_kw=dict(by_row=True, **ld), w_kw=ld)
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 33, 15), (5, 70, 17), (70, 130, 1000), (100, 100, 513), (16, 2000, 4095), (1400, 1600, 129), (1500, 1800, 300)])
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_gemm_rows_on_any_byte(nq, M, N, K, out):
+    """Few tiles and many, rows of fewer and of more than sixteen bytes, starting anywhere."""
+    check_gemm(nq, M, N, K, out=out, exact=True, seed=K, x_kw=dict(ld=K + 3, offset=1), w_kw=dict(ld=K, offset=2))
+    check_gemm(nq, M, N, K, out=out, bias=True, seed=K + 1, ldy=N + 1, yoffset=1, x_kw=dict(ld=K + 1), w_kw=dict(ld=K + 5, offset=7))
+
+
 # ---- offsets past 32 bits ----------------------------------------------------------------------------------------
 
 def slices(M):
