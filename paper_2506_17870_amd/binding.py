@@ -214,6 +214,13 @@ def _stream(s):
     return s.cuda_stream
 
 
+def torch_stream(s, device=None) -> torch.cuda.Stream:
+    """The stream that a call's `stream` argument names, as torch's object: None (the current one), a raw handle or a stream."""
+    if s is None:
+        return torch.cuda.current_stream(device)
+    return torch.cuda.ExternalStream(s, device) if isinstance(s, int) else s
+
+
 def make_cfg(n_bits=8, l_bits=2, low_format=NQ_LOW_UNSIGNED_L, layout=NQ_LAYOUT_DENSE) -> nq_cfg:
     return nq_cfg(n_bits, l_bits, low_format, layout)
 
@@ -529,9 +536,15 @@ class Fp8Matrix:
 
     @classmethod
     def from_float(cls, d_w, block_rows=128, stream=None):
-        """nq_quantize_fp8 of [rows][cols] floats (weights; block_rows=1: activations)."""
+        """nq_quantize_fp8 of [rows][cols] floats (weights; block_rows=1: activations).  With a stream, it waits for the current
+        one, which has made the memory and fills it, and what it reads and writes is not given away before it is done."""
         dtype = {torch.float32: NQ_DT_F32, torch.float16: NQ_DT_F16, torch.bfloat16: NQ_DT_BF16}[d_w.dtype]
         self = cls(d_w.shape[0], d_w.shape[1], block_rows, d_w.device)
+        if stream is not None:
+            stream = torch_stream(stream, d_w.device)
+            stream.wait_stream(torch.cuda.current_stream(d_w.device))
+            for t in (self.q, self.scale, d_w):
+                t.record_stream(stream)
         nq_quantize_fp8(d_w, dtype, d_w.stride(0) if d_w.shape[0] > 1 else d_w.shape[1], None, 0, NQ_ACT_NONE, self.desc, stream)
         return self
 
