@@ -63,14 +63,14 @@ class Fp8Mlp:
         return self
 
     def forward(self, h, stream=None):
-        """h: [tokens][D] of h_dtype.  Returns the stream behind the last block (a buffer of this object: the next forward
+        """h: [tokens][D] of h_dtype.  stream: a stream or its raw handle, as for every call.  Returns the stream behind the last block (a buffer of this object: the next forward
         overwrites it)."""
         if self.tokens != h.shape[0]:
             self.allocate(h.shape[0])
         if stream is None:
             self.h.copy_(h)
         else:
-            with torch.cuda.stream(stream):
+            with torch.cuda.stream(nq.torch_stream(stream, h.device)):
                 self.h.copy_(h)
         return self.run(stream)
 

@@ -53,3 +53,23 @@ def test_floats_are_kept_until_they_are_read(nq, busy):
     others = [torch.full_like(w, 7.0) for _ in range(4)]         # (on the current stream, which does not wait)
     torch.cuda.synchronize()
     assert same(got, want) and len(others) == 4
+
+
+def mlp_layers(n=2, D=256, F=512):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    return [dict(up=r(2 * F, D) * D ** -0.5, down=r(D, F) * F ** -0.5, pre=1 + 0.1 * r(D), post=1 + 0.1 * r(D)) for _ in range(n)]
+
+
+def stream_of(tokens, D=256, seed=5):
+    return torch.randn(tokens, D, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(torch.bfloat16)
+
+
+def test_forward_takes_a_raw_handle(nq):
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    mlp, h, side = Fp8Mlp(mlp_layers()).allocate(9), stream_of(9), torch.cuda.Stream()
+    want = mlp.forward(h).clone()
+    torch.cuda.synchronize()
+    got = mlp.forward(h, side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got, want)
