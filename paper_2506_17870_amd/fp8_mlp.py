@@ -7,6 +7,8 @@ Everything a forward pass writes is allocated by allocate(), so that it can be c
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 import paper_2506_17870_amd as nq
@@ -21,7 +23,11 @@ class Fp8Mlp:
         pre     fp32 [D], weight of the RMS norm before the block
         post    fp32 [D] or absent, weight of the RMS norm after it
         gate    dtype [D] or absent, factors of the branch per channel
-    dtype: of branches and activations (the residual stream has h_dtype)."""
+    dtype: of branches and activations (the residual stream has h_dtype).
+
+    A pass runs on the stream it is given, else on the current one, where its input has to be ready.  It comes after all that this object
+    has on other streams (the weights' quantiser, the buffers' fills, the last pass), and what it uses is not given away before
+    that stream is done.  Of a stream given as a raw handle torch cannot know that once the object is gone: keep it until then."""
 
     def __init__(self, layers, act=nq.NQ_ACT_SILU, dtype=torch.bfloat16, h_dtype=None, eps=1e-5, residual_scale=1.0, branch_scale=1.0):
         self.act, self.dtype, self.h_dtype, self.eps = act, dtype, h_dtype or dtype, eps
@@ -36,11 +42,46 @@ class Fp8Mlp:
         if len({L["D"] for L in self.layers}) > 1:
             raise ValueError("the layers differ in width")
         self.tokens = None
+        self._weights = [t for L in self.layers for t in (L["up"].q, L["up"].scale, L["down"].q, L["down"].scale, L["pre"], L["post"], L["gate"])
+                         if t is not None]
+        self._device, self._buffers, self._recorded = self._weights[0].device, [], set()
+        # by handle: the streams that the next pass has to come after, those that came as handles with an event behind the last pass
+        self._home = torch.cuda.current_stream(self._device)
+        self._after = {self._home.cuda_stream: (self._home, None)}
+
+    def _wait(self, stream):
+        for handle, (other, event) in self._after.items():
+            if handle != stream.cuda_stream:
+                stream.wait_event(event or other.record_event())
+
+    @contextlib.contextmanager
+    def _on(self, stream):
+        """The stream as the current one, behind what _after names.  A stream that is captured cannot wait for work outside its graph:
+        torch waits for the device before a capture begins, and the order of replays and other passes is the caller's."""
+        with torch.cuda.stream(nq.torch_stream(stream, self._device)) if stream is not None else contextlib.nullcontext():
+            now = torch.cuda.current_stream(self._device)
+            if torch.cuda.is_current_stream_capturing():
+                yield now
+                return
+            self._wait(now)
+            if not isinstance(stream, int) and now.cuda_stream not in self._recorded:
+                self._recorded.add(now.cuda_stream)
+                for t in self._weights + self._buffers:
+                    t.record_stream(now)
+            try:
+                yield now
+            finally:
+                self._after = {now.cuda_stream: (now, now.record_event() if isinstance(stream, int) else None)}
 
     def allocate(self, tokens: int):
-        """Buffers and descriptors for `tokens` tokens."""
+        """Buffers and descriptors for `tokens` tokens, made on the current stream."""
+        now = torch.cuda.current_stream(self._device)
+        if not torch.cuda.is_current_stream_capturing():
+            self._wait(self._home)                        # the old buffers go back to the stream they were made on
+        self._home, self._recorded = now, set()
+        self._after.setdefault(now.cuda_stream, (now, None))
         self.tokens, self.D = tokens, self.layers[0]["D"]
-        dev = self.layers[0]["up"].q.device
+        dev = self._device
         self.x = nq.Fp8Matrix(tokens, self.D, device=dev)
         self.h = torch.empty(tokens, self.D, dtype=self.h_dtype, device=dev)
         self.branch = torch.empty(tokens, self.D, dtype=self.dtype, device=dev)
@@ -60,22 +101,27 @@ class Fp8Mlp:
                 self.h, hdt, self.D, self.branch if last else None, dt, self.D, gate, self.D, tokens if gate is not None else 0,
                 self.residual_scale if last else 1.0, self.branch_scale, post, pre, self.h if last else None, self.D, None, 0,
                 self.x.desc if L else None))
+        self._buffers = [self.h, self.branch, self.mid] + [t for m in (self.x, *self.a.values()) for t in (m.q, m.scale)]
         return self
 
     def forward(self, h, stream=None):
-        """h: [tokens][D] of h_dtype.  stream: a stream or its raw handle, as for every call.  Returns the stream behind the last block (a buffer of this object: the next forward
-        overwrites it)."""
+        """h: [tokens][D] of h_dtype.  stream: a stream or its raw handle, as for every call.  Returns the stream behind the last block
+        (a buffer of this object: the next forward overwrites it)."""
         if self.tokens != h.shape[0]:
-            self.allocate(h.shape[0])
-        if stream is None:
+            with torch.cuda.stream(nq.torch_stream(stream, self._device)):
+                self.allocate(h.shape[0])
+        with self._on(stream) as now:
             self.h.copy_(h)
-        else:
-            with torch.cuda.stream(nq.torch_stream(stream, h.device)):
-                self.h.copy_(h)
-        return self.run(stream)
+            if stream is not None and not isinstance(stream, int):
+                h.record_stream(now)
+            return self._pass(stream)
 
     def run(self, stream=None):
         """The same on the stream that lies in self.h already."""
+        with self._on(stream):
+            return self._pass(stream)
+
+    def _pass(self, stream):
         dt, es = _DTYPES[self.dtype], self.mid.element_size()
         for L, norm in zip(self.layers, self.norms):
             F, rows, a = L["F"], L["up"].rows, self.a[L["F"]]

@@ -73,3 +73,40 @@ def test_forward_takes_a_raw_handle(nq):
     got = mlp.forward(h, side.cuda_stream)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_passes_in_order_on_any_stream(nq, busy, raw):
+    """Weights quantised behind a busy stream, then passes of one and of another token count, each on another stream at once."""
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    layers, hs = mlp_layers(), [stream_of(t, seed=t) for t in (12, 40, 40, 12)]
+    wants = [Fp8Mlp(layers).forward(h).clone() for h in hs]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for first in (0, 1):                                     # (the allocator has memory to hand out again from the second time on)
+        torch.cuda.synchronize()
+        busy()
+        mlp, got = Fp8Mlp(layers), []
+        for i, h in enumerate(hs):
+            side = sides[(i + first) % 2]
+            if i == 1:
+                busy(side)                                   # the next pass, on the other stream, has to wait for this one
+            got.append(mlp.forward(h, side.cuda_stream if raw else side))
+        got.append(mlp.forward(hs[0]))
+        torch.cuda.synchronize()
+        for i in (0, 2, 4):                                  # (the others' buffer is overwritten by the pass behind them)
+            assert torch.equal(got[i], (wants + wants[:1])[i]), (first, i)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_buffers_are_kept_until_the_pass_is_done(nq, busy, raw):
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    layers, a, b = mlp_layers(), stream_of(40), stream_of(12)
+    mlp, side = Fp8Mlp(layers).allocate(40), torch.cuda.Stream()
+    want = mlp.forward(a).clone()
+    torch.cuda.synchronize()
+    busy(side)
+    kept = mlp.forward(a, side.cuda_stream if raw else side)          # (its buffer lives on with this name, the others do not)
+    mlp.forward(b)                                                    # another token count, on the current stream
+    others = [torch.full((n,), 9, dtype=torch.uint8, device="cuda") for n in (40 * 512, 40 * 1024 * 2, 40 * 256 * 2, 40 * 256, 640, 320, 512) * 3]
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want) and len(others) == 21
