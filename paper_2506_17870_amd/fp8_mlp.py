@@ -27,7 +27,12 @@ class Fp8Mlp:
 
     A pass runs on the stream it is given, else on the current one, where its input has to be ready.  It comes after all that this object
     has on other streams (the weights' quantiser, the buffers' fills, the last pass), and what it uses is not given away before
-    that stream is done.  Of a stream given as a raw handle torch cannot know that once the object is gone: keep it until then."""
+    that stream is done.  Of a stream given as a raw handle torch cannot know that once the object is gone: keep it until then.
+
+    A graph captured from run() or forward() holds this object's addresses: it needs the object as long as it is replayed.  The buffers of
+    a token count that was captured stay as they are, and allocate() or forward() with that count come back to them."""
+
+    _STATE = ("tokens", "x", "h", "branch", "mid", "a", "norms", "_buffers", "_home", "_recorded")        # what allocate() makes
 
     def __init__(self, layers, act=nq.NQ_ACT_SILU, dtype=torch.bfloat16, h_dtype=None, eps=1e-5, residual_scale=1.0, branch_scale=1.0):
         self.act, self.dtype, self.h_dtype, self.eps = act, dtype, h_dtype or dtype, eps
@@ -45,6 +50,7 @@ class Fp8Mlp:
         self._weights = [t for L in self.layers for t in (L["up"].q, L["up"].scale, L["down"].q, L["down"].scale, L["pre"], L["post"], L["gate"])
                          if t is not None]
         self._device, self._buffers, self._recorded = self._weights[0].device, [], set()
+        self._captured = {}                  # by token count: the state whose addresses are in a graph
         # by handle: the streams that the next pass has to come after, those that came as handles with an event behind the last pass
         self._home = torch.cuda.current_stream(self._device)
         self._after = {self._home.cuda_stream: (self._home, None)}
@@ -61,6 +67,7 @@ class Fp8Mlp:
         with torch.cuda.stream(nq.torch_stream(stream, self._device)) if stream is not None else contextlib.nullcontext():
             now = torch.cuda.current_stream(self._device)
             if torch.cuda.is_current_stream_capturing():
+                self._captured[self.tokens] = {name: getattr(self, name) for name in self._STATE}
                 yield now
                 return
             self._wait(now)
@@ -75,6 +82,9 @@ class Fp8Mlp:
 
     def allocate(self, tokens: int):
         """Buffers and descriptors for `tokens` tokens, made on the current stream."""
+        if tokens in self._captured:
+            self.__dict__.update(self._captured[tokens])
+            return self
         now = torch.cuda.current_stream(self._device)
         if not torch.cuda.is_current_stream_capturing():
             self._wait(self._home)                        # the old buffers go back to the stream they were made on

@@ -110,3 +110,25 @@ def test_buffers_are_kept_until_the_pass_is_done(nq, busy, raw):
     others = [torch.full((n,), 9, dtype=torch.uint8, device="cuda") for n in (40 * 512, 40 * 1024 * 2, 40 * 256 * 2, 40 * 256, 640, 320, 512) * 3]
     torch.cuda.synchronize()
     assert torch.equal(kept, want) and len(others) == 21
+
+
+def test_a_graph_keeps_its_buffers(nq):
+    """Passes with other token counts between the replays: the graph's memory stays its own, and so does everybody else's."""
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    layers = mlp_layers()
+    mlp, eager = Fp8Mlp(layers).allocate(12), Fp8Mlp(layers)
+    mlp.run()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        mlp.run()
+    h12 = mlp.h
+    for i, tokens in enumerate((40, 12, 3, 40)):
+        other = stream_of(tokens, seed=i)
+        assert torch.equal(mlp.forward(other), eager.forward(other))
+        others = [torch.full((n,), 9, dtype=torch.uint8, device="cuda") for n in (12 * 512, 12 * 1024 * 2, 12 * 256 * 2, 12 * 256, 96, 192) * 3]
+        h12.copy_(stream_of(12, seed=100 + i))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(h12, eager.forward(stream_of(12, seed=100 + i))), i
+        assert all(bool((t == 9).all()) for t in others), i
+    assert mlp.allocate(12).h is h12 and mlp.tokens == 12
