@@ -98,6 +98,8 @@ class nq_norm_job(ctypes.Structure):
                 ("h_dtype", ctypes.c_int32), ("dtype", ctypes.c_int32), ("residual_scale", ctypes.c_float),
                 ("branch_scale", ctypes.c_float), ("post", nq_norm), ("pre", nq_norm), ("d_h_out", ctypes.c_void_p),
                 ("ldh_out", ctypes.c_int64), ("d_x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("q", ctypes.POINTER(nq_fp8))]
+    # (for addresses that are not a tensor's) columns that the norms' vectors have, and what the gate's memory holds
+    _columns, _gate = 1 << 62, None
 
 
 if not os.path.exists(LIB_PATH):
@@ -486,8 +488,20 @@ def make_fp8(d_q, cols, d_scale, block_rows=1) -> nq_fp8:
     return desc
 
 
+_TORCH_OF = {NQ_DT_F32: torch.float32, NQ_DT_F16: torch.float16, NQ_DT_BF16: torch.bfloat16}
+
+
+def _typed(name, t, dtype):
+    """Refuses a tensor (None and addresses are nobody's) of another type than the call is told; the call itself refuses a type it does not know."""
+    if isinstance(t, torch.Tensor) and t.dtype != _TORCH_OF.get(dtype, t.dtype):
+        raise ValueError(f"{name} is of {t.dtype}, the call is told {_TORCH_OF[dtype]}")
+
+
 def make_norm(kind=NQ_NORM_RMS, eps=1e-5, d_weight=None, d_bias=None) -> nq_norm:
     """A norm over rows; d_weight and d_bias fp32[D] or None."""
+    vectors = [t for t in (d_weight, d_bias) if isinstance(t, torch.Tensor)]
+    if any(t.dtype != torch.float32 for t in vectors):
+        raise ValueError(f"the vectors of a norm must be fp32, got {[t.dtype for t in vectors]}")
     norm = nq_norm(kind, eps, _ptr(d_weight), _ptr(d_bias))
     norm._keep = (d_weight, d_bias)
     return norm
@@ -496,10 +510,24 @@ def make_norm(kind=NQ_NORM_RMS, eps=1e-5, d_weight=None, d_bias=None) -> nq_norm
 def make_block_norm(d_h, h_dtype, ldh, d_y, dtype, ldy, d_gate, ldgate, gate_rows, residual_scale, branch_scale, post: nq_norm,
                     pre: nq_norm, d_h_out, ldh_out, d_x, ldx, q: nq_fp8 | None = None) -> nq_norm_job:
     """Descriptor of one nq_block_norm call; None for what is not there.  It keeps everything it names alive."""
+    for name, t, of in (("d_h", d_h, h_dtype), ("d_y", d_y, dtype), ("d_gate", d_gate, dtype), ("d_h_out", d_h_out, h_dtype), ("d_x", d_x, dtype)):
+        _typed(name, t, of)
     job = nq_norm_job(_rows(d_h), ldh, _rows(d_y), ldy, _rows(d_gate), ldgate, gate_rows, h_dtype, dtype, residual_scale, branch_scale,
                       post, pre, _rows(d_h_out), ldh_out, _rows(d_x), ldx, ctypes.pointer(q) if q is not None else None)
     job._keep = (d_h, d_y, d_gate, post, pre, d_h_out, d_x, q)
+    lengths = [t.numel() for n in (post, pre) for t in getattr(n, "_keep", ()) if isinstance(t, torch.Tensor)]
+    if lengths:
+        job._columns = min(lengths)
+    if isinstance(d_gate, torch.Tensor):
+        job._gate = d_gate.untyped_storage().nbytes() // d_gate.element_size() - d_gate.storage_offset()
     return job
+
+
+def _norm_fits(job, M, D):
+    if D > job._columns:
+        raise ValueError(f"the norms' vectors have {job._columns} elements, a row has {D} columns")
+    if job._gate is not None and M > 0 and job.gate_rows > 0 and (M - 1) // job.gate_rows * job.ldgate + D > job._gate:
+        raise ValueError(f"the gate has {job._gate} elements: too few for {M} rows of {D}, {job.gate_rows} to a row of it")
 
 
 def nq_quantize_fp8(d_x, dtype, ldx, d_mul, ldmul, act, q: nq_fp8, stream=None):
@@ -510,6 +538,8 @@ def nq_quantize_fp8(d_x, dtype, ldx, d_mul, ldmul, act, q: nq_fp8, stream=None):
 
 
 def nq_gemm_fp8(x: nq_fp8, w: nq_fp8, d_bias, d_y, dtype, ldy, stream=None):
+    if isinstance(d_bias, torch.Tensor) and (d_bias.dtype != torch.float32 or d_bias.numel() < w.rows):
+        raise ValueError(f"d_bias must be fp32 [{w.rows}], got {d_bias.dtype} {tuple(d_bias.shape)}")
     st = _fast.gemm_fp8(x, w, d_bias, d_y, dtype, ldy, stream if stream is None else _stream(stream))
     if st >= 0:
         return _check(st, "nq_gemm_fp8")
@@ -517,6 +547,8 @@ def nq_gemm_fp8(x: nq_fp8, w: nq_fp8, d_bias, d_y, dtype, ldy, stream=None):
 
 
 def nq_block_norm(job: nq_norm_job, M, D, stream=None):
+    if D > job._columns or job._gate is not None:
+        _norm_fits(job, M, D)
     st = _fast.block_norm(job, M, D, stream if stream is None else _stream(stream))
     if st >= 0:
         return _check(st, "nq_block_norm")
