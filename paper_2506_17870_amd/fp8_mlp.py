@@ -42,6 +42,10 @@ class Fp8Mlp:
             D, F = L["down"].shape
             if L["up"].shape[1] != D or L["up"].shape[0] not in (F, 2 * F):
                 raise ValueError(f"up {tuple(L['up'].shape)} does not fit down {tuple(L['down'].shape)}")
+            for name, want in (("pre", torch.float32), ("post", torch.float32), ("gate", dtype)):
+                t = L.get(name)
+                if t is not None and (t.dtype != want or tuple(t.shape) != (D,)):
+                    raise ValueError(f"{name} must be {want} [{D}], got {t.dtype} {tuple(t.shape)}")
             self.layers.append(dict(D=D, F=F, gated=L["up"].shape[0] == 2 * F, up=nq.Fp8Matrix.from_float(L["up"].contiguous()),
                                     down=nq.Fp8Matrix.from_float(L["down"].contiguous()), pre=L["pre"], post=L.get("post"), gate=L.get("gate")))
         if len({L["D"] for L in self.layers}) > 1:
@@ -117,6 +121,8 @@ class Fp8Mlp:
     def forward(self, h, stream=None):
         """h: [tokens][D] of h_dtype.  stream: a stream or its raw handle, as for every call.  Returns the stream behind the last block
         (a buffer of this object: the next forward overwrites it)."""
+        if h.dim() != 2 or h.shape[1] != self.layers[0]["D"]:
+            raise ValueError(f"the stream must be [tokens][{self.layers[0]['D']}], got {tuple(h.shape)}")
         if self.tokens != h.shape[0]:
             with torch.cuda.stream(nq.torch_stream(stream, self._device)):
                 self.allocate(h.shape[0])

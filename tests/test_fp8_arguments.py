@@ -74,3 +74,21 @@ def test_bias_of_the_product(nq):
             nq.nq_gemm_fp8(x, w, bad, A, nq.NQ_DT_F32, 8, stream=0)
     for good in (torch.zeros(8), torch.zeros(9), A, None):
         nq.nq_gemm_fp8(x, w, good, A, nq.NQ_DT_F32, 8, stream=0)
+
+def test_layers_of_the_mlp(nq):
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    good = dict(up=torch.zeros(128, 64), down=torch.zeros(64, 128), pre=torch.ones(64))
+    for bad in (dict(pre=torch.ones(64, dtype=torch.bfloat16)), dict(post=torch.ones(64, dtype=torch.float16)), dict(pre=torch.ones(63)),
+                dict(post=torch.ones(1, 64)), dict(gate=torch.ones(64)), dict(gate=torch.ones(63, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError, match=next(iter(bad))):
+            Fp8Mlp([dict(good, **bad)], dtype=torch.bfloat16)
+
+
+def test_input_of_the_mlp(nq):
+    """A stream of another width is refused, not spread over the columns."""
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    mlp = Fp8Mlp.__new__(Fp8Mlp)
+    mlp.layers = [dict(D=64)]
+    for bad in (torch.zeros(4, 1), torch.zeros(4, 63), torch.zeros(64), torch.zeros(4, 64, 1)):
+        with pytest.raises(ValueError, match="64"):
+            mlp.forward(bad)
