@@ -189,8 +189,9 @@ extern "C" nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, co
     p.K = (int)q->cols;
     const uint32_t blocks = (uint32_t)ceil_div(q->cols, 128);
     p.by_blocks = make_divider(blocks);
-    // at most 2^30 blocks to a launch, whole blocks of 128 rows
-    const int64_t step = std::max<int64_t>(128, (int64_t(1) << 30) / blocks / 128 * 128);
+    // A dispatch has fewer than 2^32 threads: at most 2^27 blocks of columns with sixteen (with 128 rows each: eight) threads to one,
+    // whole blocks of 128 rows.
+    const int64_t step = std::max<int64_t>(128, (int64_t(1) << 27) / blocks / 128 * 128);
     for (p.row0 = 0; p.row0 < q->rows; p.row0 += step) {
         p.rows = (uint32_t)std::min(step, q->rows - p.row0);
         p.groups = p.rows * blocks;

@@ -1,0 +1,73 @@
+"""CPU checks of what the fp8 calls launch, against a stub of the HIP runtime (hip_stub.c): each part runs in a process of its own in which
+the stub is loaded before the library."""
+import ctypes
+import os
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+A = 1 << 44                                      # an address nobody reads
+
+
+@pytest.fixture(scope="module")
+def stub(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("stub") / "libstub.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", so, os.path.join(ROOT, "tests", "hip_stub.c")], check=True)
+    return so
+
+
+def in_process(stub, part):
+    env = dict(os.environ, PYTHONPATH=ROOT)
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), stub, part], capture_output=True, text=True, env=env, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
+
+
+@pytest.mark.parametrize("part", ["quantise_sizes"])
+def test_launches(stub, part):
+    in_process(stub, part)
+
+
+# ---- in the other process ------------------------------------------------------------------------------------------
+
+class Launch(ctypes.Structure):
+    _fields_ = [("kernel", ctypes.c_void_p), ("blocks", ctypes.c_uint64), ("threads", ctypes.c_uint64), ("lds", ctypes.c_uint64),
+                ("start", ctypes.c_uint64), ("stop", ctypes.c_uint64)]
+
+
+class Stub:
+    def __init__(self, path):
+        self.lib = ctypes.CDLL(path, mode=ctypes.RTLD_GLOBAL)
+        self.launches = (Launch * (1 << 16)).in_dll(self.lib, "stub_launches")
+        self.v = {n: ctypes.c_int.in_dll(self.lib, "stub_" + n) for n in ("count", "refused", "device", "fail_grants", "grant_calls")}
+
+    def take(self):
+        n, self.v["count"].value = self.v["count"].value, 0
+        assert n <= 1 << 16
+        return [(x.kernel, x.blocks, x.threads, x.lds) for x in self.launches[:n]]
+
+
+def fp8(nq, rows, cols, block_rows=1, ld=None):
+    ld = ld or -(-cols // 16) * 16
+    return nq.nq_fp8(A, rows, cols, ld, A, 1, -(-rows // block_rows), block_rows, 0)
+
+
+def quantise_sizes(nq, stub):
+    """From one row to more than a dispatch can have threads for, every block of 128 columns once."""
+    for block_rows in (1, 128):
+        for dtype in (nq.NQ_DT_F32, nq.NQ_DT_BF16):
+            for rows, cols in ((1, 1), (300, 1000), (1 << 20, 8192), (5 << 20, 8192), (1 << 20, 65536), ((1 << 28) + 1, 1), ((1 << 32) + 5, 100)):
+                nq.nq_quantize_fp8(A, dtype, cols, None, cols, nq.NQ_ACT_NONE, fp8(nq, rows, cols, block_rows), stream=0)
+                groups, got = -(-rows // block_rows) * -(-cols // 128), stub.take()
+                if block_rows == 1:
+                    assert groups <= sum(16 * b for _, b, _, _ in got) < groups + 16 * len(got)
+                else:
+                    assert sum(b for _, b, _, _ in got) == groups
+    assert stub.v["refused"].value == 0
+
+
+if __name__ == "__main__":
+    the_stub = Stub(sys.argv[1])
+    import paper_2506_17870_amd
+    globals()[sys.argv[2]](paper_2506_17870_amd, the_stub)
