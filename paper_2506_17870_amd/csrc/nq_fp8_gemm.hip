@@ -207,6 +207,8 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
     }
 }
 
+constexpr int64_t FP8_N_STEP = 1 << 20;                    // weight rows of a launch: whole tiles and blocks of 128
+
 }  // namespace nq
 
 using namespace nq;
@@ -224,9 +226,6 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     if (!aligned_to(d_bias, 4)) return NQ_ERR_ALIGN;
 
     Fp8GemmParams p;
-    p.w = w->d_q;
-    p.sw = w->d_scale;
-    p.bias = d_bias;
     p.ldx = x->ld;
     p.ldw = w->ld;
     p.ldy = ldy;
@@ -234,7 +233,6 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     p.sxc = x->scale_col_step;
     p.swr = w->scale_row_step;
     p.swc = w->scale_col_step;
-    p.N = (int)w->rows;
     p.K = (int)w->cols;
     p.KB = (p.K + 127) / 128;
     const int es = dtype_bytes(dtype);
@@ -242,20 +240,26 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     const int64_t span = (255 * p.sxr + (int64_t)std::max(0, p.KB - 1) * p.sxc + 1) * 4;
     const bool tiled = p.KB > 0 && aligned16(x->d_q) && aligned16(w->d_q) && x->ld % 16 == 0 && w->ld % 16 == 0 && span < (int64_t(1) << 30);
     p.sx_span = tiled ? (int)span : 0;
-    // at most 2^30 tiles of 16 x 16, and 2^24 rows, to a launch (whole tiles of every form)
-    const int64_t step = std::min<int64_t>(1 << 24, std::max<int64_t>(16, (int64_t(1) << 30) / ceil_div(p.N, 16)) * 16);
-    for (int64_t m = 0; m < x->rows; m += step) {
-        p.M = (int)std::min<int64_t>(step, x->rows - m);
-        p.x = x->d_q ? x->d_q + m * x->ld : nullptr;
-        p.sx = x->d_scale ? x->d_scale + m * x->scale_row_step : nullptr;
-        p.y = static_cast<uint8_t *>(d_y) + m * ldy * es;
-        if (dtype == NQ_DT_F32)
-            tiled ? launch_gemm<float>(p, (hipStream_t)stream) : launch_any<float>(p, (hipStream_t)stream);
-        else if (dtype == NQ_DT_F16)
-            tiled ? launch_gemm<_Float16>(p, (hipStream_t)stream) : launch_any<_Float16>(p, (hipStream_t)stream);
-        else
-            tiled ? launch_gemm<bf16_t>(p, (hipStream_t)stream) : launch_any<bf16_t>(p, (hipStream_t)stream);
-        if ((st = launch_status()) != NQ_OK) return st;
+    // A dispatch has fewer than 2^32 threads: at most 2^22 tiles of 16 x 16, of up to 512 threads, go to one; whole tiles of every form.
+    for (int64_t n = 0; n < w->rows; n += FP8_N_STEP) {
+        p.N = (int)std::min(FP8_N_STEP, w->rows - n);
+        p.w = w->d_q ? w->d_q + n * w->ld : nullptr;
+        p.sw = w->d_scale ? w->d_scale + n / 128 * w->scale_row_step : nullptr;
+        p.bias = d_bias ? d_bias + n : nullptr;
+        const int64_t step = std::min<int64_t>(1 << 24, (1 << 22) / ceil_div(p.N, 16) * 16 / 256 * 256);
+        for (int64_t m = 0; m < x->rows; m += step) {
+            p.M = (int)std::min<int64_t>(step, x->rows - m);
+            p.x = x->d_q ? x->d_q + m * x->ld : nullptr;
+            p.sx = x->d_scale ? x->d_scale + m * x->scale_row_step : nullptr;
+            p.y = static_cast<uint8_t *>(d_y) + (m * ldy + n) * es;
+            if (dtype == NQ_DT_F32)
+                tiled ? launch_gemm<float>(p, (hipStream_t)stream) : launch_any<float>(p, (hipStream_t)stream);
+            else if (dtype == NQ_DT_F16)
+                tiled ? launch_gemm<_Float16>(p, (hipStream_t)stream) : launch_any<_Float16>(p, (hipStream_t)stream);
+            else
+                tiled ? launch_gemm<bf16_t>(p, (hipStream_t)stream) : launch_any<bf16_t>(p, (hipStream_t)stream);
+            if ((st = launch_status()) != NQ_OK) return st;
+        }
     }
     return NQ_OK;
 }

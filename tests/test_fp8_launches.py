@@ -24,7 +24,7 @@ def in_process(stub, part):
     assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
 
 
-@pytest.mark.parametrize("part", ["quantise_sizes"])
+@pytest.mark.parametrize("part", ["quantise_sizes", "product_sizes"])
 def test_launches(stub, part):
     in_process(stub, part)
 
@@ -64,6 +64,18 @@ def quantise_sizes(nq, stub):
                     assert groups <= sum(16 * b for _, b, _, _ in got) < groups + 16 * len(got)
                 else:
                     assert sum(b for _, b, _, _ in got) == groups
+    assert stub.v["refused"].value == 0
+
+
+def product_sizes(nq, stub):
+    """From one output to more tiles than a dispatch can have threads for, over rows and over columns, on 16 bytes and on any."""
+    for dtype in (nq.NQ_DT_F32, nq.NQ_DT_F16):
+        for aligned in (True, False):
+            for M, N, K in ((1, 1, 1), (1, 4096, 4096), (24, 1 << 20, 130), (1, 1 << 30, 1), (300, (1 << 30) - 5, 16), (1 << 24, 4096, 128),
+                            ((1 << 25) + 37, 70, 130), ((1 << 28) + 1, 1, 1), (1 << 22, 1 << 18, 256)):
+                ld = None if aligned else K + 1 if (K + 1) % 16 else K
+                nq.nq_gemm_fp8(fp8(nq, M, K, 1, ld), fp8(nq, N, K, 128, ld), None, A, dtype, N, stream=0)
+                assert stub.take(), (M, N, K)
     assert stub.v["refused"].value == 0
 
 
