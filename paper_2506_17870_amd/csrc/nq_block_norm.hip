@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(LONG_TH) k_block_norm_long(const NormParams p)
 }
 
 template <typename T, typename H, int TH, int CH = 1>
-static void launch_norm(const NormParams &p, hipStream_t s)
+static nq_status launch_norm(const NormParams &p, hipStream_t s)
 {
     // up to sixteen waves to a compute unit (16384 x 4096 bf16 90 us; 8: 126, 24: 103)
     constexpr int ROWS = norm_rows(TH), WG = TH * ROWS;
@@ -340,10 +340,11 @@ static void launch_norm(const NormParams &p, hipStream_t s)
     } else {
         k_block_norm<T, H, TH, CH, CUT><<<grid, WG, 0, s>>>(p);
     }
+    return launch_status();
 }
 
 template <typename T, typename H>
-static void norm_by_size(const NormParams &p, hipStream_t s)
+static nq_status norm_by_size(const NormParams &p, hipStream_t s)
 {
     constexpr bool WIDE = sizeof(H) == 4;                   // the stream takes half of the registers
     const int chunks = (p.D + 7) / 8;
@@ -372,10 +373,12 @@ static void norm_by_size(const NormParams &p, hipStream_t s)
     }
     if (chunks <= 768) return launch_norm<T, H, 768>(p, s);
     if (chunks <= 1024) return launch_norm<T, H, 1024>(p, s);
-    const int lds = chunks * 32;
     auto k = k_block_norm_long<T, H>;
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    k<<<(unsigned)std::min<int64_t>(p.M, 1 << 20), LONG_TH, lds, s>>>(p);
+    static std::atomic<uint64_t> granted{0};
+    const nq_status st = grant_lds(k, NQ_NORM_MAX_D * 4, granted);
+    if (st != NQ_OK) return st;
+    k<<<(unsigned)std::min<int64_t>(p.M, 1 << 20), LONG_TH, chunks * 32, s>>>(p);
+    return launch_status();
 }
 
 static nq_status check_norm(const nq_norm &n)
@@ -447,15 +450,7 @@ extern "C" nq_status nq_block_norm(const nq_norm_job *job, int64_t M, int64_t D,
     p.pre = j.pre.kind;
     p.D = (int)D;
     hipStream_t s = (hipStream_t)stream;
-    if (j.dtype == NQ_DT_F32)
-        norm_by_size<float, float>(p, s);
-    else if (j.dtype == NQ_DT_F16 && j.h_dtype == NQ_DT_F16)
-        norm_by_size<_Float16, _Float16>(p, s);
-    else if (j.dtype == NQ_DT_F16)
-        norm_by_size<_Float16, float>(p, s);
-    else if (j.h_dtype == NQ_DT_BF16)
-        norm_by_size<bf16_t, bf16_t>(p, s);
-    else
-        norm_by_size<bf16_t, float>(p, s);
-    return launch_status();
+    if (j.dtype == NQ_DT_F32) return norm_by_size<float, float>(p, s);
+    if (j.dtype == NQ_DT_F16) return j.h_dtype == NQ_DT_F16 ? norm_by_size<_Float16, _Float16>(p, s) : norm_by_size<_Float16, float>(p, s);
+    return j.h_dtype == NQ_DT_BF16 ? norm_by_size<bf16_t, bf16_t>(p, s) : norm_by_size<bf16_t, float>(p, s);
 }

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "nq_common.h"
 
@@ -248,6 +249,27 @@ inline nq_status check_matrix(const void *p, int dtype, int64_t cols, int64_t ld
     return aligned_to(p, dtype_bytes(dtype)) ? NQ_OK : NQ_ERR_ALIGN;
 }
 inline bool rows_on_16(const void *p, int dtype, int64_t ld) { return !p || (aligned16(p) && ld * dtype_bytes(dtype) % 16 == 0); }
+
+// Grants a kernel `bytes` of dynamic LDS, more than the 64 KB that every kernel has: once on each device, whose copy of the kernel
+// it is that has the limit (`devices`: those done, a static of the caller's for each kernel).  A refusal is reported, and the next call asks
+// again.  `bytes` is the most that the kernel is ever launched with, so that no call lowers the limit under another.
+template <typename K>
+nq_status grant_lds(K kernel, int bytes, std::atomic<uint64_t> &devices)
+{
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) {
+        (void)hipGetLastError();
+        return NQ_ERR_HIP;
+    }
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (devices.load(std::memory_order_acquire) & bit) return NQ_OK;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        return NQ_ERR_HIP;
+    }
+    devices.fetch_or(bit, std::memory_order_release);
+    return NQ_OK;
+}
 
 // n / d == (n * m) >> (32 + s) for every n < 2^31 and 1 <= d < 2^31, m and s made here (m fits 32 bits: 2^(32+s) / d with
 // 2^s <= d < 2^(s+1) lies in (2^31, 2^32]; rounded up it is off by less than one part in 2^31 / n).  d = 1 gives m = 2^32,

@@ -120,13 +120,14 @@ __global__ void __launch_bounds__(256 * G) k_fp8_gemm_any(const Fp8GemmParams p)
 }
 
 template <typename T>
-static void launch_any(const Fp8GemmParams &p, hipStream_t s)
+static nq_status launch_any(const Fp8GemmParams &p, hipStream_t s)
 {
     const int64_t tiles = ceil_div(p.M, 64) * ceil_div(p.N, 64);
     if (tiles <= 512)                                      // two to a compute unit
         k_fp8_gemm_any<T, 4><<<(unsigned)tiles, 1024, 0, s>>>(p);
     else
         k_fp8_gemm_any<T, 1><<<(unsigned)tiles, 256, 0, s>>>(p);
+    return launch_status();
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
@@ -167,7 +168,7 @@ static const Fp8Form FORMS_32[] = {
     {64, 64, 4, 1, 1.74f, 0.81f, 2.38f, 1.051f, 0.252f},   {128, 128, 2, 1, 2.43f, 0.00f, 5.55f, 1.261f, 0.514f}};
 
 template <typename T>
-static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
+static nq_status launch_gemm(const Fp8GemmParams &p, hipStream_t s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
@@ -191,10 +192,8 @@ static void launch_gemm(Fp8GemmParams &p, hipStream_t s)
     default: break;
     }
     if constexpr (F32) {
-        if (best == 6)
-            launch_tile<T, 64, 64, 32, 32, 4, 2, 4, false>(p, s);
-        else
-            launch_tile<T, 128, 128, 64, 64, 2, 2, 2, true>(p, s);
+        if (best == 6) return launch_tile<T, 64, 64, 32, 32, 4, 2, 4, false>(p, s);
+        return launch_tile<T, 128, 128, 64, 64, 2, 2, 2, true>(p, s);
     } else {
         switch (best) {
         case 6: return launch_tile<T, 64, 64, 32, 32, 2, 3, 2, false>(p, s);
@@ -253,12 +252,12 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
             p.sx = x->d_scale ? x->d_scale + m * x->scale_row_step : nullptr;
             p.y = static_cast<uint8_t *>(d_y) + (m * ldy + n) * es;
             if (dtype == NQ_DT_F32)
-                tiled ? launch_gemm<float>(p, (hipStream_t)stream) : launch_any<float>(p, (hipStream_t)stream);
+                st = tiled ? launch_gemm<float>(p, (hipStream_t)stream) : launch_any<float>(p, (hipStream_t)stream);
             else if (dtype == NQ_DT_F16)
-                tiled ? launch_gemm<_Float16>(p, (hipStream_t)stream) : launch_any<_Float16>(p, (hipStream_t)stream);
+                st = tiled ? launch_gemm<_Float16>(p, (hipStream_t)stream) : launch_any<_Float16>(p, (hipStream_t)stream);
             else
-                tiled ? launch_gemm<bf16_t>(p, (hipStream_t)stream) : launch_any<bf16_t>(p, (hipStream_t)stream);
-            if ((st = launch_status()) != NQ_OK) return st;
+                st = tiled ? launch_gemm<bf16_t>(p, (hipStream_t)stream) : launch_any<bf16_t>(p, (hipStream_t)stream);
+            if (st != NQ_OK) return st;
         }
     }
     return NQ_OK;

@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
 }
 
 template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC, bool AHEAD>
-static void launch_tile(const Fp8GemmParams &p, hipStream_t s)
+static nq_status launch_tile(const Fp8GemmParams &p, hipStream_t s)
 {
     constexpr int GROUP = (BN / WN) * (BM / WM);
     constexpr int ring = STAGES * G * ((BN + BM) * 128 + (BM < 64 ? 64 : BM) * 4);
@@ -322,12 +322,13 @@ static void launch_tile(const Fp8GemmParams &p, hipStream_t s)
     constexpr int lds = ring > last ? ring : last;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     auto k = k_fp8_gemm_tile<T, BN, BM, WN, WM, G, STAGES, OCC, AHEAD>;
-    static bool granted = false;
-    if (!granted) {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        granted = true;
+    if constexpr (lds > 64 * 1024) {
+        static std::atomic<uint64_t> granted{0};
+        const nq_status st = grant_lds(k, lds, granted);
+        if (st != NQ_OK) return st;
     }
     k<<<(unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN)), 64 * G * GROUP, lds, s>>>(p);
+    return launch_status();
 }
 
 }  // namespace nq

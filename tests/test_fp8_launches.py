@@ -24,7 +24,7 @@ def in_process(stub, part):
     assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
 
 
-@pytest.mark.parametrize("part", ["quantise_sizes", "product_sizes"])
+@pytest.mark.parametrize("part", ["quantise_sizes", "product_sizes", "grants"])
 def test_launches(stub, part):
     in_process(stub, part)
 
@@ -77,6 +77,41 @@ def product_sizes(nq, stub):
                 nq.nq_gemm_fp8(fp8(nq, M, K, 1, ld), fp8(nq, N, K, 128, ld), None, A, dtype, N, stream=0)
                 assert stub.take(), (M, N, K)
     assert stub.v["refused"].value == 0
+
+
+def grants(nq, stub):
+    """LDS beyond 64 KB: asked for on every device, not given twice, an error where it is refused, and asked for again after that."""
+    def product(dtype=nq.NQ_DT_BF16, M=8192, N=8192):
+        nq.nq_gemm_fp8(fp8(nq, M, 1024), fp8(nq, N, 1024, 128), None, A, dtype, N, stream=0)
+
+    def norm(D=32768):
+        none = nq.make_norm(nq.NQ_NORM_NONE)
+        nq.nq_block_norm(nq.make_block_norm(A, 0, D, A, 0, D, None, 0, 0, 1.0, 1.0, none, none, A, D, None, 0), 8, D, stream=0)
+
+    for call in (product, norm, lambda: product(nq.NQ_DT_F32), lambda: product(M=600, N=8192)):
+        stub.v["device"].value, stub.v["fail_grants"].value = 0, 1
+        try:
+            call()
+        except nq.NQError as e:
+            assert e.status == nq.NQ_ERR_HIP
+        else:
+            raise AssertionError("a refused grant was not reported")
+        assert not stub.take() and stub.v["refused"].value == 0, "launched without the grant"
+        for device in (0, 3, 0, 3):
+            stub.v["device"].value = device
+            call()
+            assert len(stub.take()) == 1 and stub.v["refused"].value == 0
+        calls = stub.v["grant_calls"].value
+        for device in (0, 3):
+            stub.v["device"].value = device
+            call()
+        assert stub.v["grant_calls"].value == calls
+        stub.take()
+    stub.v["device"].value = 0
+    calls = stub.v["grant_calls"].value
+    norm(9000)                                   # (a smaller row changes nothing for a longer one)
+    norm()
+    assert stub.v["grant_calls"].value == calls and len(stub.take()) == 2
 
 
 if __name__ == "__main__":
