@@ -359,15 +359,17 @@ nq_status nq_gconv_part(const int8_t *d_x, const nq_conv_shape *shape, int group
 typedef enum { NQ_TUNE_KERNEL = 0, NQ_TUNE_BIG_TM = 1, NQ_TUNE_GC_UNITS = 2, NQ_TUNE_STAT_ROWS = 3, NQ_TUNE_COUNT = 4 } nq_tune_key;
 nq_status nq_set_tuning(int key, int value);
 
-/* Profiling aid: the next nq_gemm_* (nq_gemm_batch included) / nq_conv_* / nq_gconv_* call made by this host thread attaches the two
- * hipEvent_t (either may be NULL) to its kernel dispatch, so that hipEventElapsedTime(start,
- * stop) is the execution time of that kernel alone.  One shot; events are the caller's. */
+/* Profiling aid: the next nq_gemm_* (nq_gemm_batch and nq_gemm_fp8 included) / nq_conv_* / nq_gconv_* call made by this host thread
+ * attaches the two hipEvent_t (either may be NULL) to its kernel dispatch, so that hipEventElapsedTime(start,
+ * stop) is the execution time of that kernel alone (of an nq_gemm_fp8 too large for one dispatch: from its first to its last).
+ * One shot; events are the caller's. */
 nq_status nq_profile_next_launch(void *start_event, void *stop_event);
 /* Profiling aid: which kernel the last nq_gemm_* / nq_conv_* / nq_gconv_* launch of this host thread ran:
  * *family as in NQ_TUNE_KERNEL (7 = depthwise / grouped on the matrix cores, 8 = word pages, 10 = other
  * grouped convolutions; 0 before the first launch), *variant for family 10: 2 wider groups on the matrix cores, 1 or 0
  * the direct kernel by dwords or by bytes; for family 6, few rows: 0 a single call, 1 a batch; for family 8 the row tiles of a
- * block (1 or 2); else the tile height of the large-GEMM kernel (2..7), the tile shape of the generic kernel, the waves along N of the stationary-weights GEMM,
+ * block (1 or 2); family 12 is nq_gemm_fp8: the tile form's place in its table (8 forms for fp32 outputs, 12 for 16-bit ones), or 100 + the
+ * groups of waves (1 or 4) for rows that do not start on 16 bytes; else the tile height of the large-GEMM kernel (2..7), the tile shape of the generic kernel, the waves along N of the stationary-weights GEMM,
  * else 0.  Lets a benchmark group its time stamps by kernel instantiation, as a kernel trace does.  Either pointer may be
  * NULL. */
 nq_status nq_profile_last_kernel(int *family, int *variant);

@@ -440,7 +440,7 @@ def nq_profile_next_launch(start_event, stop_event):
 
 
 def nq_profile_last_kernel():
-    """(family, variant) of the last GEMM / convolution launch of this thread."""
+    """(family, variant) of the last GEMM / convolution launch of this thread (family 12: nq_gemm_fp8)."""
     fam, var = ctypes.c_int(), ctypes.c_int()
     _check(_lib.nq_profile_last_kernel(ctypes.byref(fam), ctypes.byref(var)), "nq_profile_last_kernel")
     return fam.value, var.value

@@ -10,6 +10,8 @@
 // itself, but by powers of two only.)  A lane of either operand holds 32 bytes of a row; which of the block's columns they
 // are does not matter as long as both operands agree, so a lane takes the 16-byte pieces lane / 16 and 4 + lane / 16.
 #pragma once
+#include <hip/hip_ext.h>
+
 #include "nq_fp8.h"
 
 namespace nq {
@@ -151,6 +153,27 @@ __device__ __forceinline__ void fp8_store_tile(const Fp8GemmParams &p, int m, in
                 if (col + q < p.N) y[q] = e[q];
         }
     }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+// nq_gemm.hip: the events of nq_profile_next_launch, which are taken by this, and what nq_profile_last_kernel reports.
+void take_profile_events(void **start, void **stop);
+void note_last_kernel(int family, int variant);
+constexpr int FP8_FAMILY = 12, FP8_ANY = 100;            // variants: the tile form, or FP8_ANY + groups for rows on any byte
+
+struct Fp8Launch {
+    hipStream_t stream;
+    void *start, *stop;                                  // events of this launch, or null
+};
+template <typename K>
+nq_status launch_fp8(const Fp8Launch &at, K kernel, int64_t tiles, int threads, int lds, const Fp8GemmParams &p)
+{
+    if (at.start || at.stop)
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(threads), (uint32_t)lds, at.stream, (hipEvent_t)at.start, (hipEvent_t)at.stop, 0, p);
+    else
+        kernel<<<(unsigned)tiles, threads, lds, at.stream>>>(p);
+    return launch_status();
 }
 
 }  // namespace nq

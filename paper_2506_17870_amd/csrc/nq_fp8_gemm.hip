@@ -120,14 +120,12 @@ __global__ void __launch_bounds__(256 * G) k_fp8_gemm_any(const Fp8GemmParams p)
 }
 
 template <typename T>
-static nq_status launch_any(const Fp8GemmParams &p, hipStream_t s)
+static nq_status launch_any(const Fp8GemmParams &p, const Fp8Launch &s)
 {
     const int64_t tiles = ceil_div(p.M, 64) * ceil_div(p.N, 64);
-    if (tiles <= 512)                                      // two to a compute unit
-        k_fp8_gemm_any<T, 4><<<(unsigned)tiles, 1024, 0, s>>>(p);
-    else
-        k_fp8_gemm_any<T, 1><<<(unsigned)tiles, 256, 0, s>>>(p);
-    return launch_status();
+    const bool few = tiles <= 512;                         // two to a compute unit
+    note_last_kernel(FP8_FAMILY, FP8_ANY + (few ? 4 : 1));
+    return few ? launch_fp8(s, k_fp8_gemm_any<T, 4>, tiles, 1024, 0, p) : launch_fp8(s, k_fp8_gemm_any<T, 1>, tiles, 256, 0, p);
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------
@@ -168,7 +166,7 @@ static const Fp8Form FORMS_32[] = {
     {64, 64, 4, 1, 1.74f, 0.81f, 2.38f, 1.051f, 0.252f},   {128, 128, 2, 1, 2.43f, 0.00f, 5.55f, 1.261f, 0.514f}};
 
 template <typename T>
-static nq_status launch_gemm(const Fp8GemmParams &p, hipStream_t s)
+static nq_status launch_gemm(const Fp8GemmParams &p, const Fp8Launch &s)
 {
     constexpr bool F32 = sizeof(T) == 4;
     const Fp8Form *forms = F32 ? FORMS_32 : FORMS_16;
@@ -182,6 +180,7 @@ static nq_status launch_gemm(const Fp8GemmParams &p, hipStream_t s)
             best = i;
         }
     }
+    note_last_kernel(FP8_FAMILY, best);
     switch (best) {
     case 0: return launch_tile<T, 16, 16, 16, 16, 4, 2, 1, false>(p, s);
     case 1: return launch_tile<T, 16, 16, 16, 16, 8, F32 ? 2 : 3, 2, false>(p, s);
@@ -240,6 +239,9 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
     const bool tiled = p.KB > 0 && aligned16(x->d_q) && aligned16(w->d_q) && x->ld % 16 == 0 && w->ld % 16 == 0 && span < (int64_t(1) << 30);
     p.sx_span = tiled ? (int)span : 0;
     // A dispatch has fewer than 2^32 threads: at most 2^22 tiles of 16 x 16, of up to 512 threads, go to one; whole tiles of every form.
+    Fp8Launch at{(hipStream_t)stream, nullptr, nullptr};
+    void *start, *stop;                                    // (of the first and of the last launch)
+    take_profile_events(&start, &stop);
     for (int64_t n = 0; n < w->rows; n += FP8_N_STEP) {
         p.N = (int)std::min(FP8_N_STEP, w->rows - n);
         p.w = w->d_q ? w->d_q + n * w->ld : nullptr;
@@ -251,12 +253,14 @@ extern "C" nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *
             p.x = x->d_q ? x->d_q + m * x->ld : nullptr;
             p.sx = x->d_scale ? x->d_scale + m * x->scale_row_step : nullptr;
             p.y = static_cast<uint8_t *>(d_y) + (m * ldy + n) * es;
+            at.start = n == 0 && m == 0 ? start : nullptr;
+            at.stop = n + p.N == w->rows && m + p.M == x->rows ? stop : nullptr;
             if (dtype == NQ_DT_F32)
-                st = tiled ? launch_gemm<float>(p, (hipStream_t)stream) : launch_any<float>(p, (hipStream_t)stream);
+                st = tiled ? launch_gemm<float>(p, at) : launch_any<float>(p, at);
             else if (dtype == NQ_DT_F16)
-                st = tiled ? launch_gemm<_Float16>(p, (hipStream_t)stream) : launch_any<_Float16>(p, (hipStream_t)stream);
+                st = tiled ? launch_gemm<_Float16>(p, at) : launch_any<_Float16>(p, at);
             else
-                st = tiled ? launch_gemm<bf16_t>(p, (hipStream_t)stream) : launch_any<bf16_t>(p, (hipStream_t)stream);
+                st = tiled ? launch_gemm<bf16_t>(p, at) : launch_any<bf16_t>(p, at);
             if (st != NQ_OK) return st;
         }
     }

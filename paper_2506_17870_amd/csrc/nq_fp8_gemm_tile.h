@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(64 * G * (BN / WN) * (BM / WM), OCC) k_fp8_gem
 }
 
 template <typename T, int BN, int BM, int WN, int WM, int G, int STAGES, int OCC, bool AHEAD>
-static nq_status launch_tile(const Fp8GemmParams &p, hipStream_t s)
+static nq_status launch_tile(const Fp8GemmParams &p, const Fp8Launch &s)
 {
     constexpr int GROUP = (BN / WN) * (BM / WM);
     constexpr int ring = STAGES * G * ((BN + BM) * 128 + (BM < 64 ? 64 : BM) * 4);
@@ -327,8 +327,7 @@ static nq_status launch_tile(const Fp8GemmParams &p, hipStream_t s)
         const nq_status st = grant_lds(k, lds, granted);
         if (st != NQ_OK) return st;
     }
-    k<<<(unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN)), 64 * G * GROUP, lds, s>>>(p);
-    return launch_status();
+    return launch_fp8(s, k, ceil_div(p.M, BM) * ceil_div(p.N, BN), 64 * G * GROUP, lds, p);
 }
 
 }  // namespace nq

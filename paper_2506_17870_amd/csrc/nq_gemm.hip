@@ -916,6 +916,21 @@ extern "C" nq_status nq_set_tuning(int key, int value)
     return NQ_OK;
 }
 
+// For the product of fp8 matrices, whose unit is another (nq_fp8_gemm.h).
+namespace nq {
+void take_profile_events(void **start, void **stop)
+{
+    *start = g_ev_start;
+    *stop = g_ev_stop;
+    g_ev_start = g_ev_stop = nullptr;
+}
+void note_last_kernel(int family, int variant)
+{
+    g_last_family = family;
+    g_last_variant = variant;
+}
+}  // namespace nq
+
 extern "C" nq_status nq_profile_last_kernel(int *family, int *variant)
 {
     if (family) *family = g_last_family;

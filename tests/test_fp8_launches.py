@@ -24,7 +24,7 @@ def in_process(stub, part):
     assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
 
 
-@pytest.mark.parametrize("part", ["quantise_sizes", "product_sizes", "grants"])
+@pytest.mark.parametrize("part", ["quantise_sizes", "product_sizes", "grants", "profile", "forms"])
 def test_launches(stub, part):
     in_process(stub, part)
 
@@ -112,6 +112,38 @@ def grants(nq, stub):
     norm(9000)                                   # (a smaller row changes nothing for a longer one)
     norm()
     assert stub.v["grant_calls"].value == calls and len(stub.take()) == 2
+
+
+def profile(nq, stub):
+    """The events of nq_profile_next_launch are taken by the next product, start by its first launch and stop by its last, once."""
+    for M, N, ld in ((8, 300, None), (8, 300, 301), (1, 3 << 20, None)):
+        nq.nq_profile_next_launch(0x111, 0x222)
+        args = fp8(nq, M, 256, 1, ld), fp8(nq, N, 256, 128, ld), None, A, nq.NQ_DT_BF16, N
+        nq.nq_gemm_fp8(*args, stream=0)
+        n = stub.v["count"].value
+        assert [x.start for x in stub.launches[:n]] == [0x111] + [0] * (n - 1) and [x.stop for x in stub.launches[:n]] == [0] * (n - 1) + [0x222]
+        stub.take()
+        nq.nq_gemm_fp8(*args, stream=0)
+        n = stub.v["count"].value
+        assert not any(x.start or x.stop for x in stub.launches[:n])
+        stub.take()
+
+
+def forms(nq, stub):
+    """Which form the library runs: the sizes that the GPU tests have for each."""
+    from fp8_forms import ANY_BYTE, FORMS
+    call = lambda M, N, K, dt, ld=None: nq.nq_gemm_fp8(fp8(nq, M, K, 1, ld), fp8(nq, N, K, 128, ld), None, A, dt, N, stream=0)  # noqa: E731
+    for dt, name, count in ((nq.NQ_DT_F32, "f32", 8), (nq.NQ_DT_F16, "16 bits", 12), (nq.NQ_DT_BF16, "16 bits", 12)):
+        assert sorted(FORMS[name]) == list(range(count))
+        for form, sizes in FORMS[name].items():
+            for size in sizes:
+                call(*size, dt)
+                assert nq.nq_profile_last_kernel() == (12, form), (name, size)
+        for variant, sizes in ANY_BYTE.items():
+            for M, N, K in sizes:
+                call(M, N, K, dt, K if K % 16 else K + 1)
+                assert nq.nq_profile_last_kernel() == (12, variant), (name, M, N, K)
+    assert len({k for k, *_ in stub.take()}) == 8 + 12 + 12 + 3 * 2
 
 
 if __name__ == "__main__":
