@@ -63,7 +63,7 @@ def allowed(act, v, f):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
-@pytest.mark.parametrize("act", ["silu"])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
 def test_one_value_to_a_block(nq, act, dtype):
     t = values(dtype)
     q, scale = torch.zeros(t.numel(), 1, dtype=torch.uint8, device="cuda"), torch.zeros(t.numel(), 1, device="cuda")
@@ -81,7 +81,7 @@ def test_one_value_to_a_block(nq, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
-@pytest.mark.parametrize("act", ["silu"])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_blocks_of_negative_values(nq, act, dtype, block_rows):
     """Blocks whose every value is in the tail: the largest is the block's scale, the others its codes."""
