@@ -15,11 +15,8 @@ struct QuantParams {
     Divider by_blocks;                     // column blocks of a row
 };
 
-// Exponentials and quotients are the hardware's base-2 exponential and reciprocal: an error of some parts in 2^23 of the result, far below
-// a code's step, of which it moves one in a million to the other side.
-// GELU: the tail of the normal distribution, exp(-z^2 / 2) times a polynomial of 1 / (1 + 0.3 z) with the least largest relative error
-// (1.5e-7 over 0 <= z <= 14; fitted here), so that nothing cancels for negative v.  The library's erf takes three times the
-// instructions and bound the kernel (1009 x 5003 f16 8.0 us); an absolute error like 1.5e-7 moves thirty codes in a million.
+// Exponentials and quotients are the hardware's base-2 exponential and reciprocal, each good to a unit.  What the steps make of that is said
+// at each function, in parts of its result; a code's step is 2^-4 of its value at the least, so one in a million or two moves.
 template <int ACT>
 __device__ __forceinline__ float activate(float v)
 {
@@ -35,6 +32,11 @@ __device__ __forceinline__ float activate(float v)
         const float r = v * __builtin_amdgcn_rcpf(1.0f + w);
         return r * (v < 0.0f ? w : 1.0f);
     }
+    // The tail of the normal distribution is exp(-v^2 / 2) times a polynomial of 1 / (1 + 0.3 |v|) with the least largest relative error
+    // (1.5e-7 over 0 <= |v| <= 14; fitted here), so that nothing cancels for negative v.  Off by 8 parts in 2^23 for positive v, by 8 + 0.6 v^2
+    // for negative (the exponent is rounded to fp32 twice: 23 parts at -5, 100 at -12); the textbook form v (1 + erf) / 2 in fp32
+    // loses everything below -5.  Results below 2^-126 come out as 0.  The library's erf takes three times the instructions and bound
+    // the kernel (1009 x 5003 f16 8.0 us).
     if constexpr (ACT == NQ_ACT_GELU) {
         const float z = fabsf(v), t = __builtin_amdgcn_rcpf(fmaf(0.3f, z, 1.0f));
         float q = fmaf(t, 0.035674829f, -0.157203302f);

@@ -63,7 +63,7 @@ def allowed(act, v, f):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
-@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 def test_one_value_to_a_block(nq, act, dtype):
     t = values(dtype)
     q, scale = torch.zeros(t.numel(), 1, dtype=torch.uint8, device="cuda"), torch.zeros(t.numel(), 1, device="cuda")
@@ -81,7 +81,7 @@ def test_one_value_to_a_block(nq, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
-@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_blocks_of_negative_values(nq, act, dtype, block_rows):
     """Blocks whose every value is in the tail: the largest is the block's scale, the others its codes."""
@@ -101,3 +101,15 @@ def test_blocks_of_negative_values(nq, act, dtype, block_rows):
     assert (np.abs(s * 448 - largest) <= off_largest + U * largest).all()
     half = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(f) / s * (1 + 2.0 ** -10), 2.0 ** -6))) - 4)
     assert (np.abs(c * s - f) <= s * half * (1 + 2.0 ** -10) + off + 4 * U * np.abs(f)).all()
+
+
+@pytest.mark.parametrize("act", ["SILU", "GELU", "GELU_TANH"])
+def test_not_finite(nq, act):
+    """An infinite or missing input leaves a scale that is not finite, whatever its sign; its neighbours' blocks do not see it."""
+    x = torch.ones(8, 1)
+    x[:6, 0] = torch.tensor([float("inf"), 1.0, float("-inf"), 2.0, float("nan"), -3.0])
+    for dtype, dt in ((torch.float32, nq.NQ_DT_F32), (torch.float16, nq.NQ_DT_F16), (torch.bfloat16, nq.NQ_DT_BF16)):
+        m = nq.Fp8Matrix(8, 1)
+        nq.nq_quantize_fp8(x.to(dtype).cuda(), dt, 1, None, 0, getattr(nq, "NQ_ACT_" + act), m.desc)
+        finite = torch.isfinite(m.scale[0]).tolist()
+        assert finite == [False, True, False, True, False, True, True, True] and m.scale[0, 0] == float("inf") and torch.isnan(m.scale[0, 4])
