@@ -433,7 +433,10 @@ nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, const void *d
  * Y = bias.
  * fp32 outputs are as exact as fp32 sums are.  16-bit outputs are made by the fp8 matrix instructions, which cut a
  * product off about 14 bits below the largest one added with it: 1.4e-5 of the result (2-norm) on codes of
- * normally distributed values, against 2e-4 (f16) and 1.7e-3 (bf16) that rounding the outputs costs. */
+ * normally distributed values, against 2e-4 (f16) and 1.7e-3 (bf16) that rounding the outputs costs.  An output whose
+ * terms cancel can so be off by more than its own rounding: by 2^-14 of its block's largest product for each
+ * of the block's products, at most (f16 outputs under 1 % of the others' size: by 1.5e-5 of that size, where rounding
+ * costs 1.2e-6).  Where that matters, ask for fp32 outputs, at half the rate, and round those. */
 nq_status nq_gemm_fp8(const nq_fp8 *x, const nq_fp8 *w, const float *d_bias, void *d_y, int dtype, int64_t ldy,
                       void *stream);
 
