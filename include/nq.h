@@ -429,8 +429,9 @@ nq_status nq_quantize_fp8(const void *d_x, int dtype, int64_t ldx, const void *d
  * sums in fp32, rounded to `dtype` once.  x: block_rows 1; w: block_rows 128 (NQ_ERR_UNSUPPORTED otherwise);
  * x->cols == w->cols <= NQ_MAX_K, w->rows <= 2^30 (NQ_ERR_SHAPE).  d_bias: device fp32[w->rows] or NULL.
  * d_y: device [x->rows][w->rows] of `dtype`, rows ldy elements apart, aligned to its type.  Each output is
- * summed in an order that the matrices' sizes and alignment alone fix, so equal calls give equal bits.  No columns:
- * Y = bias.
+ * summed in an order that the matrices' sizes, their alignment and the steps of their rows and scales fix, so equal
+ * calls give equal bits.  The two scales of a block are multiplied first, in fp32 (so their product has to lie
+ * between 2^-126 and 2^128).  No columns: Y = bias.
  * fp32 outputs are as exact as fp32 sums are.  16-bit outputs are made by the fp8 matrix instructions, which cut a
  * product off about 14 bits below the largest one added with it: 1.4e-5 of the result (2-norm) on codes of
  * normally distributed values, against 2e-4 (f16) and 1.7e-3 (bf16) that rounding the outputs costs.  An output whose

@@ -143,6 +143,10 @@ def forms(nq, stub):
             for M, N, K in sizes:
                 call(M, N, K, dt, K if K % 16 else K + 1)
                 assert nq.nq_profile_last_kernel() == (12, variant), (name, M, N, K)
+    for step, family in ((1 << 27, lambda v: v < 100), (1 << 28, lambda v: v >= 100)):      # scales too far apart for the tiles: another order
+        x = nq.nq_fp8(A, 8, 256, 256, A, 1, step, 1, 0)
+        nq.nq_gemm_fp8(x, fp8(nq, 300, 256, 128), None, A, nq.NQ_DT_F32, 300, stream=0)
+        assert family(nq.nq_profile_last_kernel()[1])
     assert len({k for k, *_ in stub.take()}) == 8 + 12 + 12 + 3 * 2
 
 
