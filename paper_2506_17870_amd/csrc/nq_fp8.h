@@ -18,10 +18,6 @@ struct bf16_t {
     uint16_t bits;
 };
 
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(_Float16 v) { return (float)v; }
-__device__ __forceinline__ float to_float(bf16_t v) { return __builtin_bit_cast(float, (uint32_t)v.bits << 16); }
-
 // fp32 -> the type, rounded to nearest even (bf16 by the conversion instruction, two at a time)
 typedef __bf16 f8_b2 __attribute__((ext_vector_type(2)));
 typedef float f8_f2 __attribute__((ext_vector_type(2)));
@@ -248,7 +244,6 @@ inline nq_status check_matrix(const void *p, int dtype, int64_t cols, int64_t ld
     if (ld < cols || ld > (int64_t(1) << 32)) return NQ_ERR_SHAPE;
     return aligned_to(p, dtype_bytes(dtype)) ? NQ_OK : NQ_ERR_ALIGN;
 }
-inline bool rows_on_16(const void *p, int dtype, int64_t ld) { return !p || (aligned16(p) && ld * dtype_bytes(dtype) % 16 == 0); }
 
 // Grants a kernel `bytes` of dynamic LDS, more than the 64 KB that every kernel has: once on each device, whose copy of the kernel
 // it is that has the limit (`devices`: those done, a static of the caller's for each kernel).  A refusal is reported, and the next call asks
