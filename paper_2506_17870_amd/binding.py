@@ -216,6 +216,11 @@ def _stream(s):
     return s.cuda_stream
 
 
+def current_raw_stream(device: int) -> int:
+    """The current stream's handle."""
+    return _current_raw_stream(device)
+
+
 def torch_stream(s, device=None) -> torch.cuda.Stream:
     """The stream that a call's `stream` argument names, as torch's object: None (the current one), a raw handle or a stream."""
     if s is None:

@@ -84,6 +84,14 @@ class Fp8Mlp:
             finally:
                 self._after = {now.cuda_stream: (now, now.record_event() if isinstance(stream, int) else None)}
 
+    def _settled(self, stream):
+        """Whether the pass goes where the last one went, with nothing left to order: the usual case, in a microsecond instead of four."""
+        if stream is not None or len(self._after) != 1:
+            return False
+        handle = nq.current_raw_stream(self._device.index)
+        return (self._after.get(handle, (None, True))[1] is None and handle in self._recorded
+                and not torch.cuda.is_current_stream_capturing())
+
     def allocate(self, tokens: int):
         """Buffers and descriptors for `tokens` tokens, made on the current stream."""
         if tokens in self._captured:
@@ -126,6 +134,9 @@ class Fp8Mlp:
         if self.tokens != h.shape[0]:
             with torch.cuda.stream(nq.torch_stream(stream, self._device)):
                 self.allocate(h.shape[0])
+        if self._settled(stream):
+            self.h.copy_(h)
+            return self._pass(None)
         with self._on(stream) as now:
             self.h.copy_(h)
             if stream is not None and not isinstance(stream, int):
@@ -134,6 +145,8 @@ class Fp8Mlp:
 
     def run(self, stream=None):
         """The same on the stream that lies in self.h already."""
+        if self._settled(stream):
+            return self._pass(None)
         with self._on(stream):
             return self._pass(stream)
 
