@@ -132,3 +132,10 @@ def test_a_graph_keeps_its_buffers(nq):
         assert torch.equal(h12, eager.forward(stream_of(12, seed=100 + i))), i
         assert all(bool((t == 9).all()) for t in others), i
     assert mlp.allocate(12).h is h12 and mlp.tokens == 12
+
+
+def test_no_tokens(nq):
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    mlp = Fp8Mlp(mlp_layers())
+    want = mlp.forward(stream_of(3)).clone()
+    assert mlp.forward(stream_of(0)).shape == (0, 256) and torch.equal(mlp.forward(stream_of(3)), want)
