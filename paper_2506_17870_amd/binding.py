@@ -574,15 +574,19 @@ class Fp8Matrix:
     @classmethod
     def from_float(cls, d_w, block_rows=128, stream=None):
         """nq_quantize_fp8 of [rows][cols] floats (weights; block_rows=1: activations).  With a stream, it waits for the current
-        one, which has made the memory and fills it, and what it reads and writes is not given away before it is done."""
+        one, which has made the memory and fills it, and what it reads and writes is not given away before it is done (by a raw
+        handle, which need not outlive its work, torch cannot tell: there the current stream waits for it in turn)."""
         dtype = {torch.float32: NQ_DT_F32, torch.float16: NQ_DT_F16, torch.bfloat16: NQ_DT_BF16}[d_w.dtype]
         self = cls(d_w.shape[0], d_w.shape[1], block_rows, d_w.device)
         if stream is not None:
-            stream = torch_stream(stream, d_w.device)
-            stream.wait_stream(torch.cuda.current_stream(d_w.device))
-            for t in (self.q, self.scale, d_w):
-                t.record_stream(stream)
+            on, current = torch_stream(stream, d_w.device), torch.cuda.current_stream(d_w.device)
+            on.wait_stream(current)
         nq_quantize_fp8(d_w, dtype, d_w.stride(0) if d_w.shape[0] > 1 else d_w.shape[1], None, 0, NQ_ACT_NONE, self.desc, stream)
+        if isinstance(stream, int):
+            current.wait_stream(on)
+        elif stream is not None:
+            for t in (self.q, self.scale, d_w):
+                t.record_stream(on)
         return self
 
 

@@ -27,7 +27,8 @@ class Fp8Mlp:
 
     A pass runs on the stream it is given, else on the current one, where its input has to be ready.  It comes after all that this object
     has on other streams (the weights' quantiser, the buffers' fills, the last pass), and what it uses is not given away before
-    that stream is done.  Of a stream given as a raw handle torch cannot know that once the object is gone: keep it until then.
+    that stream is done.  Of a stream given as a raw handle, which need not outlive its work, torch cannot know that once the object or
+    the input is gone: keep both until then.
 
     A graph captured from run() or forward() holds this object's addresses: it needs the object as long as it is replayed.  The buffers of
     a token count that was captured stay as they are, and allocate() or forward() with that count come back to them."""
@@ -131,8 +132,8 @@ class Fp8Mlp:
         (a buffer of this object: the next forward overwrites it)."""
         if h.dim() != 2 or h.shape[1] != self.layers[0]["D"]:
             raise ValueError(f"the stream must be [tokens][{self.layers[0]['D']}], got {tuple(h.shape)}")
-        if self.tokens != h.shape[0]:
-            with torch.cuda.stream(nq.torch_stream(stream, self._device)):
+        if self.tokens != h.shape[0]:                     # (memory belongs to streams that torch knows)
+            with torch.cuda.stream(None if isinstance(stream, int) else stream):
                 self.allocate(h.shape[0])
         if self._settled(stream):
             self.h.copy_(h)

@@ -43,14 +43,15 @@ def test_fills_come_before_the_codes(nq, busy, raw, block_rows):
     assert same(got, want) and want.q.any()
 
 
-def test_floats_are_kept_until_they_are_read(nq, busy):
+@pytest.mark.parametrize("raw", [False, True])
+def test_floats_are_kept_until_they_are_read(nq, busy, raw):
     w = torch.randn(1024, 1024, device="cuda")
     want = nq.Fp8Matrix.from_float(w)
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
     busy(side)
-    got = nq.Fp8Matrix.from_float(w.clone(), stream=side)
-    others = [torch.full_like(w, 7.0) for _ in range(4)]         # (on the current stream, which does not wait)
+    got = nq.Fp8Matrix.from_float(w.clone(), stream=side.cuda_stream if raw else side)
+    others = [torch.full_like(w, 7.0) for _ in range(4)]
     torch.cuda.synchronize()
     assert same(got, want) and len(others) == 4
 
@@ -139,3 +140,14 @@ def test_no_tokens(nq):
     mlp = Fp8Mlp(mlp_layers())
     want = mlp.forward(stream_of(3)).clone()
     assert mlp.forward(stream_of(0)).shape == (0, 256) and torch.equal(mlp.forward(stream_of(3)), want)
+
+
+def test_memory_of_a_pass_by_handle_is_the_current_streams(nq):
+    """A handle may be destroyed after its work: nothing that outlives a pass on one is asked for or kept under it."""
+    from paper_2506_17870_amd.fp8_mlp import Fp8Mlp
+    mlp, side = Fp8Mlp(mlp_layers()), torch.cuda.Stream()
+    for tokens in (5, 9):
+        mlp.forward(stream_of(tokens), side.cuda_stream)
+        torch.cuda.synchronize()
+        assert mlp._home.cuda_stream == torch.cuda.current_stream().cuda_stream and side.cuda_stream not in mlp._recorded
+        assert all(event is not None for handle, (_, event) in mlp._after.items() if handle == side.cuda_stream)
