@@ -476,6 +476,111 @@ typedef struct {
 } nq_norm_job;
 nq_status nq_block_norm(const nq_norm_job *job, int64_t M, int64_t D, void *stream);
 
+/* ---- attention of a transformer (beyond the paper) -------------------------------------------------------- *
+ * What stands between the projections of a transformer's attention: the heads' norms and rotation with the keys and
+ * values on their way into a cache, rows of that cache back, attention over whole prompts, and over the cache for one
+ * new token of each sequence.  A token's heads lie beside each other, head h of a row at element h * head_dim, rows an
+ * `ld` apart.  head_dim: a multiple of 8 up to NQ_HEAD_MAX_DIM (NQ_ERR_SHAPE).  Query head h reads the keys and
+ * values of head h / (q_heads / kv_heads); kv_heads has to divide q_heads.  Arrays of int32_t and int64_t are device
+ * memory that is read when the call runs, so that a captured call sees what they hold at each replay. */
+#define NQ_HEAD_MAX_DIM 256
+#define NQ_MAX_HEADS 1024
+
+/* A cache of keys and values: pages of page_tokens tokens, heads heads of head_dim to a token.  Element d of head h
+ * of the token at place i of page p is d_k[p * page_step + i * token_step + h * head_step + d] (d_v likewise), of type
+ * f16, bf16 or e4m3 codes.  e4m3: each head of a token has a scale,
+ * d_k_scale[p * scale_page_step + i * scale_token_step + h * scale_head_step], that stands for scale * code; made as
+ * nq_quantize_fp8 makes the scale of a block, over the head's head_dim values.  For floats the scales are NULL.
+ * A token's slot is p * page_tokens + i.  Steps are not negative; any alignment to the type is right, rows
+ * on 16 bytes are fast. */
+typedef enum { NQ_KV_F16 = 1, NQ_KV_BF16 = 2, NQ_KV_E4M3 = 3 } nq_kv_type;
+typedef struct {
+    void *d_k, *d_v;
+    float *d_k_scale, *d_v_scale;
+    int64_t pages;                                          /* 0 .. 2^31 - 1               */
+    int64_t page_step, token_step, head_step;               /* in elements; the last two to 2^26, the first to 2^40 */
+    int64_t scale_page_step, scale_token_step, scale_head_step; /* in floats, likewise      */
+    int32_t type;                                           /* nq_kv_type                  */
+    int32_t page_tokens;                                    /* 1 .. 2^20                   */
+    int32_t heads, head_dim;
+} nq_kv_cache;
+
+/* q' = rotate(norm(q)), k' = rotate(norm(k)) for each head of each of T rows; k' and v into the cache.  All of it in fp32,
+ * each result rounded once.  norm: over the head_dim values of a head as in nq_block_norm, d_weight and d_bias fp32[head_dim].
+ * rotate: for the pairs (a, b) of the first `rotary` columns, at the angle t = position * freq[i] of the pair i < rotary / 2,
+ *   (a cos t - b sin t, b cos t + a sin t);  NQ_PAIRS_HALVES: columns i and i + rotary / 2;  NQ_PAIRS_NEIGHBOURS: 2 i and 2 i + 1.
+ * The angle's whole turns are taken off in 64 bits, so that far positions keep theirs.  rotary: even, 0 .. head_dim; 0: none,
+ * d_freq and d_position may be NULL.
+ * d_q, d_k, d_v [T][heads][head_dim] of dtype, each may be NULL (no such heads).  Out: d_q_out (d_q's, needed with it), d_k_out
+ * (k' as floats, may be NULL) of dtype; each may be its input, with the same ld.  cache and d_slot may both be NULL; else d_k
+ * and d_v go to the cache, row t to the slot d_slot[t].  A row whose slot is negative or not in the cache goes nowhere.  No two rows of a
+ * call may have the same slot (what such a slot then holds is a mixture).  f16 caches take values up to 65504, larger ones become
+ * infinite.  T == 0: no-op. */
+typedef enum { NQ_PAIRS_HALVES = 0, NQ_PAIRS_NEIGHBOURS = 1 } nq_pairs;
+typedef struct {
+    const void *d_q, *d_k, *d_v;
+    int64_t ldq, ldk, ldv;
+    int32_t dtype, q_heads, kv_heads, head_dim;
+    nq_norm q_norm, k_norm;
+    const float *d_freq;             /* fp32[rotary / 2], radians a position */
+    const int32_t *d_position;       /* [T] */
+    int32_t rotary, pairs;
+    void *d_q_out, *d_k_out;
+    int64_t ldq_out, ldk_out;
+    const nq_kv_cache *cache;        /* host: read before the call returns */
+    const int64_t *d_slot;           /* [T] */
+} nq_head_job;
+nq_status nq_head_norm(const nq_head_job *job, int64_t T, void *stream);
+
+/* Row t of d_k and d_v [T][cache->heads][head_dim] of dtype = the cache's token at d_slot[t] (scale * code in fp32, rounded
+ * once); zeros where the slot is negative or not in the cache.  d_k or d_v may be NULL.  T == 0: no-op. */
+nq_status nq_cache_read(const nq_kv_cache *cache, const int64_t *d_slot, int64_t T, void *d_k, int64_t ldk, void *d_v,
+                        int64_t ldv, int dtype, void *stream);
+
+/* o[i] = sum_j p_j v[j], p = softmax over j of scale * (q[i] . k[j]), for the rows i and keys j of each sequence s: rows
+ * d_q_begin[s] .. d_q_begin[s + 1] of q and o, d_k_begin[s] .. d_k_begin[s + 1] of k and v (d_k_begin NULL: the same).
+ * causal: row i of Lq sees the keys j <= i + (Lk - Lq), so that a sequence's last row sees all of them (keys ahead of the
+ * queries': a cached prefix).  A row that sees no key is 0.  Rows of q that belong to no sequence are left as they were.
+ * d_q, d_o [q_rows][q_heads][head_dim], d_k, d_v [k_rows][kv_heads][head_dim] of dtype, f16 or bf16 (fp32: NQ_ERR_UNSUPPORTED).
+ * Sums and softmax in fp32, the probabilities (relative to a row's largest) rounded to dtype for the second product,
+ * outputs rounded once.  The order of the sums depends on the sizes alone, so equal calls give equal bits.
+ * Begins are not to fall and to end within the rows; ones that do not are cut off there.  d_o must not overlap the inputs. */
+typedef struct {
+    const void *d_q, *d_k, *d_v;
+    void *d_o;
+    int64_t ldq, ldk, ldv, ldo;
+    const int32_t *d_q_begin, *d_k_begin;    /* [sequences + 1] */
+    int64_t sequences, q_rows, k_rows;
+    int32_t dtype, q_heads, kv_heads, head_dim, causal;
+    float scale;
+} nq_prompt_job;
+nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream);
+
+/* The same for one row of each sequence, over the cache: row s of d_q and d_o [sequences][q_heads][head_dim] sees the first
+ * d_length[s] tokens of the pages d_table[s * ldtable ..].  No tokens: 0.  A length counts up to max_length (which sizes the launch and
+ * the workspace: the nearer to the longest, the better), tokens of a page that the cache does not have (-1, say) are left out; ldtable *
+ * page_tokens >= max_length.  dtype: f16 or bf16; the cache e4m3 or of the same type (NQ_ERR_UNSUPPORTED).
+ * Sums, softmax and probabilities as exact as fp32 makes them.  A sequence's tokens are split over workgroups whose results the
+ * workspace holds until they are joined; how depends on all lengths of the call.  d_workspace: 16-byte aligned, of
+ * nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length) or more (0: NULL will do); its
+ * contents count only while the call runs, so calls that may run at the same time (on two streams, in two graphs) need one each. */
+typedef struct {
+    const void *d_q;
+    void *d_o;
+    int64_t ldq, ldo;
+    const nq_kv_cache *cache;        /* host: read before the call returns */
+    const int32_t *d_table;          /* [sequences][ldtable] */
+    const int32_t *d_length;         /* [sequences] */
+    int64_t ldtable, sequences, max_length;
+    int32_t dtype, q_heads;
+    float scale;
+    int32_t reserved_;
+    void *d_workspace;
+    uint64_t workspace_bytes;
+} nq_token_job;
+size_t nq_attention_token_workspace_bytes(int64_t sequences, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_length);
+nq_status nq_attention_token(const nq_token_job *job, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

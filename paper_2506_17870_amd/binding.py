@@ -31,6 +31,9 @@ NQ_DT_F32, NQ_DT_F16, NQ_DT_BF16 = 0, 1, 2
 NQ_ACT_NONE, NQ_ACT_RELU, NQ_ACT_SILU, NQ_ACT_GELU, NQ_ACT_GELU_TANH = range(5)
 NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER = range(3)
 NQ_NORM_MAX_D = 32768
+NQ_KV_F16, NQ_KV_BF16, NQ_KV_E4M3 = 1, 2, 3
+NQ_PAIRS_HALVES, NQ_PAIRS_NEIGHBOURS = 0, 1
+NQ_HEAD_MAX_DIM, NQ_MAX_HEADS = 256, 1024
 
 EXPORTS = ["nq_version", "nq_status_string", "nq_packed_bytes", "nq_quantize", "nq_tensor_scale", "nq_quantize_tensor", "nq_quantize_decompose_pack",
            "nq_decompose", "nq_pack", "nq_decompose_pack", "nq_decompose_pack_batch",
@@ -38,7 +41,8 @@ EXPORTS = ["nq_version", "nq_status_string", "nq_packed_bytes", "nq_quantize", "
            "nq_weight_init_group", "nq_page_out_low_batch", "nq_page_in_low_batch",
            "nq_gemm_full", "nq_gemm_part", "nq_gemm_batch_workspace_bytes", "nq_gemm_batch", "nq_gemm_batch_static", "nq_conv_full", "nq_conv_part", "nq_gconv_full", "nq_gconv_part",
            "nq_set_tuning", "nq_profile_next_launch", "nq_profile_last_kernel", "nq_event_create", "nq_event_destroy",
-           "nq_event_elapsed_ms", "nq_maxpool_i8", "nq_avgpool_i8", "nq_quantize_fp8", "nq_gemm_fp8", "nq_block_norm"]
+           "nq_event_elapsed_ms", "nq_maxpool_i8", "nq_avgpool_i8", "nq_quantize_fp8", "nq_gemm_fp8", "nq_block_norm",
+           "nq_head_norm", "nq_cache_read", "nq_attention_prompt", "nq_attention_token_workspace_bytes", "nq_attention_token"]
 
 
 class nq_cfg(ctypes.Structure):
@@ -102,6 +106,36 @@ class nq_norm_job(ctypes.Structure):
     _columns, _gate = 1 << 62, None
 
 
+class nq_kv_cache(ctypes.Structure):
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_k_scale", ctypes.c_void_p), ("d_v_scale", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_step", ctypes.c_int64), ("token_step", ctypes.c_int64), ("head_step", ctypes.c_int64),
+                ("scale_page_step", ctypes.c_int64), ("scale_token_step", ctypes.c_int64), ("scale_head_step", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class nq_head_job(ctypes.Structure):
+    _fields_ = [("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64),
+                ("ldv", ctypes.c_int64), ("dtype", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("q_norm", nq_norm), ("k_norm", nq_norm), ("d_freq", ctypes.c_void_p), ("d_position", ctypes.c_void_p),
+                ("rotary", ctypes.c_int32), ("pairs", ctypes.c_int32), ("d_q_out", ctypes.c_void_p), ("d_k_out", ctypes.c_void_p),
+                ("ldq_out", ctypes.c_int64), ("ldk_out", ctypes.c_int64), ("cache", ctypes.POINTER(nq_kv_cache)), ("d_slot", ctypes.c_void_p)]
+    _rows = 1 << 62                      # rows that the job's tensors have (addresses that are not a tensor's: any)
+
+
+class nq_prompt_job(ctypes.Structure):
+    _fields_ = [("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_o", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+                ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64), ("d_q_begin", ctypes.c_void_p), ("d_k_begin", ctypes.c_void_p),
+                ("sequences", ctypes.c_int64), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class nq_token_job(ctypes.Structure):
+    _fields_ = [("d_q", ctypes.c_void_p), ("d_o", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("ldo", ctypes.c_int64), ("cache", ctypes.POINTER(nq_kv_cache)),
+                ("d_table", ctypes.c_void_p), ("d_length", ctypes.c_void_p), ("ldtable", ctypes.c_int64), ("sequences", ctypes.c_int64),
+                ("max_length", ctypes.c_int64), ("dtype", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("reserved_", ctypes.c_int32), ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2506_17870_amd.build` "
                       "(there is no CPU or PyTorch fallback for the HIP path)")
@@ -150,6 +184,11 @@ _SIGS = {
     "nq_quantize_fp8": (_int, [_vp, _int, _i64, _vp, _i64, _int, ctypes.POINTER(nq_fp8), _vp]),
     "nq_gemm_fp8": (_int, [ctypes.POINTER(nq_fp8), ctypes.POINTER(nq_fp8), _vp, _vp, _int, _i64, _vp]),
     "nq_block_norm": (_int, [ctypes.POINTER(nq_norm_job), _i64, _i64, _vp]),
+    "nq_head_norm": (_int, [ctypes.POINTER(nq_head_job), _i64, _vp]),
+    "nq_cache_read": (_int, [ctypes.POINTER(nq_kv_cache), _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
+    "nq_attention_prompt": (_int, [ctypes.POINTER(nq_prompt_job), _vp]),
+    "nq_attention_token_workspace_bytes": (ctypes.c_size_t, [_i64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _i64]),
+    "nq_attention_token": (_int, [ctypes.POINTER(nq_token_job), _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -184,6 +223,9 @@ _fast.setup(torch.Tensor, nq_weight, nq_epilogue, nq_conv_shape, nq_cfg,
                         "nq_quantize_decompose_pack")])
 _fast.setup_fp8(nq_fp8, nq_norm_job, *[ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value
                                        for n in ("nq_quantize_fp8", "nq_gemm_fp8", "nq_block_norm")])
+_fast.setup_attention(nq_kv_cache, nq_head_job, nq_prompt_job, nq_token_job,
+                      *[ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value
+                        for n in ("nq_head_norm", "nq_cache_read", "nq_attention_prompt", "nq_attention_token")])
 # a forked child has to go through torch's own initialisation (and its error) again
 os.register_at_fork(after_in_child=lambda: _fast.set_stream_ready(False))
 
@@ -558,6 +600,169 @@ def nq_block_norm(job: nq_norm_job, M, D, stream=None):
     if st >= 0:
         return _check(st, "nq_block_norm")
     _check(_lib.nq_block_norm(ctypes.byref(job), M, D, _stream(stream)), "nq_block_norm")
+
+
+_KV_TYPES = {torch.float16: NQ_KV_F16, torch.bfloat16: NQ_KV_BF16, torch.float8_e4m3fn: NQ_KV_E4M3, torch.uint8: NQ_KV_E4M3}
+
+
+def make_kv_cache(d_k, d_v, d_k_scale=None, d_v_scale=None) -> nq_kv_cache:
+    """Descriptor of a cache: d_k and d_v [pages][page_tokens][heads][head_dim] of f16, bf16, or e4m3 codes (float8_e4m3fn or uint8), any
+    steps between pages, tokens and heads (views of memory in another order, say), those of d_v as those of d_k; e4m3: d_k_scale and
+    d_v_scale fp32 [pages][page_tokens][heads] likewise.  It keeps all of them alive."""
+    if d_k.dim() != 4 or d_k.dtype not in _KV_TYPES:
+        raise ValueError(f"d_k must be [pages][page_tokens][heads][head_dim] of f16, bf16 or e4m3, got {d_k.dtype} {tuple(d_k.shape)}")
+    if d_v.shape != d_k.shape or d_v.dtype != d_k.dtype or (d_v.numel() and d_v.stride() != d_k.stride()):
+        raise ValueError(f"d_v must be as d_k, got {d_v.dtype} {tuple(d_v.shape)} {d_v.stride()}")
+    if d_k.numel() and d_k.shape[3] > 1 and d_k.stride(3) != 1:
+        raise ValueError("the elements of a head must lie beside each other")
+    codes = _KV_TYPES[d_k.dtype] == NQ_KV_E4M3
+    if codes:
+        for name, t in (("d_k_scale", d_k_scale), ("d_v_scale", d_v_scale)):
+            if t is None or t.dtype != torch.float32 or t.shape != d_k.shape[:3]:
+                raise ValueError(f"{name} must be fp32 {tuple(d_k.shape[:3])}")
+        if d_v_scale.numel() and d_v_scale.stride() != d_k_scale.stride():
+            raise ValueError("d_v_scale must be as d_k_scale")
+    elif d_k_scale is not None or d_v_scale is not None:
+        raise ValueError("a cache of floats has no scales")
+    pages, tokens, heads, dim = d_k.shape
+    steps, scales = d_k.stride()[:3], d_k_scale.stride() if codes else (0, 0, 0)
+    cache = nq_kv_cache(d_k.data_ptr(), d_v.data_ptr(), _ptr_of(d_k_scale), _ptr_of(d_v_scale), pages, *steps, *scales, _KV_TYPES[d_k.dtype],
+                        tokens, heads, dim)
+    cache._keep = (d_k, d_v, d_k_scale, d_v_scale)
+    return cache
+
+
+def _ptr_of(t):
+    return None if t is None else t.data_ptr()
+
+
+def _indices(name, t, dtype, least=0):
+    """Refuses a tensor of indices of another type, or with too few of them."""
+    if isinstance(t, torch.Tensor) and (t.dtype != dtype or t.numel() < least or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous {dtype} of {least} elements or more, got {t.dtype} {tuple(t.shape)}")
+
+
+def _row_count(t, ld, width):
+    """How many rows of `width` elements, `ld` apart, a tensor's memory holds; of an address or None: any number."""
+    if not isinstance(t, torch.Tensor):
+        return 1 << 62
+    there = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    return 0 if there < width else 1 << 62 if ld <= 0 else (there - width) // ld + 1
+
+
+def make_head_norm(d_q, ldq, d_k, ldk, d_v, ldv, dtype, q_heads, kv_heads, head_dim, q_norm: nq_norm, k_norm: nq_norm, d_freq, rotary, pairs,
+                   d_position, d_q_out, ldq_out, d_k_out, ldk_out, cache: nq_kv_cache | None = None, d_slot=None) -> nq_head_job:
+    """Descriptor of nq_head_norm calls; None for what is not there.  It keeps everything it names alive."""
+    wq, wk = q_heads * head_dim, kv_heads * head_dim
+    rows = 1 << 62
+    for name, t, ld, width in (("d_q", d_q, ldq, wq), ("d_k", d_k, ldk, wk), ("d_v", d_v, ldv, wk), ("d_q_out", d_q_out, ldq_out, wq),
+                               ("d_k_out", d_k_out, ldk_out, wk)):
+        _typed(name, t, dtype)
+        rows = min(rows, _row_count(t, ld, width))
+    for n in (q_norm, k_norm):
+        if any(isinstance(t, torch.Tensor) and t.numel() < head_dim for t in getattr(n, "_keep", ())):
+            raise ValueError(f"the norms' vectors need {head_dim} elements")
+    if isinstance(d_freq, torch.Tensor) and (d_freq.dtype != torch.float32 or d_freq.numel() < rotary // 2 or not d_freq.is_contiguous()):
+        raise ValueError(f"d_freq must be contiguous fp32 [{rotary // 2}], got {d_freq.dtype} {tuple(d_freq.shape)}")
+    _indices("d_position", d_position, torch.int32)
+    _indices("d_slot", d_slot, torch.int64)
+    rows = min([rows] + [t.numel() for t in (d_position if rotary else None, d_slot) if isinstance(t, torch.Tensor)])
+    job = nq_head_job(_rows(d_q), _rows(d_k), _rows(d_v), ldq, ldk, ldv, dtype, q_heads, kv_heads, head_dim, q_norm, k_norm, _ptr(d_freq),
+                      _ptr(d_position), rotary, pairs, _rows(d_q_out), _rows(d_k_out), ldq_out, ldk_out,
+                      ctypes.pointer(cache) if cache is not None else None, _ptr(d_slot))
+    job._keep = (d_q, d_k, d_v, q_norm, k_norm, d_freq, d_position, d_q_out, d_k_out, cache, d_slot)
+    job._rows = rows
+    return job
+
+
+def nq_head_norm(job: nq_head_job, T, stream=None):
+    if T > job._rows:
+        raise ValueError(f"the job's tensors have {job._rows} rows, the call is for {T}")
+    st = _fast.head_norm(job, T, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_head_norm")
+    _check(_lib.nq_head_norm(ctypes.byref(job), T, _stream(stream)), "nq_head_norm")
+
+
+def nq_cache_read(cache: nq_kv_cache, d_slot, T, d_k, ldk, d_v, ldv, dtype, stream=None):
+    _indices("d_slot", d_slot, torch.int64, T)
+    for name, t, ld in (("d_k", d_k, ldk), ("d_v", d_v, ldv)):
+        _typed(name, t, dtype)
+        if isinstance(t, torch.Tensor) and T > _row_count(t, ld, cache.heads * cache.head_dim):
+            raise ValueError(f"{name} is too small for {T} rows, {ld} apart")
+    st = _fast.cache_read(cache, d_slot, T, d_k, ldk, d_v, ldv, dtype, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_cache_read")
+    _check(_lib.nq_cache_read(ctypes.byref(cache), _ptr(d_slot), T, _rows(d_k), ldk, _rows(d_v), ldv, dtype, _stream(stream)), "nq_cache_read")
+
+
+def make_attention_prompt(d_q, ldq, d_k, ldk, d_v, ldv, d_o, ldo, d_q_begin, d_k_begin, sequences, q_rows, k_rows, dtype, q_heads, kv_heads,
+                          head_dim, causal, scale) -> nq_prompt_job:
+    """Descriptor of nq_attention_prompt calls; it keeps everything it names alive."""
+    for name, t, ld, heads, rows in (("d_q", d_q, ldq, q_heads, q_rows), ("d_k", d_k, ldk, kv_heads, k_rows), ("d_v", d_v, ldv, kv_heads, k_rows),
+                                     ("d_o", d_o, ldo, q_heads, q_rows)):
+        _typed(name, t, dtype)
+        if rows > _row_count(t, ld, heads * head_dim):
+            raise ValueError(f"{name} is too small for {rows} rows, {ld} apart")
+    _indices("d_q_begin", d_q_begin, torch.int32, sequences + 1)
+    _indices("d_k_begin", d_k_begin, torch.int32, sequences + 1)
+    job = nq_prompt_job(_rows(d_q), _rows(d_k), _rows(d_v), _rows(d_o), ldq, ldk, ldv, ldo, _ptr(d_q_begin), _ptr(d_k_begin), sequences, q_rows,
+                        k_rows, dtype, q_heads, kv_heads, head_dim, int(causal), scale)
+    job._keep = (d_q, d_k, d_v, d_o, d_q_begin, d_k_begin)
+    return job
+
+
+def nq_attention_prompt(job: nq_prompt_job, stream=None):
+    st = _fast.attention_prompt(job, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_attention_prompt")
+    _check(_lib.nq_attention_prompt(ctypes.byref(job), _stream(stream)), "nq_attention_prompt")
+
+
+def nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length) -> int:
+    return int(_lib.nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length))
+
+
+def make_attention_token(d_q, ldq, d_o, ldo, cache: nq_kv_cache, d_table, d_length, sequences, max_length, dtype, q_heads, scale,
+                         d_workspace=None, ldtable=None) -> nq_token_job:
+    """Descriptor of nq_attention_token calls; it keeps everything it names alive.  d_table: int32 [sequences][pages], the numbers of a row
+    beside each other (or an address, with ldtable)."""
+    for name, t, ld in (("d_q", d_q, ldq), ("d_o", d_o, ldo)):
+        _typed(name, t, dtype)
+        if sequences > _row_count(t, ld, q_heads * cache.head_dim):
+            raise ValueError(f"{name} is too small for {sequences} rows, {ld} apart")
+    _indices("d_length", d_length, torch.int32, sequences)
+    if isinstance(d_table, torch.Tensor):
+        if d_table.dtype != torch.int32 or d_table.dim() != 2 or d_table.shape[0] < sequences or (d_table.shape[1] > 1 and d_table.stride(1) != 1):
+            raise ValueError(f"d_table must be int32 [{sequences}][pages], got {d_table.dtype} {tuple(d_table.shape)}")
+        if d_table.shape[1] * cache.page_tokens < max_length:
+            raise ValueError(f"a row of d_table has {d_table.shape[1]} pages of {cache.page_tokens} tokens, max_length is {max_length}")
+        ldtable = d_table.stride(0) if d_table.shape[0] > 1 else d_table.shape[1]
+    job = nq_token_job(_rows(d_q), _rows(d_o), ldq, ldo, ctypes.pointer(cache), _rows(d_table), _ptr(d_length), ldtable or 0, sequences, max_length,
+                       dtype, q_heads, scale, 0, _ptr(d_workspace),
+                       d_workspace.numel() * d_workspace.element_size() if isinstance(d_workspace, torch.Tensor) else 0)
+    job._keep = (d_q, d_o, cache, d_table, d_length, d_workspace)
+    return job
+
+
+def nq_attention_token(job: nq_token_job, stream=None):
+    st = _fast.attention_token(job, stream if stream is None else _stream(stream))
+    if st >= 0:
+        return _check(st, "nq_attention_token")
+    _check(_lib.nq_attention_token(ctypes.byref(job), _stream(stream)), "nq_attention_token")
+
+
+class KvCache:
+    """Owner of the memory of one nq_kv_cache descriptor (memory plumbing only): empty pages, the tokens of a head in a page beside each other,
+    the order in which nq_attention_token reads longest runs.  dtype: float16, bfloat16 or float8_e4m3fn."""
+
+    def __init__(self, pages, page_tokens, heads, head_dim, dtype=torch.float8_e4m3fn, device="cuda"):
+        make = lambda: torch.zeros(pages, heads, page_tokens, head_dim, dtype=dtype, device=device).transpose(1, 2)  # noqa: E731
+        self.k, self.v = make(), make()
+        self.k_scale = self.v_scale = None
+        if dtype == torch.float8_e4m3fn:
+            self.k_scale, self.v_scale = (torch.ones(pages, heads, page_tokens, device=device).transpose(1, 2) for _ in range(2))
+        self.desc = make_kv_cache(self.k, self.v, self.k_scale, self.v_scale)
 
 
 class Fp8Matrix:

@@ -31,7 +31,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 def _units():
     units = [(os.path.join(CSRC, f + ".hip"), os.path.join(OBJ, f + ".o"), [])
-             for f in ("nq_block_norm", "nq_fp8_quant", "nq_fp8_gemm", "nq_pack", "nq_page", "nq_glue",
+             for f in ("nq_attention_prompt", "nq_attention_token", "nq_head_norm", "nq_block_norm", "nq_fp8_quant", "nq_fp8_gemm", "nq_pack", "nq_page", "nq_glue",
                        "nq_gemm")]                                    # nq_yardsticks.hip is a program of its own
     # the longest first (the large kernel's units take twice as long as the next), so that none is left to run alone at the end
     for part in (1, 0, 3, 2):

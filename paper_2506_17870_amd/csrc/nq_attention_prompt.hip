@@ -1,0 +1,385 @@
+// nq_attention_prompt: attention over whole prompts, packed sequences, causal or not, grouped heads.
+//
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(x_ij - m_i),  x_ij = scale log2(e) (q_i . k_j),  m_i the largest x so far
+//
+// Bound by the matrix core, and next to it by the exponentials.  A workgroup takes 128 (or 256) rows of a head, a wave 32 (64) of
+// them, and goes over the keys 64 (32) at a time.  Both products are transposed: S^T = K Q^T, O^T = V^T P^T.  A lane then holds scores of
+// one row only, its maximum and sum need one exchange with another lane, and because the order in which a product sums its keys is
+// free, the scores' places after the first product are the probabilities' places in the second one's operand: they never leave
+// their registers.  K and V tiles go through LDS, V's fragments by the transposing read.
+#include "nq_attention.h"
+
+namespace nq {
+
+typedef __bf16 at_b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 at_h2 __attribute__((ext_vector_type(2)));
+typedef float at_f16 __attribute__((ext_vector_type(16)));
+typedef short at_s4 __attribute__((ext_vector_type(4)));
+
+constexpr float PR_LOG2E = 1.44269504088896340736f;
+// A row's maximum is moved only when a score passes it by this much (in powers of two): the probabilities are relative to it, so
+// any reference will do that keeps them within their type.
+constexpr float PR_SLACK = 8.0f;
+
+struct PromptParams {
+    const void *q, *k, *v;
+    void *o;
+    const int32_t *q_begin, *k_begin;
+    int64_t ldq, ldk, ldv, ldo;
+    int32_t sequences, q_rows, k_rows, Hq, Hkv, group, D, causal, tiles;
+    Divider by_heads;
+    float scale;                                // times log2(e), its magnitude
+    uint32_t flip;                              // sign bits for q where the scale is negative
+    int32_t zero;                               // a scale of 0
+};
+
+template <typename T>
+__device__ __forceinline__ at_f16 mma32(uint4 a, uint4 b, at_f16 c)
+{
+    if constexpr (__is_same(T, _Float16))
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f8_h8, a), __builtin_bit_cast(f8_h8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_b8, a), __builtin_bit_cast(at_b8, b), c, 0, 0, 0);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pair16(float a, float b)
+{
+    if constexpr (__is_same(T, _Float16))
+        return __builtin_bit_cast(uint32_t, at_h2{(_Float16)a, (_Float16)b});
+    else
+        return pack_bf16(a, b);
+}
+template <typename T>
+__device__ __forceinline__ float value16(uint16_t v)
+{
+    if constexpr (__is_same(T, _Float16))
+        return (float)__builtin_bit_cast(_Float16, v);
+    else
+        return __builtin_bit_cast(float, (uint32_t)v << 16);
+}
+__device__ __forceinline__ float across32(float v, bool sum)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t x = r[0], y = r[1];                                   // (a bit cast of a vector's element takes its first)
+    const float a = __builtin_bit_cast(float, x), b = __builtin_bit_cast(float, y);
+    return sum ? a + b : fmaxf(a, b);
+}
+__device__ __forceinline__ uint2 read_transposed(const uint16_t *at)
+{
+    typedef __attribute__((address_space(3))) at_s4 lds_s4;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)at));
+}
+
+// LDS rows of PITCH elements in pieces of 16 bytes, exchanged so that neither the rows that a wave reads at once nor the four rows of a
+// transposing read meet in a bank.
+template <int PITCH>
+__device__ __forceinline__ int k_piece(int row, int piece) { return piece ^ (PITCH == 64 ? (row ^ (row >> 3)) & 7 : row & 15); }
+template <int PITCH>
+__device__ __forceinline__ int v_piece(int row, int piece) { return piece ^ (PITCH == 64 ? (row & 2) << 1 : ((row & 3) << 2) | ((row >> 2) & 3)); }
+
+constexpr int pitch_of(int DP) { return DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
+// keys of a step: as many as the registers hold beside the outputs
+constexpr int keys_of(int DP) { return DP <= 128 ? 64 : 32; }
+
+template <typename T, int DP, int QT>
+__global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt(const PromptParams p)
+{
+    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP), U = KEYS / 32, KJ = DP / 16, DT = DP / 32, CH = KEYS * DP / 8 / 256, PIECES = DP / 8;
+    constexpr int ROWS = 128 * QT, TILE = KEYS * PITCH;
+    constexpr bool F16 = __is_same(T, _Float16);
+    constexpr uint32_t EXP = F16 ? 0x7c00 : 0x7f80;                      // the exponent of infinities and NaN
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];     // two stages of K and V
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, half = lane >> 5;
+
+    // ---- which rows: tile t belongs to the last sequence s with begin / ROWS + s <= t
+    const uint32_t order = divide(blockIdx.x, p.by_heads), h = blockIdx.x - order * p.by_heads.d;
+    const int t = p.tiles - 1 - (int)order;                              // (the rows with the most keys first)
+    int lo = -1, hi = p.sequences;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((int64_t)(p.q_begin[mid] / ROWS) + mid <= t) lo = mid; else hi = mid;
+    }
+    if (lo < 0) return;
+    const int first = t - (p.q_begin[lo] / ROWS + lo);
+    const int q0 = min(max(p.q_begin[lo], 0), p.q_rows), q1 = min(max(p.q_begin[lo + 1], q0), p.q_rows), Lq = q1 - q0;
+    const int k0 = min(max(p.k_begin[lo], 0), p.k_rows), k1 = min(max(p.k_begin[lo + 1], k0), p.k_rows), Lk = k1 - k0;
+    if (first < 0 || (int64_t)first * ROWS >= Lq) return;
+    const int row0 = first * ROWS, off = p.causal ? Lk - Lq : Lk;        // row i sees the keys j <= i + off (without causal: all)
+    const int end = min(Lk, max(0, min(row0 + ROWS, Lq) + off));         // keys that any row sees
+    const int hk = (int)h / p.group;
+
+    uint4 q[QT][KJ];
+#pragma unroll
+    for (int a = 0; a < QT; ++a) {
+        const int row = row0 + (wave * QT + a) * 32 + r;
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) {
+            const int d = 16 * j + 8 * half;
+            q[a][j] = make_uint4(0, 0, 0, 0);
+            if (row < Lq && d < p.D && !p.zero) {
+                __builtin_memcpy(&q[a][j], static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D + d, 16);
+                q[a][j].x ^= p.flip; q[a][j].y ^= p.flip; q[a][j].z ^= p.flip; q[a][j].w ^= p.flip;
+            }
+        }
+    }
+
+    const T *k_base = static_cast<const T *>(p.k) + (int64_t)k0 * p.ldk + (int64_t)hk * p.D;
+    const T *v_base = static_cast<const T *>(p.v) + (int64_t)k0 * p.ldv + (int64_t)hk * p.D;
+    uint4 ks[CH], vs[CH];
+    auto fetch = [&](int j0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int id = i * 256 + threadIdx.x, row = id / PIECES, d = id % PIECES * 8;
+            ks[i] = vs[i] = make_uint4(0, 0, 0, 0);
+            if (j0 + row < end && d < p.D) {
+                __builtin_memcpy(&ks[i], k_base + (int64_t)(j0 + row) * p.ldk + d, 16);
+                __builtin_memcpy(&vs[i], v_base + (int64_t)(j0 + row) * p.ldv + d, 16);
+            }
+        }
+    };
+    auto put = [&](int stage) {
+        uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int id = i * 256 + threadIdx.x, row = id / PIECES, piece = id % PIECES;
+            *reinterpret_cast<uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, piece) * 8) = ks[i];
+            *reinterpret_cast<uint4 *>(vt + row * PITCH + v_piece<PITCH>(row, piece) * 8) = vs[i];
+        }
+    };
+
+    at_f16 o[QT][DT];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int a = 0; a < QT; ++a) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[a][d][i] = 0.0f;
+        m[a] = -__builtin_inff();
+        l[a] = 0.0f;
+    }
+
+    // A key that only some rows see has probability 0 in the others, and 0 times an infinite or NaN value is no 0.  From the first key on
+    // that not all rows see, steps with such values take a way of their own.
+    const int partial = row0 + 1 + off;
+    auto odd_values = [&] {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const uint32_t w[4] = {vs[i].x, vs[i].y, vs[i].z, vs[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= (w[e] & EXP) == EXP || (w[e] >> 16 & EXP) == EXP;
+        }
+        return odd;
+    };
+    bool odd = false;
+    auto settle = [&](int j0) {                                          // the barrier before the step of j0
+        if (j0 + KEYS > partial)
+            odd = __syncthreads_or(odd_values());
+        else
+            __syncthreads();
+    };
+
+    if (end > 0) {
+        fetch(0);
+        put(0);
+        settle(0);
+    }
+    int stage = 0;
+    for (int j0 = 0; j0 < end; j0 += KEYS, stage ^= 1) {
+        const bool more = j0 + KEYS < end;
+        const bool odd_now = odd;
+        if (more) fetch(j0 + KEYS);
+        uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        // ---- scores: lane (r, half) has row r, keys 32 u + 8 (i / 4) + 4 half + i % 4
+        at_f16 s[QT][U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int a = 0; a < QT; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[a][u][i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) {
+                const int row = 32 * u + r;
+                const uint4 f = *reinterpret_cast<const uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, 2 * j + half) * 8);
+#pragma unroll
+                for (int a = 0; a < QT; ++a) s[a][u] = mma32<T>(f, q[a][j], s[a][u]);
+            }
+        }
+        uint4 pr[QT][2 * U];
+#pragma unroll
+        for (int a = 0; a < QT; ++a) {
+            const int row = row0 + (wave * QT + a) * 32 + r, last = min(Lk - 1, row + off);    // the last key that the row sees
+            if (j0 + KEYS > min(Lk, row0 + (wave * QT + a) * 32 + 1 + off)) {               // (for the tile's first row, and so for all)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (j0 + 32 * u + 8 * (i / 4) + 4 * half + i % 4 > last) s[a][u][i] = -__builtin_inff();
+            }
+            float top = s[a][0][0];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[a][u][i]);
+            top = across32(top, false) * p.scale;
+            if (__any(top > m[a] + PR_SLACK)) {
+                const float n = fmaxf(m[a], top);
+                const float w = m[a] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[a] - n);
+                m[a] = n;
+                l[a] *= w;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[a][d][i] *= w;
+            }
+            // (f16 probabilities are 2^7 times as large, 2^15 at most, so that small ones keep their bits)
+            const float base = m[a] == -__builtin_inff() ? 0.0f : m[a] - (F16 ? 7.0f : 0.0f);
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[a][u][i] = __builtin_amdgcn_exp2f(fmaf(s[a][u][i], p.scale, -base));
+                    sum += s[a][u][i];
+                }
+            l[a] += sum;
+#pragma unroll
+            for (int e = 0; e < 2 * U; ++e)
+                pr[a][e] = make_uint4(pair16<T>(s[a][e / 2][8 * (e & 1)], s[a][e / 2][8 * (e & 1) + 1]),
+                                      pair16<T>(s[a][e / 2][8 * (e & 1) + 2], s[a][e / 2][8 * (e & 1) + 3]),
+                                      pair16<T>(s[a][e / 2][8 * (e & 1) + 4], s[a][e / 2][8 * (e & 1) + 5]),
+                                      pair16<T>(s[a][e / 2][8 * (e & 1) + 6], s[a][e / 2][8 * (e & 1) + 7]));
+        }
+        if (odd_now) {
+            // p v = v for such a value in a row that sees it (p > 0), so it is added as it is, and is 0 in the product
+            for (int j = 0; j < KEYS; ++j)
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int col = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+                        const uint16_t v = vt[j * PITCH + v_piece<PITCH>(j, col >> 3) * 8 + (col & 7)];
+#pragma unroll
+                        for (int a = 0; a < QT; ++a)
+                            if ((v & EXP) == EXP && j0 + j < Lk && j0 + j <= row0 + (wave * QT + a) * 32 + r + off) o[a][d][i] += value16<T>(v);
+                    }
+            __syncthreads();
+            for (int i = threadIdx.x; i < TILE; i += 256)
+                if ((vt[i] & EXP) == EXP) vt[i] = 0;
+            __syncthreads();
+        }
+        // ---- V^T P^T: keys 16 e + 4 half + (0 .. 3) and eight further on, as the scores lie
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 2 * U; ++e) {
+                const int row = 16 * e + 4 * half + (lane & 15) / 4, col = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+                const uint2 a = read_transposed(vt + row * PITCH + v_piece<PITCH>(row, col >> 3) * 8 + (col & 7));
+                const uint2 b = read_transposed(vt + (row + 8) * PITCH + v_piece<PITCH>(row + 8, col >> 3) * 8 + (col & 7));
+                const uint4 f = make_uint4(a.x, a.y, b.x, b.y);
+#pragma unroll
+                for (int c = 0; c < QT; ++c) o[c][d] = mma32<T>(f, pr[c][e], o[c][d]);
+            }
+        if (more) {
+            put(stage ^ 1);
+            settle(j0 + KEYS);
+        }
+    }
+
+    // ---- lane: row r, columns 32 d + 8 (i / 4) + 4 half + i % 4
+#pragma unroll
+    for (int a = 0; a < QT; ++a) {
+        const int row = row0 + (wave * QT + a) * 32 + r;
+        const bool any = min(Lk - 1, row + off) >= 0;
+        // (a row whose every score is -inf has a sum of 0 and comes out as NaN, as its definition does; a row without keys as 0)
+        const float w = 1.0f / across32(l[a], true);
+        if (row >= Lq) continue;
+        T *to = static_cast<T *>(p.o) + (int64_t)(q0 + row) * p.ldo + (int64_t)h * p.D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int col = 32 * d + 2 * i + 4 * half;
+                const uint2 y = any ? make_uint2(pair16<T>(o[a][d][i] * w, o[a][d][i + 1] * w), pair16<T>(o[a][d][i + 2] * w, o[a][d][i + 3] * w)) : make_uint2(0, 0);
+                if (col < p.D) __builtin_memcpy(to + col, &y, 8);
+            }
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+template <typename T, int DP, int QT>
+static nq_status launch_prompt(PromptParams &p, hipStream_t s)
+{
+    constexpr int BYTES = 4 * keys_of(DP) * pitch_of(DP) * 2;
+    auto kernel = k_attention_prompt<T, DP, QT>;
+    static std::atomic<uint64_t> granted{0};
+    const nq_status st = grant_lds(kernel, BYTES, granted);
+    if (st != NQ_OK) return st;
+    p.tiles = p.q_rows / (128 * QT) + p.sequences;
+    kernel<<<(unsigned)p.tiles * (unsigned)p.Hq, 256, BYTES, s>>>(p);
+    return launch_status();
+}
+
+template <typename T>
+static nq_status run_prompt(PromptParams &p, hipStream_t s)
+{
+    if (p.D <= 64) return launch_prompt<T, 64, 1>(p, s);
+    if (p.D <= 96) return launch_prompt<T, 96, 1>(p, s);
+    if (p.D <= 128) return launch_prompt<T, 128, 1>(p, s);
+    if (p.D <= 192) return launch_prompt<T, 192, 1>(p, s);
+    return launch_prompt<T, 256, 1>(p, s);
+}
+
+}  // namespace nq
+
+using namespace nq;
+
+extern "C" nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream)
+{
+    if (!job || job->sequences < 0 || job->q_rows < 0 || job->k_rows < 0) return NQ_ERR_INVALID_ARG;
+    const nq_prompt_job &j = *job;
+    if (!is_dtype(j.dtype)) return NQ_ERR_INVALID_ARG;
+    nq_status st;
+    if ((st = check_heads(j.q_heads, j.kv_heads, j.head_dim)) != NQ_OK) return st;
+    if (j.q_heads % j.kv_heads) return NQ_ERR_SHAPE;
+    if (j.dtype == NQ_DT_F32) return NQ_ERR_UNSUPPORTED;
+    if (j.q_rows > ATT_MAX_ROWS || j.k_rows > ATT_MAX_ROWS || j.sequences > ATT_MAX_ROWS) return NQ_ERR_SHAPE;
+    // (a dispatch has fewer than 2^32 threads)
+    if ((j.q_rows / 128 + j.sequences) * j.q_heads >= (int64_t(1) << 24)) return NQ_ERR_SHAPE;
+    if (j.sequences == 0 || j.q_rows == 0) return NQ_OK;
+    const int64_t wq = (int64_t)j.q_heads * j.head_dim, wk = (int64_t)j.kv_heads * j.head_dim;
+    if ((st = check_matrix(j.d_q, j.dtype, wq, j.ldq)) != NQ_OK) return st;
+    if ((st = check_matrix(j.d_o, j.dtype, wq, j.ldo)) != NQ_OK) return st;
+    if (j.k_rows > 0 && (st = check_matrix(j.d_k, j.dtype, wk, j.ldk)) != NQ_OK) return st;
+    if (j.k_rows > 0 && (st = check_matrix(j.d_v, j.dtype, wk, j.ldv)) != NQ_OK) return st;
+    if (!j.d_q_begin) return NQ_ERR_INVALID_ARG;
+    if (!aligned_to(j.d_q_begin, 4) || !aligned_to(j.d_k_begin, 4)) return NQ_ERR_ALIGN;
+
+    PromptParams p;
+    p.q = j.d_q;
+    p.k = j.d_k;
+    p.v = j.d_v;
+    p.o = j.d_o;
+    p.q_begin = j.d_q_begin;
+    p.k_begin = j.d_k_begin ? j.d_k_begin : j.d_q_begin;
+    p.ldq = j.ldq;
+    p.ldk = j.ldk;
+    p.ldv = j.ldv;
+    p.ldo = j.ldo;
+    p.sequences = (int32_t)j.sequences;
+    p.q_rows = (int32_t)j.q_rows;
+    p.k_rows = (int32_t)j.k_rows;
+    p.Hq = j.q_heads;
+    p.Hkv = j.kv_heads;
+    p.group = j.q_heads / j.kv_heads;
+    p.D = j.head_dim;
+    p.causal = j.causal != 0;
+    p.by_heads = make_divider((uint32_t)j.q_heads);
+    p.scale = j.scale == 0.0f ? 1.0f : j.scale < 0.0f ? -j.scale * PR_LOG2E : j.scale * PR_LOG2E;
+    p.flip = j.scale < 0.0f ? 0x80008000u : 0u;
+    p.zero = j.scale == 0.0f;
+    return j.dtype == NQ_DT_F16 ? run_prompt<_Float16>(p, (hipStream_t)stream) : run_prompt<bf16_t>(p, (hipStream_t)stream);
+}

@@ -35,6 +35,16 @@ qfp8_fn qfp8_of;
 gfp8_fn gfp8_of;
 norm_fn norm_of;
 
+PyObject *t_cache, *t_head_job, *t_prompt_job, *t_token_job;
+typedef nq_status (*head_fn)(const nq_head_job *, int64_t, void *);
+typedef nq_status (*read_fn)(const nq_kv_cache *, const int64_t *, int64_t, void *, int64_t, void *, int64_t, int, void *);
+typedef nq_status (*prompt_fn)(const nq_prompt_job *, void *);
+typedef nq_status (*token_fn)(const nq_token_job *, void *);
+head_fn head_of;
+read_fn read_of;
+prompt_fn prompt_of;
+token_fn token_of;
+
 // A descriptor's memory for the length of a call.
 struct Struct {
     Py_buffer view;
@@ -312,6 +322,72 @@ PyObject *setup_fp8(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// (job, T, stream)
+PyObject *head_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct j;
+    void *s;
+    int64_t T;
+    if (n != 3 || !j.take(a[0], t_head_job, sizeof(nq_head_job)) || !integer(a[1], &T) || !stream(a[2], &s)) return not_plain();
+    NQ_CALL(st, head_of(j.as<nq_head_job>(), T, s));
+    return PyLong_FromLong(st);
+}
+
+// (cache, slot, T, k, ldk, v, ldv, dtype, stream)
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct c;
+    void *slot, *k, *v, *s;
+    int64_t T, ldk, ldv, dtype;
+    if (n != 9 || !c.take(a[0], t_cache, sizeof(nq_kv_cache)) || !pointer(a[1], &slot) || !integer(a[2], &T) || !pointer(a[3], &k) ||
+        !integer(a[4], &ldk) || !pointer(a[5], &v) || !integer(a[6], &ldv) || !integer(a[7], &dtype) || dtype != (int)dtype || !stream(a[8], &s))
+        return not_plain();
+    NQ_CALL(st, read_of(c.as<nq_kv_cache>(), (const int64_t *)slot, T, k, ldk, v, ldv, (int)dtype, s));
+    return PyLong_FromLong(st);
+}
+
+// (job, stream)
+PyObject *attention_prompt(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct j;
+    void *s;
+    if (n != 2 || !j.take(a[0], t_prompt_job, sizeof(nq_prompt_job)) || !stream(a[1], &s)) return not_plain();
+    NQ_CALL(st, prompt_of(j.as<nq_prompt_job>(), s));
+    return PyLong_FromLong(st);
+}
+
+// (job, stream)
+PyObject *attention_token(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Struct j;
+    void *s;
+    if (n != 2 || !j.take(a[0], t_token_job, sizeof(nq_token_job)) || !stream(a[1], &s)) return not_plain();
+    NQ_CALL(st, token_of(j.as<nq_token_job>(), s));
+    return PyLong_FromLong(st);
+}
+
+// (types: cache, head job, prompt job, token job; addresses: heads, read, prompt, token)
+PyObject *setup_attention(PyObject *, PyObject *args)
+{
+    PyObject *o[4], *f[4];
+    if (!PyArg_ParseTuple(args, "OOOOOOOO", o, o + 1, o + 2, o + 3, f, f + 1, f + 2, f + 3)) return nullptr;
+    void *at[4];
+    for (int i = 0; i < 4; ++i)
+        if (!(at[i] = PyLong_AsVoidPtr(f[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "no address");
+    for (PyObject *p : o)
+        if (!PyType_Check(p)) return PyErr_Format(PyExc_TypeError, "not a type");
+    for (PyObject *p : o) Py_INCREF(p);                        // held for the life of the process
+    t_cache = o[0];
+    t_head_job = o[1];
+    t_prompt_job = o[2];
+    t_token_job = o[3];
+    head_of = (head_fn)at[0];
+    read_of = (read_fn)at[1];
+    prompt_of = (prompt_fn)at[2];
+    token_of = (token_fn)at[3];
+    Py_RETURN_NONE;
+}
+
 PyObject *set_stream_ready(PyObject *, PyObject *v)
 {
     stream_ready = PyObject_IsTrue(v) == 1;
@@ -321,6 +397,8 @@ PyObject *set_stream_ready(PyObject *, PyObject *v)
 #define NQ_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NQ_FAST(gemm), NQ_FAST(conv), NQ_FAST(gconv), NQ_FAST(quantize_pack), NQ_FAST(layer),
                          NQ_FAST(quantize_fp8), NQ_FAST(gemm_fp8), NQ_FAST(block_norm), {"setup_fp8", setup_fp8, METH_VARARGS, nullptr},
+                         NQ_FAST(head_norm), NQ_FAST(cache_read), NQ_FAST(attention_prompt), NQ_FAST(attention_token),
+                         {"setup_attention", setup_attention, METH_VARARGS, nullptr},
                          {"setup", setup, METH_VARARGS, nullptr},
                          {"set_stream_ready", set_stream_ready, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
