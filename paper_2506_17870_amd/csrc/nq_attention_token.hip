@@ -15,39 +15,115 @@ typedef __bf16 at_b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 at_h2 __attribute__((ext_vector_type(2)));
 typedef float at_f4 __attribute__((ext_vector_type(4)));
 
-constexpr int TK_WAVES = 4, TK_TILE = 32, TK_COLS = 16;   // tokens of a wave's step; query heads of a matrix tile
+constexpr int TK_TILE = 32, TK_COLS = 16;                  // tokens of a wave's step; query heads of a matrix tile
 constexpr float TK_LOG2E = 1.44269504088896340736f;
+
+constexpr int TK_LEAST = 128;                              // tokens of a piece, at least
+// Workgroups to a compute unit, by their registers.
+__host__ __device__ constexpr int workgroups_of(int head_dim, bool codes) { return head_dim <= 128 ? 3 : codes ? 2 : 1; }
 
 struct TokenParams {
     const void *q;
     void *o;
     const int32_t *table, *length;
-    float *partial;                       // [sequences][q_heads][parts][D + 4]: sums of o, then m and l
+    float *partial;                       // sums of o [pieces][q_heads][D], then m and l [pieces][q_heads][2]
     CacheView cache;
     int64_t ldq, ldo, ldtable;
-    int32_t sequences, max_length, Hq, Hkv, group, col_tiles, D, parts, target;
+    int32_t sequences, max_length, Hq, Hkv, group, col_tiles, D, pieces;   // pieces: 0 where no sequence is split
+    float share;                          // of all tokens, for a workgroup
     float scale;                          // times log2(e)
 };
 
-// How a sequence of `length` tokens is split: into chunks of this many, `parts` at most.  The chunk is the share of a workgroup if
-// all tokens of the call were dealt evenly to p.target of them, so that long sequences of a mixed batch go to more workgroups than short ones.
-// Every wave that asks makes the same sum.
-__device__ __forceinline__ int chunk_of(const TokenParams &p, int length)
-{
-    if (p.parts == 1) return max(length, 1);
-    int64_t total = 0;
-    for (int i = threadIdx.x & 63; i < p.sequences; i += 64) total += min(max(p.length[i], 0), p.max_length);
-    if (p.sequences > 1) {
+// How the call's tokens are dealt to workgroups.  chunk is the share of each if all tokens were dealt evenly to as many as the card holds.  A sequence
+// of more than half a chunk goes into pieces of equal size, as few as have a chunk at most; those come first, and the shorter sequences,
+// a piece each, fill the gaps that they leave.  So there are as many pieces as workgroups wanted, and one more for each sequence, at most.
+// Every wave that asks makes the same sums in the same order.
+constexpr int TK_MOST_PLANNED = 1024;     // sequences: sixteen to a lane
+
+__device__ __forceinline__ int length_of(const TokenParams &p, int i) { return i < p.sequences ? min(max(p.length[i], 0), p.max_length) : 0; }
+
+// The call's lengths, a lane each of 64 sequences, 256 asked for at once and kept if there are no more.
+struct Lengths {
+    const TokenParams &p;
+    int at, held[4];
+    __device__ __forceinline__ explicit Lengths(const TokenParams &params) : p(params) { ask(0); }
+    __device__ __forceinline__ void ask(int from)
+    {
+        at = from;
 #pragma unroll
-        for (int k = 1; k < 64; k *= 2) total += __shfl_xor(total, k);
-    } else {
-        total = __shfl(total, 0);
+        for (int r = 0; r < 4; ++r) held[r] = length_of(p, from + 64 * r + (threadIdx.x & 63));
     }
-    const int64_t blocks = (int64_t)p.Hkv * p.col_tiles;
-    const int64_t even = (total * blocks + p.target - 1) / p.target;
-    const int64_t least = (length + p.parts - 1) / p.parts;
-    const int64_t chunk = min(max(max(even, least), (int64_t)(TK_WAVES * TK_TILE)), (int64_t)length + 1);
-    return (int)((chunk + TK_TILE - 1) / TK_TILE * TK_TILE);
+    // f(first of 64 sequences, this lane's length), until it returns true
+    template <typename F>
+    __device__ __forceinline__ void each(F f)
+    {
+        for (int i = 0; i < p.sequences; i += 256) {
+            if (at != i) ask(i);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (i + 64 * r < p.sequences && f(i + 64 * r, held[r])) return;
+        }
+    }
+};
+
+__device__ __forceinline__ int chunk_of(const TokenParams &p, Lengths &lengths)
+{
+    float total = 0.0f;
+    lengths.each([&](int, int length) {
+        total += (float)length;
+        return false;
+    });
+    const float even = fminf(ceilf(sum64(total) * p.share), 2147483520.0f);
+    return __builtin_amdgcn_readfirstlane((max((int)even, TK_LEAST) + TK_TILE - 1) / TK_TILE * TK_TILE);
+}
+// Sum over the lanes before this one.
+__device__ __forceinline__ int before(int v, int *all)
+{
+    int x = v;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // one, two, four and eight lanes on in the row of sixteen
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the row before's last to the second and fourth row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // the half's last to the other half
+    *all = __builtin_amdgcn_readlane(x, 63);
+    return x - v;
+}
+struct Pieces {
+    int first, count, size;               // numbers of a sequence's pieces, tokens of one
+};
+// Calls found(sequence, length, Pieces) for 64 sequences at a time, a lane each, until it says that that was it.
+template <typename F>
+__device__ __forceinline__ void each_sequence(const TokenParams &p, F found)
+{
+    const int lane = threadIdx.x & 63;
+    Lengths lengths(p);
+    const int chunk = chunk_of(p, lengths);
+    auto pieces = [&](int length) {
+        const int n = max((length + chunk - 1) / chunk, 1), size = max(((length + n - 1) / n + TK_TILE - 1) / TK_TILE * TK_TILE, TK_TILE);
+        return Pieces{0, max((length + size - 1) / size, 1), size};
+    };
+    auto large = [&](int length) { return length > chunk / 2; };
+    int behind = 0, first = 0, all;                                      // behind: pieces of the large sequences
+    if (p.sequences > 64) {
+        lengths.each([&](int, int length) {
+            behind += large(length) ? pieces(length).count : 0;
+            return false;
+        });
+        (void)before(behind, &behind);
+    }
+    lengths.each([&](int i, int length) {
+        const bool is = large(length);
+        Pieces x = pieces(length);
+        const int here = before(is ? x.count : 0, &all);
+        if (p.sequences <= 64) behind = all;
+        const uint64_t mask = __ballot(!is && i + lane < p.sequences);
+        x.first = is ? first + here : behind + __popcll(mask & ((uint64_t(1) << lane) - 1));
+        if (i + lane >= p.sequences) x.count = 0;
+        first += all;
+        behind += __popcll(mask);
+        return found(i + lane, length, x);
+    });
 }
 
 template <typename T>
@@ -94,34 +170,100 @@ __device__ __forceinline__ uint32_t codes2(uint32_t d)
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, 1.0f, HIGH));
 }
 
-// T: queries and outputs; CODES: an e4m3 cache; DP: columns, head_dim rounded up to a form; FAST: head_dim == DP and pages of
-// whole 16 tokens, so that a tile of 16 tokens has one page, found by scalar loads.
-template <typename T, bool CODES, int DP, bool FAST>
-__global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenParams p)
-{
-    constexpr int KJ = DP / 32, VC = DP / 16, ES = CODES ? 1 : 2;      // products to a score; columns of V to a lane
-    constexpr int KW = CODES ? 2 : 4;                                   // dwords of eight elements
-    using VT = typename std::conditional<CODES, bf16_t, T>::type;       // codes times their scale: bf16's range, in two parts
-    __shared__ float joined[2][TK_COLS][DP + 4];
-    __shared__ float tops[TK_WAVES][TK_COLS];
+// What a lane holds of 32 tokens, half u of them 16.  k: token n of a half, columns 32 j + 8 g; v: tokens 4 g + i, columns column(n, c).
+template <int KJ, int KW, int VW>
+struct TokenTile {
+    uint32_t k[2][KJ][KW], v[2][4][VW];
+    float scale;                          // of token n of half (lane / 32): its key's (lanes 0 .. 15 of the half wave) or its value's
+    uint32_t live;                        // bit 4 u + i: token 4 g + i of half u is there
+};
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    const int s = blockIdx.z, hk = blockIdx.y / p.col_tiles, col0 = (blockIdx.y - hk * p.col_tiles) * TK_COLS;
+// T: queries and outputs; CODES: an e4m3 cache; DP: columns, head_dim rounded up to a form; CUT: head_dim < DP.
+template <typename T, bool CODES, int DP, bool CUT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : workgroups_of(DP, CODES)) k_attention_token(const TokenParams p)
+{
+    constexpr int KJ = DP / 32, VC = DP / 16, RUN = VC < 8 ? VC : 8, ES = CODES ? 1 : 2;      // products to a score; columns of V to a lane, and beside each other
+    constexpr int KW = CODES ? 2 : 4, VW = VC / (4 / ES), RW = RUN / (4 / ES);                // dwords of eight elements; of VC; of RUN
+    constexpr int STEP = WAVES * TK_TILE;
+    using VT = typename std::conditional<CODES, bf16_t, T>::type;       // codes times their scale: bf16's range, in two parts
+    using Tile = TokenTile<KJ, KW, VW>;
+    __shared__ __attribute__((aligned(16))) float joined[WAVES / 2][TK_COLS][DP + 4];
+    __shared__ float tops[WAVES][TK_COLS];
+    __shared__ __attribute__((aligned(16))) float scales[WAVES][64];
+    __shared__ __attribute__((aligned(16))) int64_t rows[WAVES][TK_TILE];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    // (heads first: neighbouring workgroups go to the eight dies in turn)
+    const int hk = blockIdx.x / p.col_tiles, col0 = (blockIdx.x - hk * p.col_tiles) * TK_COLS, piece = blockIdx.y;
     const int cols = min(TK_COLS, p.group - col0), head0 = hk * p.group + col0;
-    const int length = min(max(__builtin_amdgcn_readfirstlane(p.length[s]), 0), p.max_length);
-    const int chunk = chunk_of(p, length);
-    if (blockIdx.x > 0 && (int64_t)blockIdx.x * chunk >= length) return; // (the first part of a sequence without tokens writes its zeros)
-    const int begin = blockIdx.x * chunk, end = min(length, begin + chunk);
+    int s = piece, begin = 0, end = 0;
+    bool whole = true;
+    if (p.pieces) {
+        s = -1;
+        each_sequence(p, [&](int i, int length, const Pieces &x) {
+            const uint64_t mask = __ballot(piece >= x.first && piece < x.first + x.count);
+            if (!mask) return false;
+            const int from = __builtin_ctzll(mask), at = (piece - x.first) * x.size;
+            s = __builtin_amdgcn_readlane(i, from);
+            begin = __builtin_amdgcn_readlane(at, from);
+            end = __builtin_amdgcn_readlane(at + min(length - at, x.size), from);
+            whole = __builtin_amdgcn_readlane(x.count, from) == 1;
+            return true;
+        });
+        if (s < 0) return;
+    } else {
+        end = __builtin_amdgcn_readfirstlane(length_of(p, s));
+    }
+    auto column = [&](int c) { return RUN * n + (c / RUN) * 16 * RUN + c % RUN; };
+
+    // ---- loading, in three steps: the page of a token, where its row is, the row
+    const int32_t *table = p.table + s * p.ldtable;
+    const int mine = 16 * (lane >> 5) + n;                              // the token of 32 that this lane looks up
+    auto token_at = [&](int t0) { return (uint32_t)min(t0 + mine, end - 1); };
+    auto page_of = [&](int t0) { return table[divide(token_at(t0), p.cache.by_page)]; };
+    const uint8_t *k_head = p.cache.k + hk * p.cache.head_step * ES, *v_head = p.cache.v + hk * p.cache.head_step * ES;
+    const float *scale_head = (lane & 16 ? p.cache.v_scale : p.cache.k_scale) + hk * p.cache.scale_head_step;
+    auto load = [&](Tile &x, int t0, int32_t page) {
+        const uint32_t t = token_at(t0), place = t - divide(t, p.cache.by_page) * p.cache.by_page.d;
+        const bool there = t0 + mine < end && (uint32_t)page < (uint32_t)p.cache.pages;
+        const int64_t row = (int64_t)page * p.cache.page_step + (int64_t)place * p.cache.token_step;
+        rows[wave][mine] = there ? row : -1;                             // (two lanes write the same)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();                                 // (LDS serves a wave's requests in order)
+        if constexpr (CODES) x.scale = scale_head[there ? (int64_t)page * p.cache.scale_page_step + (int64_t)place * p.cache.scale_token_step : 0];
+        x.live = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            // (a token that is not there: the cache's first, whose value is not used)
+            const uint8_t *k = k_head + max(rows[wave][16 * u + n], (int64_t)0) * ES;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) {
+                const int d = 32 * j + 8 * g;
+                __builtin_memcpy(x.k[u][j], k + (CUT && d >= p.D ? 0 : d) * ES, sizeof x.k[u][j]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t at = rows[wave][16 * u + 4 * g + i];
+                x.live |= at >= 0 ? 1u << (4 * u + i) : 0u;
+                const uint8_t *v = v_head + max(at, (int64_t)0) * ES;
+#pragma unroll
+                for (int c = 0; c < VC; c += RUN)
+                    __builtin_memcpy(&x.v[u][i][c / RUN * RW], v + (CUT && column(c) >= p.D ? 0 : column(c)) * ES, RW * 4);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
 
     uint4 q[KJ];
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
         q[j] = make_uint4(0, 0, 0, 0);
         const int d = 32 * j + 8 * g;
-        if (n < cols && d < p.D) __builtin_memcpy(&q[j], static_cast<const T *>(p.q) + s * p.ldq + (int64_t)(head0 + n) * p.D + d, 16);
+        if (n < cols && (!CUT || d < p.D)) __builtin_memcpy(&q[j], static_cast<const T *>(p.q) + s * p.ldq + (int64_t)(head0 + n) * p.D + d, 16);
     }
-    const int32_t *table = p.table + s * p.ldtable;
-    const int64_t at_head = hk * p.cache.head_step, scale_head = hk * p.cache.scale_head_step;
 
     at_f4 o[VC];
 #pragma unroll
@@ -129,100 +271,81 @@ __global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenPa
     float m = -__builtin_inff(), l = 0.0f;
     bool seen = false;
 
-    for (int t0 = begin + wave * TK_TILE; t0 < end; t0 += TK_WAVES * TK_TILE) {
-        // ---- keys and values of 32 tokens: token 16 u + n for the first product, 16 u + 4 g + i for the second
-        uint32_t k[2][KJ][KW], v[2][4][VC / (4 / ES)];
+    auto attend = [&](Tile &y) {
         float ks[2][4], vs[2][4];
-        bool live[2][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int tu = t0 + 16 * u;
-            auto row = [&](int t, bool &ok, int64_t &at, int64_t &scale) {
-                ok = t < end;
-                const int tc = ok ? t : 0;
-                int pg, place;
-                if constexpr (FAST) {
-                    const int first = tu < end ? tu : 0;
-                    pg = (int)divide((uint32_t)first, p.cache.by_page);
-                    place = first - pg * (int)p.cache.by_page.d + (ok ? t - tu : 0);
-                } else {
-                    pg = (int)divide((uint32_t)tc, p.cache.by_page);
-                    place = tc - pg * (int)p.cache.by_page.d;
-                }
-                const int32_t page = table[pg];
-                ok = ok && (uint32_t)page < (uint32_t)p.cache.pages;
-                at = ok ? (int64_t)page * p.cache.page_step + (int64_t)place * p.cache.token_step + at_head : at_head;
-                scale = ok ? (int64_t)page * p.cache.scale_page_step + (int64_t)place * p.cache.scale_token_step + scale_head : scale_head;
-            };
-            bool ok;
-            int64_t at, scale;
-            row(tu + n, ok, at, scale);
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) {
-                const int d = 32 * j + 8 * g;
-                const bool in = FAST || d < p.D;
-                uint32_t x[KW];
-                __builtin_memcpy(x, p.cache.k + (at + (in ? d : 0)) * ES, sizeof x);
-#pragma unroll
-                for (int i = 0; i < KW; ++i) k[u][j][i] = in ? x[i] : 0u;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                row(tu + 4 * g + i, ok, at, scale);
-                live[u][i] = ok;
-                const int d = VC * n;
-                const bool in = FAST || d < p.D;
-                uint32_t x[VC / (4 / ES)];
-                if (FAST || d + VC <= p.D) {
-                    __builtin_memcpy(x, p.cache.v + (at + (in ? d : 0)) * ES, sizeof x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VC / (4 / ES); ++e) {
-                        x[e] = 0;
-                        if (d + (4 / ES) * e < p.D) __builtin_memcpy(&x[e], p.cache.v + (at + d + (4 / ES) * e) * ES, 4);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < VC / (4 / ES); ++e) v[u][i][e] = ok ? x[e] : 0u;
-                if constexpr (CODES) {
-                    ks[u][i] = p.cache.k_scale[scale];
-                    vs[u][i] = ok ? p.cache.v_scale[scale] : 0.0f;
-                }
-            }
+        if constexpr (CODES) {                                          // (LDS serves a wave's requests in order)
+            scales[wave][lane] = y.scale;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
         // ---- scores
         float x[2][4];
-        float top = -__builtin_inff();
+        at_f4 acc[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            at_f4 acc{0, 0, 0, 0};
+            acc[u] = at_f4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < KJ; ++j) {
+                if (CUT && 32 * j + 8 * g >= p.D) {
+#pragma unroll
+                    for (int i = 0; i < KW; ++i) y.k[u][j][i] = 0;
+                }
                 uint4 a;
                 if constexpr (CODES)
-                    a = make_uint4(codes2<T, false>(k[u][j][0]), codes2<T, true>(k[u][j][0]), codes2<T, false>(k[u][j][1]), codes2<T, true>(k[u][j][1]));
+                    a = make_uint4(codes2<T, false>(y.k[u][j][0]), codes2<T, true>(y.k[u][j][0]), codes2<T, false>(y.k[u][j][1]), codes2<T, true>(y.k[u][j][1]));
                 else
-                    a = make_uint4(k[u][j][0], k[u][j][1], k[u][j][2], k[u][j][3]);
-                acc = mma<T>(a, q[j], acc);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float y = acc[i] * p.scale;
-                if constexpr (CODES) y *= ks[u][i];
-                x[u][i] = live[u][i] ? y : -__builtin_inff();
-                top = fmaxf(top, x[u][i]);
-                seen |= live[u][i];
+                    a = make_uint4(y.k[u][j][0], y.k[u][j][1], y.k[u][j][2], y.k[u][j][3]);
+                acc[u] = mma<T>(a, q[j], acc[u]);
             }
         }
+        if constexpr (CODES) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                __builtin_memcpy(ks[u], &scales[wave][32 * u + 4 * g], 16);
+                __builtin_memcpy(vs[u], &scales[wave][32 * u + 16 + 4 * g], 16);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[u][i] = acc[u][i] * p.scale;
+                if constexpr (CODES) x[u][i] *= ks[u][i];
+            }
+        if (!__all(y.live == 0xffu)) {
+            // what is not there has no weight, and no value that could be infinite or NaN
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(y.live >> (4 * u + i) & 1)) {
+                        x[u][i] = -__builtin_inff();
+                        if constexpr (CODES) vs[u][i] = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) y.v[u][i][e] = 0;
+                    }
+            seen |= y.live != 0;
+        } else {
+            seen = true;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, x[u][i]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         // (f16 probabilities are 2^15 times as large, so that small ones keep their bits: 2^-39 of the largest is the least)
         const float m_new = fmaxf(m, top), base = m_new == -__builtin_inff() ? 0.0f : m_new - (__is_same(VT, _Float16) ? 15.0f : 0.0f);
-        const float alpha = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= alpha;
+        if (__any(m_new > m)) {                                         // (seldom after the first tokens)
+            const float alpha = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
 #pragma unroll
-        for (int c = 0; c < VC; ++c) o[c] *= alpha;
+            for (int c = 0; c < VC; ++c) o[c] *= alpha;
+        }
         // ---- probabilities, each as the sum of two parts of VT, which together have twice its bits; the matrix core has time for it
         uint32_t hi[4], lo[4];
 #pragma unroll
@@ -250,11 +373,11 @@ __global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenPa
                 for (int i = 0; i < 4; i += 2) {
                     uint32_t a, b;
                     if constexpr (CODES) {
-                        a = c % 4 ? codes2<VT, true>(v[u][i][c / 4]) : codes2<VT, false>(v[u][i][c / 4]);
-                        b = c % 4 ? codes2<VT, true>(v[u][i + 1][c / 4]) : codes2<VT, false>(v[u][i + 1][c / 4]);
+                        a = c % 4 ? codes2<VT, true>(y.v[u][i][c / 4]) : codes2<VT, false>(y.v[u][i][c / 4]);
+                        b = c % 4 ? codes2<VT, true>(y.v[u][i + 1][c / 4]) : codes2<VT, false>(y.v[u][i + 1][c / 4]);
                     } else {
-                        a = v[u][i][c / 2];
-                        b = v[u][i + 1][c / 2];
+                        a = y.v[u][i][c / 2];
+                        b = y.v[u][i + 1][c / 2];
                     }
                     even[2 * u + i / 2] = __builtin_amdgcn_perm(b, a, 0x05040100u);
                     odd[2 * u + i / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
@@ -262,6 +385,23 @@ __global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenPa
             const uint4 ve = make_uint4(even[0], even[1], even[2], even[3]), vo = make_uint4(odd[0], odd[1], odd[2], odd[3]);
             o[c] = mma<VT>(ve, pl, mma<VT>(ve, ph, o[c]));
             o[c + 1] = mma<VT>(vo, pl, mma<VT>(vo, ph, o[c + 1]));
+        }
+    };
+
+    int t0 = begin + wave * TK_TILE;
+    if (t0 < end) {
+        // The pages of the next tokens are looked up ahead (behind the last ones, theirs again).  The next tokens themselves are not: three
+        // workgroups to a compute unit cover the memory's latency as well as twice the registers do (4 x 65536 tokens of bf16 187 us, with
+        // two tiles in registers 186; 256 x 1024 of e4m3 51.6 and 55.5).
+        auto next = [&](int t) { return t + STEP < end ? t + STEP : t; };
+        Tile x;
+        int32_t page = page_of(t0), after = page_of(next(t0));
+        for (;;) {
+            load(x, t0, page);
+            page = after;
+            after = page_of(next(next(t0)));
+            attend(x);
+            if ((t0 += STEP) >= end) break;
         }
     }
 
@@ -272,19 +412,20 @@ __global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenPa
     const bool any = __syncthreads_or(seen);
     float top = tops[0][n];
 #pragma unroll
-    for (int w = 1; w < TK_WAVES; ++w) top = fmaxf(top, tops[w][n]);
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w][n]);
     const float alpha = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top);
     l *= alpha;
 #pragma unroll
     for (int c = 0; c < VC; ++c) o[c] *= alpha;
-    // lane: head n, columns VC (4 g + i) + c
+    // lane: head n, columns of the rows 4 g + i of the product
+    auto column_of = [&](int i, int c) { return RUN * (4 * g + i) + (c / RUN) * 16 * RUN + c % RUN; };
 #pragma unroll
-    for (int half = TK_WAVES / 2; half >= 1; half /= 2) {
+    for (int half = WAVES / 2; half >= 1; half /= 2) {
         if (wave >= half && wave < 2 * half) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int c = 0; c < VC; ++c) joined[wave - half][n][VC * (4 * g + i) + c] = o[c][i];
+                for (int c = 0; c < VC; ++c) joined[wave - half][n][column_of(i, c)] = o[c][i];
             if (g == 0) joined[wave - half][n][DP] = l;
         }
         __syncthreads();
@@ -292,13 +433,13 @@ __global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenPa
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int c = 0; c < VC; ++c) o[c][i] += joined[wave][n][VC * (4 * g + i) + c];
+                for (int c = 0; c < VC; ++c) o[c][i] += joined[wave][n][column_of(i, c)];
             l += joined[wave][n][DP];
         }
         __syncthreads();
     }
     if (wave != 0 || n >= cols) return;
-    if (p.parts == 1) {
+    if (whole) {
         // (a row whose every score is -inf has l = 0 and comes out as NaN, as its definition does; a row without tokens as 0)
         const float r = any ? 1.0f / l : 0.0f;
         T *to = static_cast<T *>(p.o) + s * p.ldo + (int64_t)(head0 + n) * p.D;
@@ -306,68 +447,103 @@ __global__ void __launch_bounds__(TK_WAVES * 64) k_attention_token(const TokenPa
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < VC; c += 2) {
-                const int d = VC * (4 * g + i) + c;
+                const int d = column_of(i, c);
                 const uint32_t w = any ? pack2<T>(o[c][i] * r, o[c + 1][i] * r) : 0u;
-                if (FAST || d < p.D) __builtin_memcpy(to + d, &w, 4);
+                if (!CUT || d < p.D) __builtin_memcpy(to + d, &w, 4);
             }
     } else {
-        float *to = p.partial + (((int64_t)s * p.Hq + head0 + n) * p.parts + blockIdx.x) * (p.D + 4);
+        const int64_t row = (int64_t)piece * p.Hq + head0 + n;
+        float *to = p.partial + row * p.D;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < VC; c += 2) {
-                const int d = VC * (4 * g + i) + c;
+                const int d = column_of(i, c);
                 const f8_f2 w{o[c][i], o[c + 1][i]};
-                if (FAST || d < p.D) __builtin_memcpy(to + d, &w, 8);
+                if (!CUT || d < p.D) __builtin_memcpy(to + d, &w, 8);
             }
-        if (g == 0) {
-            to[p.D] = top;
-            to[p.D + 1] = any ? l : -1.0f;                               // (no token of the chunk was there)
-        }
+        if (g == 0)                                                      // (a sum of -1: no token of the piece was there)
+            reinterpret_cast<f8_f2 *>(p.partial + (int64_t)p.pieces * p.Hq * p.D)[row] = f8_f2{top, any ? l : -1.0f};
     }
 }
 
-// Joins the parts of a head: a workgroup for each sequence and query head, D / 4 lanes a part.
-template <typename T>
+// Joins the pieces of a sequence: TH threads for each query head.  All loads are on their way at once: a thread asks for the
+// maximum and sum of one piece, and for four columns of every (4 TH / D)-th.
+template <typename T, int TH>
 __global__ void __launch_bounds__(256) k_attention_join(const TokenParams p)
 {
-    __shared__ float sums[256][5];
-    const int s = blockIdx.y, h = blockIdx.x;
-    const int length = min(max(__builtin_amdgcn_readfirstlane(p.length[s]), 0), p.max_length);
-    const int chunk = chunk_of(p, length);
-    const int parts = max(1, (length + chunk - 1) / chunk);
-    const float *from = p.partial + ((int64_t)s * p.Hq + h) * p.parts * (p.D + 4);
-    const int per = p.D / 4, at = threadIdx.x % per, lane0 = threadIdx.x / per, step = 256 / per;
-    float m = -__builtin_inff();
+    constexpr int AHEAD = TH == 64 ? 8 : 4, HEADS = 256 / TH;
+    __shared__ float sums[HEADS][TH][5], weight[HEADS][TH], tops[4];
+    const int s = blockIdx.y, group = threadIdx.x / TH, tid = threadIdx.x % TH, h = min((int)blockIdx.x * HEADS + group, p.Hq - 1);
+    Pieces all{0, 0, 0};
+    each_sequence(p, [&](int i, int, const Pieces &x) {
+        if (s >= (i & ~63) + 64) return false;
+        all = Pieces{__builtin_amdgcn_readlane(x.first, s & 63), __builtin_amdgcn_readlane(x.count, s & 63), 0};
+        return true;
+    });
+    if (all.count <= 1) return;                                          // (k_attention_token has written the row)
+    const f8_f2 *ml = reinterpret_cast<const f8_f2 *>(p.partial + (int64_t)p.pieces * p.Hq * p.D);
+    const int per = p.D / 4, at = tid % per, mine = tid / per, step = TH / per;
+    auto row = [&](int i) { return (int64_t)(all.first + i) * p.Hq + h; };
+    float m = -__builtin_inff(), l = 0.0f;
     bool any = false;
-    for (int i = 0; i < parts; ++i) {
-        const float l = from[(int64_t)i * (p.D + 4) + p.D + 1];
-        any |= !(l < 0.0f);
-        if (!(l < 0.0f)) m = fmaxf(m, from[(int64_t)i * (p.D + 4) + p.D]);
-    }
     at_f4 o{0, 0, 0, 0};
-    float l = 0.0f;
-    if (lane0 < step)
-        for (int i = lane0; i < parts; i += step) {
-            const float *x = from + (int64_t)i * (p.D + 4);
-            const float mi = x[p.D], li = x[p.D + 1];
-            if (li < 0.0f) continue;
-            const float w = mi == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mi - m);
-            at_f4 y;
-            __builtin_memcpy(&y, x + 4 * at, 16);
-            o += y * w;
-            l = fmaf(li, w, l);
+    for (int base = 0; base < all.count; base += TH) {
+        const int count = min(all.count - base, TH);
+        f8_f2 x{-__builtin_inff(), -1.0f};
+        if (tid < count) x = ml[row(base + tid)];
+        at_f4 y[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (mine < step && mine + i * step < count) __builtin_memcpy(&y[i], p.partial + row(base + mine + i * step) * p.D + 4 * at, 16);
+        const bool there = !(x[1] < 0.0f);                               // (a piece without any token has no weight)
+        float top = there ? x[0] : -__builtin_inff();
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+        if (TH > 64) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
         }
+        any |= __syncthreads_or(there) != 0;                             // (the same tokens for every head of the sequence)
+        if (TH > 64) top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        const float m_new = fmaxf(top, m);
+        const float keep = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
+        const float w = !there || x[0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[0] - m_new);
+        m = m_new;
+        weight[group][tid] = w;
+        l = l * keep + (there ? x[1] * w : 0.0f);
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sums[threadIdx.x][i] = o[i];
-    sums[threadIdx.x][4] = l;
-    __syncthreads();
-    if (threadIdx.x >= per) return;
-    for (int k = 1; k < step; ++k) {
+        for (int c = 0; c < 4; ++c) o[c] *= keep;
+        auto add = [&](int i, const at_f4 &z) {
+            const float v = weight[group][i];
+            if (v != 0.0f) {                                             // (what a piece without weight holds is not used; NaN is one)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += sums[threadIdx.x + k * per][i];
-        l += sums[threadIdx.x + k * per][4];
+                for (int c = 0; c < 4; ++c) o[c] = fmaf(z[c], v, o[c]);
+            }
+        };
+        if (mine < step) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (mine + i * step < count) add(mine + i * step, y[i]);
+            for (int i = mine + AHEAD * step; i < count; i += step) {
+                at_f4 z;
+                __builtin_memcpy(&z, p.partial + row(base + i) * p.D + 4 * at, 16);
+                add(i, z);
+            }
+        }
+        __syncthreads();
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[group][tid][i] = o[i];
+    sums[group][tid][4] = l;
+    __syncthreads();
+    if (tid >= per || (int)blockIdx.x * HEADS + group >= p.Hq) return;
+    for (int k = 1; k < step; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += sums[group][tid + k * per][i];
+    l = 0.0f;
+    for (int k = 0; k < min(TH, all.count); ++k) l += sums[group][k][4];
     const float r = any ? 1.0f / l : 0.0f;
     const uint2 w = any ? make_uint2(pack2<T>(o[0] * r, o[1] * r), pack2<T>(o[2] * r, o[3] * r)) : make_uint2(0, 0);
     __builtin_memcpy(static_cast<T *>(p.o) + s * p.ldo + (int64_t)h * p.D + 4 * at, &w, 8);
@@ -375,47 +551,68 @@ __global__ void __launch_bounds__(256) k_attention_join(const TokenParams p)
 
 // ---- host ------------------------------------------------------------------------------------------------------
 
-// The most parts that a sequence is split into.  About two workgroups to a compute unit are wanted; where lengths differ, the longest get
-// up to four times their even share.  A part has 128 tokens or more.
-static int most_parts(int64_t sequences, int64_t blocks, int64_t max_length, int *target)
+// Calls of short sequences that do not fill the card: eight waves to a workgroup and no pieces to join, a second launch saved (one sequence of
+// 517 tokens 9.6 us, in pieces 10.5; of 1000 tokens 13.7 and 10.5; of 100, which four waves take in one step, 5.9 and 5.5).
+static bool short_call(int64_t sequences, int64_t blocks, int64_t max_length, int head_dim)
 {
-    *target = 512;
-    if (sequences * blocks >= 2 * *target) return 1;
-    const int64_t even = ceil_div(*target, sequences * blocks), slack = sequences > 1 ? 4 : 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(even * slack, max_length / (TK_WAVES * TK_TILE)));
+    return head_dim <= 128 && max_length > TK_LEAST && max_length <= 640 && sequences * blocks <= 256;
+}
+
+// Pieces of the call's tokens for each of `blocks` head blocks, 0: a sequence is one.  `target` workgroups are wanted.  Two to a compute unit carry the
+// memory's rate and leave the third's place to what is short (64 sequences of 1024 tokens, 128 columns e4m3, 32.4 us, for three 37.6; 64 columns bf16,
+// whose tiles are smaller, 42.6 and 39.8).  From twice that many sequences on they even out by themselves (256 of up to 1024 tokens 49.2 us, in pieces 60.7).
+static int64_t pieces_of(int64_t sequences, int64_t blocks, int64_t max_length, int head_dim, int64_t *target)
+{
+    *target = 256 * (head_dim <= 64 ? 3 : 2);
+    if (max_length <= TK_LEAST || sequences > TK_MOST_PLANNED || sequences * blocks >= 2 * *target) return 0;
+    if (short_call(sequences, blocks, max_length, head_dim)) return 0;
+    return std::min(ceil_div(*target, blocks) + 1, sequences * (max_length / TK_LEAST)) + sequences;
 }
 
 static int64_t head_blocks(int q_heads, int kv_heads) { return kv_heads * ceil_div(q_heads / kv_heads, TK_COLS); }
 
-template <typename T, bool CODES, int DP>
-static void launch_token(const TokenParams &p, bool fast, hipStream_t s)
+template <typename T, bool CODES, int DP, int WAVES>
+static void launch_waves(const TokenParams &p, hipStream_t s)
 {
-    const dim3 grid(p.parts, p.Hkv * p.col_tiles, p.sequences);
-    if (fast && p.D == DP)
-        k_attention_token<T, CODES, DP, true><<<grid, TK_WAVES * 64, 0, s>>>(p);
+    const dim3 grid(p.Hkv * p.col_tiles, p.pieces ? p.pieces : p.sequences);
+    if (p.D == DP)
+        k_attention_token<T, CODES, DP, false, WAVES><<<grid, WAVES * 64, 0, s>>>(p);
     else
-        k_attention_token<T, CODES, DP, false><<<grid, TK_WAVES * 64, 0, s>>>(p);
+        k_attention_token<T, CODES, DP, true, WAVES><<<grid, WAVES * 64, 0, s>>>(p);
+}
+
+template <typename T, bool CODES, int DP>
+static void launch_token(const TokenParams &p, hipStream_t s)
+{
+    if constexpr (DP <= 128) {
+        if (short_call(p.sequences, p.Hkv * p.col_tiles, p.max_length, DP)) return launch_waves<T, CODES, DP, 8>(p, s);
+    }
+    launch_waves<T, CODES, DP, 4>(p, s);
 }
 
 template <typename T>
-static nq_status run_token(const TokenParams &p, bool fast, hipStream_t s)
+static nq_status run_token(const TokenParams &p, hipStream_t s)
 {
     auto by_dim = [&](auto codes) {
         constexpr bool C = decltype(codes)::value;
         if (p.D <= 64)
-            launch_token<T, C, 64>(p, fast, s);
+            launch_token<T, C, 64>(p, s);
         else if (p.D <= 128)
-            launch_token<T, C, 128>(p, fast, s);
+            launch_token<T, C, 128>(p, s);
         else
-            launch_token<T, C, 256>(p, fast, s);
+            launch_token<T, C, 256>(p, s);
     };
     if (p.cache.type == NQ_KV_E4M3)
         by_dim(std::true_type{});
     else
         by_dim(std::false_type{});
     const nq_status st = launch_status();
-    if (st != NQ_OK || p.parts == 1) return st;
-    k_attention_join<T><<<dim3(p.Hq, p.sequences), 256, 0, s>>>(p);
+    if (st != NQ_OK || !p.pieces) return st;
+    // a wave for a head, four where there are few heads and many pieces of them
+    if (p.pieces - p.sequences <= 8 || p.sequences * p.Hq >= 1024)
+        k_attention_join<T, 64><<<dim3((unsigned)ceil_div(p.Hq, 4), p.sequences), 256, 0, s>>>(p);
+    else
+        k_attention_join<T, 256><<<dim3(p.Hq, p.sequences), 256, 0, s>>>(p);
     return launch_status();
 }
 
@@ -427,9 +624,10 @@ extern "C" size_t nq_attention_token_workspace_bytes(int64_t sequences, int32_t 
 {
     if (sequences < 1 || max_length < 1 || sequences > ATT_MAX_ROWS || max_length > INT32_MAX) return 0;
     if (check_heads(q_heads, kv_heads, head_dim) != NQ_OK || q_heads % kv_heads) return 0;
-    int target;
-    const int parts = most_parts(sequences, head_blocks(q_heads, kv_heads), max_length, &target);
-    return parts == 1 ? 0 : (size_t)sequences * q_heads * parts * (head_dim + 4) * sizeof(float);
+    int64_t target;
+    const int64_t blocks = head_blocks(q_heads, kv_heads);
+    const int64_t pieces = pieces_of(sequences, blocks, max_length, head_dim, &target);
+    return (size_t)pieces * q_heads * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" nq_status nq_attention_token(const nq_token_job *job, void *stream)
@@ -470,12 +668,14 @@ extern "C" nq_status nq_attention_token(const nq_token_job *job, void *stream)
     p.col_tiles = (int32_t)ceil_div(p.group, TK_COLS);
     p.D = c.head_dim;
     p.scale = j.scale * TK_LOG2E;
-    p.parts = most_parts(p.sequences, head_blocks(j.q_heads, c.heads), j.max_length, &p.target);
-    if (p.parts > 1) {
+    int64_t target;
+    const int64_t blocks = head_blocks(j.q_heads, c.heads);
+    p.pieces = (int32_t)pieces_of(p.sequences, blocks, j.max_length, c.head_dim, &target);
+    p.share = (float)blocks / (float)target;
+    if (p.pieces) {
         if (!j.d_workspace) return NQ_ERR_INVALID_ARG;
         if (!aligned16(j.d_workspace)) return NQ_ERR_ALIGN;
         if (j.workspace_bytes < nq_attention_token_workspace_bytes(j.sequences, j.q_heads, c.heads, c.head_dim, j.max_length)) return NQ_ERR_RANGE;
     }
-    const bool fast = c.page_tokens % 16 == 0;
-    return j.dtype == NQ_DT_F16 ? run_token<_Float16>(p, fast, (hipStream_t)stream) : run_token<bf16_t>(p, fast, (hipStream_t)stream);
+    return j.dtype == NQ_DT_F16 ? run_token<_Float16>(p, (hipStream_t)stream) : run_token<bf16_t>(p, (hipStream_t)stream);
 }

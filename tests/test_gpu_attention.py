@@ -373,6 +373,11 @@ TOKEN = [  # lengths, longest or None, Hq, Hkv, D, dtype, cache, page, order
     ([50, 513], None, 2, 1, 8, F16, E4M3, 16, "head"),
     ([64] * 130, None, 2, 2, 64, BF16, E4M3, 16, "head"),
     ([128, 2047], None, 9, 3, 248, BF16, BF16, 48, "head"),
+    ([i * 37 % 900 + (1500 if i % 23 == 0 else 0) for i in range(70)], None, 2, 1, 64, BF16, E4M3, 16, "head"),
+    ([i * 53 % 400 for i in range(150)] + [5000] + [i * 31 % 300 for i in range(160)], None, 1, 1, 64, F16, F16, 16, "token"),
+    ([3] * 1030 + [700], None, 1, 1, 16, BF16, E4M3, 16, "head"),
+    ([20000], None, 1, 1, 64, BF16, BF16, 16, "head"),
+    ([640, 500], None, 2, 1, 80, BF16, BF16, 16, "head"),
 ]
 
 
