@@ -81,15 +81,19 @@ constexpr int pitch_of(int DP) { return DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
 // keys of a step: as many as the registers hold beside the outputs
 constexpr int keys_of(int DP) { return DP <= 128 ? 64 : 32; }
 
-template <typename T, int DP, int QT>
+// DIRECT: K and V travel global -> LDS by direct loads, which want rows on 16 bytes; else through registers.
+template <typename T, int DP, int QT, bool DIRECT>
 __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt(const PromptParams p)
 {
-    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP), U = KEYS / 32, KJ = DP / 16, DT = DP / 32, CH = KEYS * DP / 8 / 256, PIECES = DP / 8;
+    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP), U = KEYS / 32, KJ = DP / 16, DT = DP / 32;
     constexpr int ROWS = 128 * QT, TILE = KEYS * PITCH;
+    constexpr int PIECES = DIRECT ? PITCH / 8 : DP / 8, CH = KEYS * PIECES / 256;      // pieces of 16 bytes of a row; of a thread and tile
     constexpr bool F16 = __is_same(T, _Float16);
     constexpr uint32_t EXP = F16 ? 0x7c00 : 0x7f80;                      // the exponent of infinities and NaN
+    constexpr int NOWHERE = 0x7fffffff, RANGE = 0x7ffffff0;
+    typedef __attribute__((address_space(3))) void *lds_ptr;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];     // two stages of K and V
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
 
     // ---- which rows: tile t belongs to the last sequence s with begin / ROWS + s <= t
     const uint32_t order = divide(blockIdx.x, p.by_heads), h = blockIdx.x - order * p.by_heads.d;
@@ -116,35 +120,75 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
         for (int j = 0; j < KJ; ++j) {
             const int d = 16 * j + 8 * half;
             q[a][j] = make_uint4(0, 0, 0, 0);
-            if (row < Lq && d < p.D && !p.zero) {
-                __builtin_memcpy(&q[a][j], static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D + d, 16);
-                q[a][j].x ^= p.flip; q[a][j].y ^= p.flip; q[a][j].z ^= p.flip; q[a][j].w ^= p.flip;
-            }
+            if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[a][j], static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D + d, 16);
         }
+    }
+    if (p.flip) {
+#pragma unroll
+        for (int a = 0; a < QT; ++a)
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) q[a][j] = make_uint4(q[a][j].x ^ p.flip, q[a][j].y ^ p.flip, q[a][j].z ^ p.flip, q[a][j].w ^ p.flip);
     }
 
     const T *k_base = static_cast<const T *>(p.k) + (int64_t)k0 * p.ldk + (int64_t)hk * p.D;
     const T *v_base = static_cast<const T *>(p.v) + (int64_t)k0 * p.ldv + (int64_t)hk * p.D;
-    uint4 ks[CH], vs[CH];
-    auto fetch = [&](int j0) {
+    // ---- a tile's way into LDS
+    uint4 ks[DIRECT ? 1 : CH], vs[DIRECT ? 1 : CH];
+    int k_off[DIRECT ? CH : 1], v_off[DIRECT ? CH : 1];
+    if constexpr (DIRECT) {
+        // a wave's 64 pieces land beside each other: which piece of the row a lane asks for makes the exchange
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int id = i * 256 + threadIdx.x, row = id / PIECES, d = id % PIECES * 8;
-            ks[i] = vs[i] = make_uint4(0, 0, 0, 0);
-            if (j0 + row < end && d < p.D) {
-                __builtin_memcpy(&ks[i], k_base + (int64_t)(j0 + row) * p.ldk + d, 16);
-                __builtin_memcpy(&vs[i], v_base + (int64_t)(j0 + row) * p.ldv + d, 16);
+            const int id = (wave * CH + i) * 64 + lane, row = id / PIECES, piece = id % PIECES;
+            const int kd = k_piece<PITCH>(row, piece) * 8, vd = v_piece<PITCH>(row, piece) * 8;
+            k_off[i] = kd < p.D ? (int)(row * p.ldk + kd) * 2 : NOWHERE;
+            v_off[i] = vd < p.D ? (int)(row * p.ldv + vd) * 2 : NOWHERE;
+        }
+    }
+    auto fetch = [&](int j0, uint16_t *kt) __attribute__((always_inline)) {
+        if constexpr (DIRECT) {
+            uint16_t *vt = kt + TILE;
+            const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(k_base + (int64_t)j0 * p.ldk), 0, RANGE, 0x00020000);
+            const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(v_base + (int64_t)j0 * p.ldv), 0, RANGE, 0x00020000);
+            const int rows = end - j0;                                   // (rows that are not there: zeros)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int row = ((wave * CH + i) * 64 + lane) / PIECES;
+                const int at = rows >= KEYS || row < rows ? k_off[i] : NOWHERE;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_ptr)(kt + (wave * CH + i) * 512), 16, at, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int row = ((wave * CH + i) * 64 + lane) / PIECES;
+                const int at = rows >= KEYS || row < rows ? v_off[i] : NOWHERE;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr)(vt + (wave * CH + i) * 512), 16, at, 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int id = i * 256 + threadIdx.x, row = id / PIECES, d = id % PIECES * 8;
+                ks[i] = vs[i] = make_uint4(0, 0, 0, 0);
+                if (j0 + row < end && d < p.D) {
+                    __builtin_memcpy(&ks[i], k_base + (int64_t)(j0 + row) * p.ldk + d, 16);
+                    __builtin_memcpy(&vs[i], v_base + (int64_t)(j0 + row) * p.ldv + d, 16);
+                }
             }
         }
     };
-    auto put = [&](int stage) {
-        uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+    // the tile for everybody
+    auto arrived = [&](int stage) {
+        if constexpr (DIRECT) {
+            __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));         // all loads, all LDS accesses
+        } else {
+            uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int id = i * 256 + threadIdx.x, row = id / PIECES, piece = id % PIECES;
-            *reinterpret_cast<uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, piece) * 8) = ks[i];
-            *reinterpret_cast<uint4 *>(vt + row * PITCH + v_piece<PITCH>(row, piece) * 8) = vs[i];
+            for (int i = 0; i < CH; ++i) {
+                const int id = i * 256 + threadIdx.x, row = id / PIECES, piece = id % PIECES;
+                *reinterpret_cast<uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, piece) * 8) = ks[i];
+                *reinterpret_cast<uint4 *>(vt + row * PITCH + v_piece<PITCH>(row, piece) * 8) = vs[i];
+            }
         }
+        __syncthreads();
     };
 
     at_f16 o[QT][DT];
@@ -162,35 +206,9 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
     // A key that only some rows see has probability 0 in the others, and 0 times an infinite or NaN value is no 0.  From the first key on
     // that not all rows see, steps with such values take a way of their own.
     const int partial = row0 + 1 + off;
-    auto odd_values = [&] {
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const uint32_t w[4] = {vs[i].x, vs[i].y, vs[i].z, vs[i].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= (w[e] & EXP) == EXP || (w[e] >> 16 & EXP) == EXP;
-        }
-        return odd;
-    };
-    bool odd = false;
-    auto settle = [&](int j0) {                                          // the barrier before the step of j0
-        if (j0 + KEYS > partial)
-            odd = __syncthreads_or(odd_values());
-        else
-            __syncthreads();
-    };
-
-    if (end > 0) {
-        fetch(0);
-        put(0);
-        settle(0);
-    }
-    int stage = 0;
-    for (int j0 = 0; j0 < end; j0 += KEYS, stage ^= 1) {
-        const bool more = j0 + KEYS < end;
-        const bool odd_now = odd;
-        if (more) fetch(j0 + KEYS);
-        uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+    // One step.  The two stages are named apart so that the compiler knows that what is on its way into one does not hold up reading the other.
+    auto step = [&](uint16_t *__restrict kt, uint16_t *__restrict vt, uint16_t *__restrict next, int j0) __attribute__((always_inline)) {
+        if (j0 + KEYS < end) fetch(j0 + KEYS, next);
         // ---- scores: lane (r, half) has row r, keys 32 u + 8 (i / 4) + 4 half + i % 4
         at_f16 s[QT][U];
 #pragma unroll
@@ -207,16 +225,25 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
                 for (int a = 0; a < QT; ++a) s[a][u] = mma32<T>(f, q[a][j], s[a][u]);
             }
         }
+        // (fragments are read AHEAD products before they are used)
+        constexpr int AHEAD = 4;
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < U * KJ - AHEAD; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * QT, 0);
         uint4 pr[QT][2 * U];
 #pragma unroll
         for (int a = 0; a < QT; ++a) {
-            const int row = row0 + (wave * QT + a) * 32 + r, last = min(Lk - 1, row + off);    // the last key that the row sees
+            const int row = row0 + (wave * QT + a) * 32 + r, last = min(Lk - 1, row + off) - j0 - 4 * half;    // the last key that the row sees, from this lane's first on
             if (j0 + KEYS > min(Lk, row0 + (wave * QT + a) * 32 + 1 + off)) {               // (for the tile's first row, and so for all)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (j0 + 32 * u + 8 * (i / 4) + 4 * half + i % 4 > last) s[a][u][i] = -__builtin_inff();
+                        if (32 * u + 8 * (i / 4) + i % 4 > last) s[a][u][i] = -__builtin_inff();
             }
             float top = s[a][0][0];
 #pragma unroll
@@ -252,7 +279,17 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
                                       pair16<T>(s[a][e / 2][8 * (e & 1) + 4], s[a][e / 2][8 * (e & 1) + 5]),
                                       pair16<T>(s[a][e / 2][8 * (e & 1) + 6], s[a][e / 2][8 * (e & 1) + 7]));
         }
-        if (odd_now) {
+        bool odd = false;
+        if (j0 + KEYS > partial) {
+            for (int i = threadIdx.x * 8; i < TILE; i += 2048) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(vt + i);
+                const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) odd |= (e[x] & EXP) == EXP || (e[x] >> 16 & EXP) == EXP;
+            }
+            odd = __syncthreads_or(odd);
+        }
+        if (odd) {
             // p v = v for such a value in a row that sees it (p > 0), so it is added as it is, and is 0 in the product
             for (int j = 0; j < KEYS; ++j)
 #pragma unroll
@@ -282,10 +319,18 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
 #pragma unroll
                 for (int c = 0; c < QT; ++c) o[c][d] = mma32<T>(f, pr[c][e], o[c][d]);
             }
-        if (more) {
-            put(stage ^ 1);
-            settle(j0 + KEYS);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < DT * 2 * U - AHEAD; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * QT, 0);
+    };
+    if (end > 0) fetch(0, lds);
+    for (int j0 = 0, stage = 0; j0 < end; j0 += KEYS, stage ^= 1) {
+        arrived(stage);                                                  // (and nobody reads the other stage any more)
+        step(lds + stage * 2 * TILE, lds + stage * 2 * TILE + TILE, lds + (stage ^ 1) * 2 * TILE, j0);
     }
 
     // ---- lane: row r, columns 32 d + 8 (i / 4) + 4 half + i % 4
@@ -311,26 +356,28 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
 // ---- host ------------------------------------------------------------------------------------------------------
 
 template <typename T, int DP, int QT>
-static nq_status launch_prompt(PromptParams &p, hipStream_t s)
+static nq_status launch_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
     constexpr int BYTES = 4 * keys_of(DP) * pitch_of(DP) * 2;
-    auto kernel = k_attention_prompt<T, DP, QT>;
-    static std::atomic<uint64_t> granted{0};
-    const nq_status st = grant_lds(kernel, BYTES, granted);
-    if (st != NQ_OK) return st;
     p.tiles = p.q_rows / (128 * QT) + p.sequences;
-    kernel<<<(unsigned)p.tiles * (unsigned)p.Hq, 256, BYTES, s>>>(p);
-    return launch_status();
+    auto launch = [&](auto kernel, std::atomic<uint64_t> &granted) {
+        const nq_status st = grant_lds(kernel, BYTES, granted);
+        if (st != NQ_OK) return st;
+        kernel<<<(unsigned)p.tiles * (unsigned)p.Hq, 256, BYTES, s>>>(p);
+        return launch_status();
+    };
+    static std::atomic<uint64_t> granted[2] = {};
+    return direct ? launch(k_attention_prompt<T, DP, QT, true>, granted[1]) : launch(k_attention_prompt<T, DP, QT, false>, granted[0]);
 }
 
 template <typename T>
-static nq_status run_prompt(PromptParams &p, hipStream_t s)
+static nq_status run_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
-    if (p.D <= 64) return launch_prompt<T, 64, 1>(p, s);
-    if (p.D <= 96) return launch_prompt<T, 96, 1>(p, s);
-    if (p.D <= 128) return launch_prompt<T, 128, 1>(p, s);
-    if (p.D <= 192) return launch_prompt<T, 192, 1>(p, s);
-    return launch_prompt<T, 256, 1>(p, s);
+    if (p.D <= 64) return launch_prompt<T, 64, 1>(p, direct, s);
+    if (p.D <= 96) return launch_prompt<T, 96, 1>(p, direct, s);
+    if (p.D <= 128) return launch_prompt<T, 128, 1>(p, direct, s);
+    if (p.D <= 192) return launch_prompt<T, 192, 1>(p, direct, s);
+    return launch_prompt<T, 256, 1>(p, direct, s);
 }
 
 }  // namespace nq
@@ -381,5 +428,7 @@ extern "C" nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream)
     p.scale = j.scale == 0.0f ? 1.0f : j.scale < 0.0f ? -j.scale * PR_LOG2E : j.scale * PR_LOG2E;
     p.flip = j.scale < 0.0f ? 0x80008000u : 0u;
     p.zero = j.scale == 0.0f;
-    return j.dtype == NQ_DT_F16 ? run_prompt<_Float16>(p, (hipStream_t)stream) : run_prompt<bf16_t>(p, (hipStream_t)stream);
+    // rows on 16 bytes, a tile's offsets within 31 bits
+    const bool direct = aligned16(j.d_k) && aligned16(j.d_v) && j.ldk % 8 == 0 && j.ldv % 8 == 0 && std::max(j.ldk, j.ldv) < (int64_t(1) << 23);
+    return j.dtype == NQ_DT_F16 ? run_prompt<_Float16>(p, direct, (hipStream_t)stream) : run_prompt<bf16_t>(p, direct, (hipStream_t)stream);
 }
