@@ -26,6 +26,19 @@ __device__ __forceinline__ Place place_of(const CacheView &c, int64_t slot)
     return Place{page, slot - page * c.by_page.d};
 }
 
+// Sum over the lanes before this one, and over all.
+__device__ __forceinline__ int before(int v, int *all)
+{
+    int x = v;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // one, two, four and eight lanes on in the row of sixteen
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the row before's last to the second and fourth row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // the half's last to the other half
+    *all = __builtin_amdgcn_readlane(x, 63);
+    return x - v;
+}
 // ---- host ------------------------------------------------------------------------------------------------------
 
 // (a row of heads of floats is at most 2^32 elements away from the next, as check_matrix has it)

@@ -15,6 +15,7 @@ typedef __bf16 at_b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 at_h2 __attribute__((ext_vector_type(2)));
 typedef float at_f16 __attribute__((ext_vector_type(16)));
 typedef short at_s4 __attribute__((ext_vector_type(4)));
+typedef short at_s2 __attribute__((ext_vector_type(2)));
 
 constexpr float PR_LOG2E = 1.44269504088896340736f;
 // A row's maximum is moved only when a score passes it by this much (in powers of two): the probabilities are relative to it, so
@@ -26,7 +27,7 @@ struct PromptParams {
     void *o;
     const int32_t *q_begin, *k_begin;
     int64_t ldq, ldk, ldv, ldo;
-    int32_t sequences, q_rows, k_rows, Hq, Hkv, group, D, causal, tiles;
+    int32_t sequences, q_rows, k_rows, Hq, Hkv, group, D, causal, tiles;   // tiles: of rows, at most
     Divider by_heads;
     float scale;                                // times log2(e), its magnitude
     uint32_t flip;                              // sign bits for q where the scale is negative
@@ -57,6 +58,14 @@ __device__ __forceinline__ float value16(uint16_t v)
     else
         return __builtin_bit_cast(float, (uint32_t)v << 16);
 }
+template <typename T>
+__device__ __forceinline__ float sum_pair(uint32_t p, float sum)
+{
+    if constexpr (__is_same(T, _Float16))
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(at_h2, p), at_h2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+    else
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(at_s2, p), __builtin_bit_cast(at_s2, 0x3f803f80u), sum, false);
+}
 __device__ __forceinline__ float across32(float v, bool sum)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
@@ -81,9 +90,92 @@ constexpr int pitch_of(int DP) { return DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
 // keys of a step: as many as the registers hold beside the outputs
 constexpr int keys_of(int DP) { return DP <= 128 ? 64 : 32; }
 
-// DIRECT: K and V travel global -> LDS by direct loads, which want rows on 16 bytes; else through registers.
+// Which rows a workgroup takes: number w in the order of the keys that they see, the most first (in steps of PR_LEVEL keys), so that what
+// is left for the end is short.  For up to PR_PLANNED sequences, a lane each of 64; every wave makes the same sums.
+constexpr int PR_LEVEL = 256, PR_PLANNED = 256;
+struct Rows {
+    int sequence, tile;                          // -1: none
+};
+template <int ROWS>
+__device__ __forceinline__ Rows rows_of(const PromptParams &p, int w)
+{
+    const int lane = threadIdx.x & 63;
+    if (p.sequences > PR_PLANNED) {
+        // in the order of the sequences from the last on: tile t belongs to the last sequence s with begin / ROWS + s <= t
+        const int t = p.tiles - 1 - w;
+        int lo = -1, hi = p.sequences;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)(p.q_begin[mid] / ROWS) + mid <= t) lo = mid; else hi = mid;
+        }
+        return lo < 0 ? Rows{-1, 0} : Rows{lo, t - (p.q_begin[lo] / ROWS + lo)};
+    }
+    if (p.sequences == 1) {
+        const int q0 = min(max(p.q_begin[0], 0), p.q_rows), n = (min(max(p.q_begin[1], q0), p.q_rows) - q0 + ROWS - 1) / ROWS;
+        return Rows{w < n ? 0 : -1, n - 1 - w};
+    }
+    constexpr int CH = PR_PLANNED / 64;
+    int tiles[CH], keys[CH], ahead[CH], most = 0, total = 0, all;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int i = 64 * c + lane;
+        tiles[c] = keys[c] = ahead[c] = 0;
+        if (i < p.sequences) {
+            const int q0 = min(max(p.q_begin[i], 0), p.q_rows), Lq = min(max(p.q_begin[i + 1], q0), p.q_rows) - q0;
+            const int k0 = min(max(p.k_begin[i], 0), p.k_rows);
+            keys[c] = min(max(p.k_begin[i + 1], k0), p.k_rows) - k0;
+            tiles[c] = (Lq + ROWS - 1) / ROWS;
+            ahead[c] = keys[c] - Lq;
+        }
+        total += tiles[c];
+        most = max(most, keys[c]);
+    }
+    (void)before(total, &all);
+    if (w >= all) return Rows{-1, 0};
+    // tiles of a sequence that see more than (x - 1) * PR_LEVEL keys, the last ones of it
+    auto count = [&](int c, int x) {
+        if (x == 0) return tiles[c];
+        const int y = (x - 1) * PR_LEVEL + 1;
+        if (keys[c] < y) return 0;
+        return p.causal ? min(tiles[c], tiles[c] - (max(y - ahead[c], 1) + ROWS - 1) / ROWS + 1) : tiles[c];
+    };
+    auto sum = [&](int x) {
+        int n = 0, s;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (64 * c < p.sequences) n += count(c, x);
+        (void)before(n, &s);
+        return s;
+    };
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) most = max(most, __shfl_xor(most, k));
+    int x = 0, hi = __builtin_amdgcn_readfirstlane(most) / PR_LEVEL + 2, more = 0;    // sum(x) > w >= sum(hi) == more
+    while (hi - x > 1) {
+        const int mid = (x + hi) >> 1, s = sum(mid);
+        if (s > w) {
+            x = mid;
+        } else {
+            hi = mid;
+            more = s;
+        }
+    }
+    int at = w - more;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int upper = 64 * c < p.sequences ? count(c, x + 1) : 0, here = 64 * c < p.sequences ? count(c, x) - upper : 0, first = before(here, &all);
+        const uint64_t mask = __ballot(at >= first && at < first + here);
+        if (mask) {
+            const int from = __builtin_ctzll(mask);
+            return Rows{64 * c + from, __builtin_amdgcn_readlane(tiles[c] - upper - here + at - first, from)};
+        }
+        at -= all;
+    }
+    return Rows{-1, 0};
+}
+
+// DIRECT: K and V travel global -> LDS by direct loads a step ahead, which want rows on 16 bytes; else through registers, when they are used.
 template <typename T, int DP, int QT, bool DIRECT>
-__global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt(const PromptParams p)
+__global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_attention_prompt(const PromptParams p)
 {
     constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP), U = KEYS / 32, KJ = DP / 16, DT = DP / 32;
     constexpr int ROWS = 128 * QT, TILE = KEYS * PITCH;
@@ -95,16 +187,13 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];     // two stages of K and V
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
 
-    // ---- which rows: tile t belongs to the last sequence s with begin / ROWS + s <= t
-    const uint32_t order = divide(blockIdx.x, p.by_heads), h = blockIdx.x - order * p.by_heads.d;
-    const int t = p.tiles - 1 - (int)order;                              // (the rows with the most keys first)
-    int lo = -1, hi = p.sequences;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((int64_t)(p.q_begin[mid] / ROWS) + mid <= t) lo = mid; else hi = mid;
-    }
-    if (lo < 0) return;
-    const int first = t - (p.q_begin[lo] / ROWS + lo);
+    // Neighbouring workgroups take the heads in turn, those of one key head on one of the eight dies, whose cache then holds its keys.
+    const uint32_t w = divide(blockIdx.x, p.by_heads);
+    uint32_t h = blockIdx.x - w * p.by_heads.d;
+    if (p.Hq % 8 == 0) h = (h & 7) * (p.Hq >> 3) + (h >> 3);
+    const Rows mine = rows_of<ROWS>(p, (int)w);
+    if (mine.sequence < 0) return;
+    const int lo = mine.sequence, first = mine.tile;
     const int q0 = min(max(p.q_begin[lo], 0), p.q_rows), q1 = min(max(p.q_begin[lo + 1], q0), p.q_rows), Lq = q1 - q0;
     const int k0 = min(max(p.k_begin[lo], 0), p.k_rows), k1 = min(max(p.k_begin[lo + 1], k0), p.k_rows), Lk = k1 - k0;
     if (first < 0 || (int64_t)first * ROWS >= Lq) return;
@@ -112,28 +201,9 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
     const int end = min(Lk, max(0, min(row0 + ROWS, Lq) + off));         // keys that any row sees
     const int hk = (int)h / p.group;
 
-    uint4 q[QT][KJ];
-#pragma unroll
-    for (int a = 0; a < QT; ++a) {
-        const int row = row0 + (wave * QT + a) * 32 + r;
-#pragma unroll
-        for (int j = 0; j < KJ; ++j) {
-            const int d = 16 * j + 8 * half;
-            q[a][j] = make_uint4(0, 0, 0, 0);
-            if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[a][j], static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D + d, 16);
-        }
-    }
-    if (p.flip) {
-#pragma unroll
-        for (int a = 0; a < QT; ++a)
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) q[a][j] = make_uint4(q[a][j].x ^ p.flip, q[a][j].y ^ p.flip, q[a][j].z ^ p.flip, q[a][j].w ^ p.flip);
-    }
-
     const T *k_base = static_cast<const T *>(p.k) + (int64_t)k0 * p.ldk + (int64_t)hk * p.D;
     const T *v_base = static_cast<const T *>(p.v) + (int64_t)k0 * p.ldv + (int64_t)hk * p.D;
     // ---- a tile's way into LDS
-    uint4 ks[DIRECT ? 1 : CH], vs[DIRECT ? 1 : CH];
     int k_off[DIRECT ? CH : 1], v_off[DIRECT ? CH : 1];
     if constexpr (DIRECT) {
         // a wave's 64 pieces land beside each other: which piece of the row a lane asks for makes the exchange
@@ -163,33 +233,75 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
                 const int at = rows >= KEYS || row < rows ? v_off[i] : NOWHERE;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr)(vt + (wave * CH + i) * 512), 16, at, 0, 0, 0);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const int id = i * 256 + threadIdx.x, row = id / PIECES, d = id % PIECES * 8;
-                ks[i] = vs[i] = make_uint4(0, 0, 0, 0);
-                if (j0 + row < end && d < p.D) {
-                    __builtin_memcpy(&ks[i], k_base + (int64_t)(j0 + row) * p.ldk + d, 16);
-                    __builtin_memcpy(&vs[i], v_base + (int64_t)(j0 + row) * p.ldv + d, 16);
-                }
-            }
         }
     };
-    // the tile for everybody
-    auto arrived = [&](int stage) {
+    // A key that only some rows see has probability 0 in the others, and 0 times an infinite or NaN value is no 0.  So such values become zeros
+    // in the tiles of those keys, and are added at the end to the rows that see them.
+    const int partial = row0 + 1 + off;                                  // keys that all rows see
+    uint32_t *const odd_of = reinterpret_cast<uint32_t *>(lds + 4 * TILE);    // for each wave: whether it found such values
+    if (lane == 0) odd_of[wave] = 0;
+    auto tame = [&](uint4 &w) __attribute__((always_inline)) {
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        uint32_t found = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) found |= (x[i] & (EXP << 16 | EXP)) + ((EXP & -EXP) << 16 | (EXP & -EXP));     // (a carry out of an exponent of ones)
+        if (!(found & 0x80008000u)) return false;
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = ((x[i] & EXP) == EXP ? 0u : x[i] & 0xffffu) | ((x[i] >> 16 & EXP) == EXP ? 0u : x[i] & 0xffff0000u);
+        w = make_uint4(y[0], y[1], y[2], y[3]);
+        odd_of[wave] = 1;
+        return true;
+    };
+    // the tile of the keys from j0 on for everybody
+    auto arrived = [&](int stage, int j0) __attribute__((always_inline)) {
+        uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
         if constexpr (DIRECT) {
             __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));         // all loads, all LDS accesses
+            if (j0 + KEYS > partial) {
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {                           // (what this lane has asked for)
+                    uint4 *at = reinterpret_cast<uint4 *>(vt + (wave * CH + i) * 512 + lane * 8), w = *at;
+                    if (tame(w)) *at = w;
+                }
+            }
         } else {
-            uint16_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int id = i * 256 + threadIdx.x, row = id / PIECES, piece = id % PIECES;
-                *reinterpret_cast<uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, piece) * 8) = ks[i];
-                *reinterpret_cast<uint4 *>(vt + row * PITCH + v_piece<PITCH>(row, piece) * 8) = vs[i];
+                const int id = i * 256 + threadIdx.x, row = id / PIECES, piece = id % PIECES, d = piece * 8;
+                uint4 k = make_uint4(0, 0, 0, 0), v = make_uint4(0, 0, 0, 0);
+                if (j0 + row < end && d < p.D) {
+                    __builtin_memcpy(&k, k_base + (int64_t)(j0 + row) * p.ldk + d, 16);
+                    __builtin_memcpy(&v, v_base + (int64_t)(j0 + row) * p.ldv + d, 16);
+                }
+                if (j0 + KEYS > partial) (void)tame(v);
+                *reinterpret_cast<uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, piece) * 8) = k;
+                *reinterpret_cast<uint4 *>(vt + row * PITCH + v_piece<PITCH>(row, piece) * 8) = v;
             }
         }
         __syncthreads();
     };
+
+    if (end > 0) fetch(0, lds);
+    uint4 q[QT][KJ];
+#pragma unroll
+    for (int a = 0; a < QT; ++a) {
+        const int row = row0 + (wave * QT + a) * 32 + r;
+        const T *q_row = static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D;
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) {
+            const int d = 16 * j + 8 * half;
+            q[a][j] = make_uint4(0, 0, 0, 0);
+            if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[a][j], q_row + d, 16);
+        }
+    }
+    if (p.flip) {
+#pragma unroll
+        for (int a = 0; a < QT; ++a)
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) q[a][j] = make_uint4(q[a][j].x ^ p.flip, q[a][j].y ^ p.flip, q[a][j].z ^ p.flip, q[a][j].w ^ p.flip);
+    }
 
     at_f16 o[QT][DT];
     float m[QT], l[QT];
@@ -203,12 +315,20 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
         l[a] = 0.0f;
     }
 
-    // A key that only some rows see has probability 0 in the others, and 0 times an infinite or NaN value is no 0.  From the first key on
-    // that not all rows see, steps with such values take a way of their own.
-    const int partial = row0 + 1 + off;
+    // keys that some row of the wave sees, that all of them see
+    const int first_row = row0 + wave * QT * 32, wave_end = first_row < Lq ? min(Lk, max(0, min(first_row + QT * 32, Lq) + off)) : 0;
+    const int seen_by_all = min(Lk, first_row + 1 + off);
+    // V^T of the columns 32 d .., keys 16 e + 4 half + (0 .. 3) and eight further on, as the scores lie
+    auto v_fragment = [&](const uint16_t *vt, int d, int e) __attribute__((always_inline)) {
+        const int at = 16 * e + 4 * half + (lane & 15) / 4, col = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        const uint2 x = read_transposed(vt + at * PITCH + v_piece<PITCH>(at, col >> 3) * 8 + (col & 7));
+        const uint2 y = read_transposed(vt + (at + 8) * PITCH + v_piece<PITCH>(at + 8, col >> 3) * 8 + (col & 7));
+        return make_uint4(x.x, x.y, y.x, y.y);
+    };
     // One step.  The two stages are named apart so that the compiler knows that what is on its way into one does not hold up reading the other.
     auto step = [&](uint16_t *__restrict kt, uint16_t *__restrict vt, uint16_t *__restrict next, int j0) __attribute__((always_inline)) {
         if (j0 + KEYS < end) fetch(j0 + KEYS, next);
+        if (j0 >= wave_end) return;
         // ---- scores: lane (r, half) has row r, keys 32 u + 8 (i / 4) + 4 half + i % 4
         at_f16 s[QT][U];
 #pragma unroll
@@ -238,7 +358,7 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
 #pragma unroll
         for (int a = 0; a < QT; ++a) {
             const int row = row0 + (wave * QT + a) * 32 + r, last = min(Lk - 1, row + off) - j0 - 4 * half;    // the last key that the row sees, from this lane's first on
-            if (j0 + KEYS > min(Lk, row0 + (wave * QT + a) * 32 + 1 + off)) {               // (for the tile's first row, and so for all)
+            if (j0 + KEYS > seen_by_all) {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -263,59 +383,26 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
             }
             // (f16 probabilities are 2^7 times as large, 2^15 at most, so that small ones keep their bits)
             const float base = m[a] == -__builtin_inff() ? 0.0f : m[a] - (F16 ? 7.0f : 0.0f);
-            float sum = 0.0f;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[a][u][i] = __builtin_amdgcn_exp2f(fmaf(s[a][u][i], p.scale, -base));
-                    sum += s[a][u][i];
-                }
-            l[a] += sum;
+                for (int i = 0; i < 16; ++i) s[a][u][i] = __builtin_amdgcn_exp2f(fmaf(s[a][u][i], p.scale, -base));
 #pragma unroll
             for (int e = 0; e < 2 * U; ++e)
                 pr[a][e] = make_uint4(pair16<T>(s[a][e / 2][8 * (e & 1)], s[a][e / 2][8 * (e & 1) + 1]),
                                       pair16<T>(s[a][e / 2][8 * (e & 1) + 2], s[a][e / 2][8 * (e & 1) + 3]),
                                       pair16<T>(s[a][e / 2][8 * (e & 1) + 4], s[a][e / 2][8 * (e & 1) + 5]),
                                       pair16<T>(s[a][e / 2][8 * (e & 1) + 6], s[a][e / 2][8 * (e & 1) + 7]));
+            // (the sum of what the second product takes, so that the weights add up to 1)
+#pragma unroll
+            for (int e = 0; e < 2 * U; ++e) l[a] = sum_pair<T>(pr[a][e].w, sum_pair<T>(pr[a][e].z, sum_pair<T>(pr[a][e].y, sum_pair<T>(pr[a][e].x, l[a]))));
         }
-        bool odd = false;
-        if (j0 + KEYS > partial) {
-            for (int i = threadIdx.x * 8; i < TILE; i += 2048) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(vt + i);
-                const uint32_t e[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int x = 0; x < 4; ++x) odd |= (e[x] & EXP) == EXP || (e[x] >> 16 & EXP) == EXP;
-            }
-            odd = __syncthreads_or(odd);
-        }
-        if (odd) {
-            // p v = v for such a value in a row that sees it (p > 0), so it is added as it is, and is 0 in the product
-            for (int j = 0; j < KEYS; ++j)
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int col = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
-                        const uint16_t v = vt[j * PITCH + v_piece<PITCH>(j, col >> 3) * 8 + (col & 7)];
-#pragma unroll
-                        for (int a = 0; a < QT; ++a)
-                            if ((v & EXP) == EXP && j0 + j < Lk && j0 + j <= row0 + (wave * QT + a) * 32 + r + off) o[a][d][i] += value16<T>(v);
-                    }
-            __syncthreads();
-            for (int i = threadIdx.x; i < TILE; i += 256)
-                if ((vt[i] & EXP) == EXP) vt[i] = 0;
-            __syncthreads();
-        }
-        // ---- V^T P^T: keys 16 e + 4 half + (0 .. 3) and eight further on, as the scores lie
+        // ---- V^T P^T
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int e = 0; e < 2 * U; ++e) {
-                const int row = 16 * e + 4 * half + (lane & 15) / 4, col = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-                const uint2 a = read_transposed(vt + row * PITCH + v_piece<PITCH>(row, col >> 3) * 8 + (col & 7));
-                const uint2 b = read_transposed(vt + (row + 8) * PITCH + v_piece<PITCH>(row + 8, col >> 3) * 8 + (col & 7));
-                const uint4 f = make_uint4(a.x, a.y, b.x, b.y);
+                const uint4 f = v_fragment(vt, d, e);
 #pragma unroll
                 for (int c = 0; c < QT; ++c) o[c][d] = mma32<T>(f, pr[c][e], o[c][d]);
             }
@@ -327,10 +414,26 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
         }
         __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * QT, 0);
     };
-    if (end > 0) fetch(0, lds);
     for (int j0 = 0, stage = 0; j0 < end; j0 += KEYS, stage ^= 1) {
-        arrived(stage);                                                  // (and nobody reads the other stage any more)
+        arrived(stage, j0);                                              // (and nobody reads the other stage any more)
         step(lds + stage * 2 * TILE, lds + stage * 2 * TILE + TILE, lds + (stage ^ 1) * 2 * TILE, j0);
+    }
+
+    if (end > 0 && end > partial && (odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3])) {
+        for (int j = max(partial, 0) / KEYS * KEYS; j < end; ++j) {
+            const uint16_t *values = reinterpret_cast<const uint16_t *>(v_base + (int64_t)j * p.ldv);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                    const int col = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+                    const uint16_t v = col < p.D ? values[col] : 0;
+#pragma unroll
+                    for (int a = 0; a < QT; ++a)
+                        if ((v & EXP) == EXP && j <= min(Lk - 1, row0 + (wave * QT + a) * 32 + r + off)) o[a][d][i] += value16<T>(v);
+                }
+        }
     }
 
     // ---- lane: row r, columns 32 d + 8 (i / 4) + 4 half + i % 4
@@ -358,7 +461,7 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : 2) k_attention_prompt
 template <typename T, int DP, int QT>
 static nq_status launch_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
-    constexpr int BYTES = 4 * keys_of(DP) * pitch_of(DP) * 2;
+    constexpr int BYTES = 4 * keys_of(DP) * pitch_of(DP) * 2 + 16;
     p.tiles = p.q_rows / (128 * QT) + p.sequences;
     auto launch = [&](auto kernel, std::atomic<uint64_t> &granted) {
         const nq_status st = grant_lds(kernel, BYTES, granted);

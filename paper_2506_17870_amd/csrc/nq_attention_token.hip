@@ -76,19 +76,6 @@ __device__ __forceinline__ int chunk_of(const TokenParams &p, Lengths &lengths)
     const float even = fminf(ceilf(sum64(total) * p.share), 2147483520.0f);
     return __builtin_amdgcn_readfirstlane((max((int)even, TK_LEAST) + TK_TILE - 1) / TK_TILE * TK_TILE);
 }
-// Sum over the lanes before this one.
-__device__ __forceinline__ int before(int v, int *all)
-{
-    int x = v;
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // one, two, four and eight lanes on in the row of sixteen
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the row before's last to the second and fourth row
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // the half's last to the other half
-    *all = __builtin_amdgcn_readlane(x, 63);
-    return x - v;
-}
 struct Pieces {
     int first, count, size;               // numbers of a sequence's pieces, tokens of one
 };
