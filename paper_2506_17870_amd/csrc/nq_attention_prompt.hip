@@ -82,17 +82,18 @@ __device__ __forceinline__ uint2 read_transposed(const uint16_t *at)
 // LDS rows of PITCH elements in pieces of 16 bytes, exchanged so that neither the rows that a wave reads at once nor the four rows of a
 // transposing read meet in a bank.
 template <int PITCH>
-__device__ __forceinline__ int k_piece(int row, int piece) { return piece ^ (PITCH == 64 ? (row ^ (row >> 3)) & 7 : row & 15); }
+__device__ __forceinline__ int k_piece(int row, int piece) { return piece ^ (PITCH == 64 ? (row ^ (row >> 3 & 3)) & 7 : row & 15); }
 template <int PITCH>
 __device__ __forceinline__ int v_piece(int row, int piece) { return piece ^ (PITCH == 64 ? (row & 2) << 1 : ((row & 3) << 2) | ((row >> 2) & 3)); }
 
 constexpr int pitch_of(int DP) { return DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
 // keys of a step: as many as the registers hold beside the outputs
-constexpr int keys_of(int DP) { return DP <= 128 ? 64 : 32; }
+constexpr int stages_of(int DP, bool split) { return split && DP > 64 ? 1 : 2; }
+constexpr int keys_of(int DP, bool split) { return split ? 128 : DP <= 128 ? 64 : 32; }
 
 // Which rows a workgroup takes: number w in the order of the keys that they see, the most first (in steps of PR_LEVEL keys), so that what
 // is left for the end is short.  For up to PR_PLANNED sequences, a lane each of 64; every wave makes the same sums.
-constexpr int PR_LEVEL = 256, PR_PLANNED = 256;
+constexpr int PR_LEVEL = 512, PR_PLANNED = 256;
 struct Rows {
     int sequence, tile;                          // -1: none
 };
@@ -174,12 +175,13 @@ __device__ __forceinline__ Rows rows_of(const PromptParams &p, int w)
 }
 
 // DIRECT: K and V travel global -> LDS by direct loads a step ahead, which want rows on 16 bytes; else through registers, when they are used.
-template <typename T, int DP, int QT, bool DIRECT>
-__global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_attention_prompt(const PromptParams p)
+template <typename T, int DP, bool SPLIT, bool DIRECT>
+__global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 3) k_attention_prompt(const PromptParams p)
 {
-    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP), U = KEYS / 32, KJ = DP / 16, DT = DP / 32;
-    constexpr int ROWS = 128 * QT, TILE = KEYS * PITCH;
+    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP, SPLIT), STAGES = stages_of(DP, SPLIT), U = SPLIT ? 1 : KEYS / 32, KJ = DP / 16, DT = DP / 32;
+    constexpr int ROWS = SPLIT ? 32 : 128, TILE = KEYS * PITCH;
     constexpr int PIECES = DIRECT ? PITCH / 8 : DP / 8, CH = KEYS * PIECES / 256;      // pieces of 16 bytes of a row; of a thread and tile
+    constexpr int SUMS = SPLIT ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;    // bytes for the waves' sums
     constexpr bool F16 = __is_same(T, _Float16);
     constexpr uint32_t EXP = F16 ? 0x7c00 : 0x7f80;                      // the exponent of infinities and NaN
     constexpr int NOWHERE = 0x7fffffff, RANGE = 0x7ffffff0;
@@ -188,10 +190,10 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_at
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
 
     // Neighbouring workgroups take the heads in turn, those of one key head on one of the eight dies, whose cache then holds its keys.
-    const uint32_t w = divide(blockIdx.x, p.by_heads);
-    uint32_t h = blockIdx.x - w * p.by_heads.d;
+    const uint32_t number = divide(blockIdx.x, p.by_heads);
+    uint32_t h = blockIdx.x - number * p.by_heads.d;
     if (p.Hq % 8 == 0) h = (h & 7) * (p.Hq >> 3) + (h >> 3);
-    const Rows mine = rows_of<ROWS>(p, (int)w);
+    const Rows mine = rows_of<ROWS>(p, (int)number);
     if (mine.sequence < 0) return;
     const int lo = mine.sequence, first = mine.tile;
     const int q0 = min(max(p.q_begin[lo], 0), p.q_rows), q1 = min(max(p.q_begin[lo + 1], q0), p.q_rows), Lq = q1 - q0;
@@ -238,7 +240,7 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_at
     // A key that only some rows see has probability 0 in the others, and 0 times an infinite or NaN value is no 0.  So such values become zeros
     // in the tiles of those keys, and are added at the end to the rows that see them.
     const int partial = row0 + 1 + off;                                  // keys that all rows see
-    uint32_t *const odd_of = reinterpret_cast<uint32_t *>(lds + 4 * TILE);    // for each wave: whether it found such values
+    uint32_t *const odd_of = reinterpret_cast<uint32_t *>(lds + (STAGES * 2 * TILE > SUMS / 2 ? STAGES * 2 * TILE : SUMS / 2));    // for each wave: whether it found such values
     if (lane == 0) odd_of[wave] = 0;
     auto tame = [&](uint4 &w) __attribute__((always_inline)) {
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
@@ -284,40 +286,31 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_at
     };
 
     if (end > 0) fetch(0, lds);
-    uint4 q[QT][KJ];
+    // this wave's rows, this lane's row
+    const int first_row = row0 + (SPLIT ? 0 : wave * 32), row = first_row + r;
+    uint4 q[KJ];
+    const T *q_row = static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D;
 #pragma unroll
-    for (int a = 0; a < QT; ++a) {
-        const int row = row0 + (wave * QT + a) * 32 + r;
-        const T *q_row = static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D;
-#pragma unroll
-        for (int j = 0; j < KJ; ++j) {
-            const int d = 16 * j + 8 * half;
-            q[a][j] = make_uint4(0, 0, 0, 0);
-            if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[a][j], q_row + d, 16);
-        }
+    for (int j = 0; j < KJ; ++j) {
+        const int d = 16 * j + 8 * half;
+        q[j] = make_uint4(0, 0, 0, 0);
+        if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[j], q_row + d, 16);
     }
     if (p.flip) {
 #pragma unroll
-        for (int a = 0; a < QT; ++a)
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) q[a][j] = make_uint4(q[a][j].x ^ p.flip, q[a][j].y ^ p.flip, q[a][j].z ^ p.flip, q[a][j].w ^ p.flip);
+        for (int j = 0; j < KJ; ++j) q[j] = make_uint4(q[j].x ^ p.flip, q[j].y ^ p.flip, q[j].z ^ p.flip, q[j].w ^ p.flip);
     }
 
-    at_f16 o[QT][DT];
-    float m[QT], l[QT];
+    at_f16 o[DT];
+    float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-    for (int a = 0; a < QT; ++a) {
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[a][d][i] = 0.0f;
-        m[a] = -__builtin_inff();
-        l[a] = 0.0f;
-    }
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
 
-    // keys that some row of the wave sees, that all of them see
-    const int first_row = row0 + wave * QT * 32, wave_end = first_row < Lq ? min(Lk, max(0, min(first_row + QT * 32, Lq) + off)) : 0;
-    const int seen_by_all = min(Lk, first_row + 1 + off);
+    // keys that some row of the wave sees, that all of them see; the last that this lane's row sees
+    const int wave_end = first_row < Lq ? min(Lk, max(0, min(first_row + 32, Lq) + off)) : 0, seen_by_all = min(Lk, first_row + 1 + off);
+    const int row_last = min(Lk - 1, row + off);
     // V^T of the columns 32 d .., keys 16 e + 4 half + (0 .. 3) and eight further on, as the scores lie
     auto v_fragment = [&](const uint16_t *vt, int d, int e) __attribute__((always_inline)) {
         const int at = 16 * e + 4 * half + (lane & 15) / 4, col = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
@@ -325,24 +318,26 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_at
         const uint2 y = read_transposed(vt + (at + 8) * PITCH + v_piece<PITCH>(at + 8, col >> 3) * 8 + (col & 7));
         return make_uint4(x.x, x.y, y.x, y.y);
     };
-    // One step.  The two stages are named apart so that the compiler knows that what is on its way into one does not hold up reading the other.
+    // One step: the keys from j0 on, whose tiles are kt and vt.  The two stages are named apart so that the compiler knows that what is on its
+    // way into one does not hold up reading the other.
     auto step = [&](uint16_t *__restrict kt, uint16_t *__restrict vt, uint16_t *__restrict next, int j0) __attribute__((always_inline)) {
-        if (j0 + KEYS < end) fetch(j0 + KEYS, next);
+        if (STAGES == 2 && j0 + KEYS < end) fetch(j0 + KEYS, next);
+        if constexpr (SPLIT) {
+            j0 += wave * 32;
+            kt += wave * 32 * PITCH;
+            vt += wave * 32 * PITCH;
+        }
         if (j0 >= wave_end) return;
         // ---- scores: lane (r, half) has row r, keys 32 u + 8 (i / 4) + 4 half + i % 4
-        at_f16 s[QT][U];
+        at_f16 s[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int a = 0; a < QT; ++a)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[a][u][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
 #pragma unroll
             for (int j = 0; j < KJ; ++j) {
-                const int row = 32 * u + r;
-                const uint4 f = *reinterpret_cast<const uint4 *>(kt + row * PITCH + k_piece<PITCH>(row, 2 * j + half) * 8);
-#pragma unroll
-                for (int a = 0; a < QT; ++a) s[a][u] = mma32<T>(f, q[a][j], s[a][u]);
+                const int at = 32 * u + r;
+                s[u] = mma32<T>(*reinterpret_cast<const uint4 *>(kt + at * PITCH + k_piece<PITCH>(at, 2 * j + half) * 8), q[j], s[u]);
             }
         }
         // (fragments are read AHEAD products before they are used)
@@ -350,76 +345,108 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_at
         __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
         for (int i = 0; i < U * KJ - AHEAD; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * QT, 0);
-        uint4 pr[QT][2 * U];
-#pragma unroll
-        for (int a = 0; a < QT; ++a) {
-            const int row = row0 + (wave * QT + a) * 32 + r, last = min(Lk - 1, row + off) - j0 - 4 * half;    // the last key that the row sees, from this lane's first on
-            if (j0 + KEYS > seen_by_all) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (32 * u + 8 * (i / 4) + i % 4 > last) s[a][u][i] = -__builtin_inff();
-            }
-            float top = s[a][0][0];
+        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+        if (j0 + 32 * U > seen_by_all) {
+            const int last = row_last - j0 - 4 * half;                   // from this lane's first key on
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[a][u][i]);
-            top = across32(top, false) * p.scale;
-            if (__any(top > m[a] + PR_SLACK)) {
-                const float n = fmaxf(m[a], top);
-                const float w = m[a] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[a] - n);
-                m[a] = n;
-                l[a] *= w;
+                for (int i = 0; i < 16; ++i)
+                    if (32 * u + 8 * (i / 4) + i % 4 > last) s[u][i] = -__builtin_inff();
+        }
+        float top = s[0][0];
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[a][d][i] *= w;
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+        top = across32(top, false) * p.scale;
+        if (__any(top > m + PR_SLACK)) {
+            const float n = fmaxf(m, top), w = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - n);
+            m = n;
+            l *= w;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= w;
+        }
+        // (f16 probabilities are 2^7 times as large, 2^15 at most, so that small ones keep their bits)
+        const float base = m == -__builtin_inff() ? 0.0f : m - (F16 ? 7.0f : 0.0f);
+        uint4 pr[2 * U];
+#pragma unroll
+        for (int e = 0; e < 2 * U; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = s[e / 2][8 * (e & 1) + 2 * i], y = s[e / 2][8 * (e & 1) + 2 * i + 1];
+                w[i] = pair16<T>(__builtin_amdgcn_exp2f(fmaf(x, p.scale, -base)), __builtin_amdgcn_exp2f(fmaf(y, p.scale, -base)));
+                l = sum_pair<T>(w[i], l);                                // (what the second product takes, so that the weights add up to 1)
             }
-            // (f16 probabilities are 2^7 times as large, 2^15 at most, so that small ones keep their bits)
-            const float base = m[a] == -__builtin_inff() ? 0.0f : m[a] - (F16 ? 7.0f : 0.0f);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[a][u][i] = __builtin_amdgcn_exp2f(fmaf(s[a][u][i], p.scale, -base));
-#pragma unroll
-            for (int e = 0; e < 2 * U; ++e)
-                pr[a][e] = make_uint4(pair16<T>(s[a][e / 2][8 * (e & 1)], s[a][e / 2][8 * (e & 1) + 1]),
-                                      pair16<T>(s[a][e / 2][8 * (e & 1) + 2], s[a][e / 2][8 * (e & 1) + 3]),
-                                      pair16<T>(s[a][e / 2][8 * (e & 1) + 4], s[a][e / 2][8 * (e & 1) + 5]),
-                                      pair16<T>(s[a][e / 2][8 * (e & 1) + 6], s[a][e / 2][8 * (e & 1) + 7]));
-            // (the sum of what the second product takes, so that the weights add up to 1)
-#pragma unroll
-            for (int e = 0; e < 2 * U; ++e) l[a] = sum_pair<T>(pr[a][e].w, sum_pair<T>(pr[a][e].z, sum_pair<T>(pr[a][e].y, sum_pair<T>(pr[a][e].x, l[a]))));
+            pr[e] = make_uint4(w[0], w[1], w[2], w[3]);
         }
         // ---- V^T P^T
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int e = 0; e < 2 * U; ++e) {
-                const uint4 f = v_fragment(vt, d, e);
-#pragma unroll
-                for (int c = 0; c < QT; ++c) o[c][d] = mma32<T>(f, pr[c][e], o[c][d]);
-            }
+            for (int e = 0; e < 2 * U; ++e) o[d] = mma32<T>(v_fragment(vt, d, e), pr[e], o[d]);
         __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
         for (int i = 0; i < DT * 2 * U - AHEAD; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * QT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
     };
-    for (int j0 = 0, stage = 0; j0 < end; j0 += KEYS, stage ^= 1) {
+    for (int j0 = 0, stage = 0; j0 < end; j0 += KEYS, stage ^= STAGES - 1) {
         arrived(stage, j0);                                              // (and nobody reads the other stage any more)
         step(lds + stage * 2 * TILE, lds + stage * 2 * TILE + TILE, lds + (stage ^ 1) * 2 * TILE, j0);
+        if (STAGES == 1 && j0 + KEYS < end) {
+            __syncthreads();
+            fetch(j0 + KEYS, lds);
+        }
+    }
+    const bool odd = end > partial && (odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3]);
+
+    if constexpr (SPLIT) {
+        // ---- the four waves' sums, by way of LDS: a lane's are of the same row and columns in all of them
+        float *const tops = reinterpret_cast<float *>(lds), *const sums = tops + 256;
+        __syncthreads();
+        tops[threadIdx.x] = m;
+        __syncthreads();
+        const float top = fmaxf(fmaxf(tops[lane], tops[64 + lane]), fmaxf(tops[128 + lane], tops[192 + lane]));
+        const float w = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        l *= w;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= w;
+        constexpr int PER = DT * 16 + 1;
+#pragma unroll
+        for (int n = 2; n >= 1; n /= 2) {
+            float *to = sums + (wave & (n - 1)) * 64 * PER + lane;
+            if (wave >= n && wave < 2 * n) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) to[(d * 16 + i) * 64] = o[d][i];
+                to[DT * 16 * 64] = l;
+            }
+            __syncthreads();
+            if (wave < n) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] += to[(d * 16 + i) * 64];
+                l += to[DT * 16 * 64];
+            }
+            __syncthreads();
+        }
+        if (wave) return;
     }
 
-    if (end > 0 && end > partial && (odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3])) {
+    if (odd) {
         for (int j = max(partial, 0) / KEYS * KEYS; j < end; ++j) {
             const uint16_t *values = reinterpret_cast<const uint16_t *>(v_base + (int64_t)j * p.ldv);
 #pragma unroll
@@ -429,40 +456,35 @@ __global__ void __launch_bounds__(256, QT * DP > 128 ? 1 : DP > 64 ? 2 : 3) k_at
                     if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                     const int col = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
                     const uint16_t v = col < p.D ? values[col] : 0;
-#pragma unroll
-                    for (int a = 0; a < QT; ++a)
-                        if ((v & EXP) == EXP && j <= min(Lk - 1, row0 + (wave * QT + a) * 32 + r + off)) o[a][d][i] += value16<T>(v);
+                    if ((v & EXP) == EXP && j <= row_last) o[d][i] += value16<T>(v);
                 }
         }
     }
 
     // ---- lane: row r, columns 32 d + 8 (i / 4) + 4 half + i % 4
+    const bool any = row_last >= 0;
+    // (a row whose every score is -inf has a sum of 0 and comes out as NaN, as its definition does; a row without keys as 0)
+    const float w = 1.0f / across32(l, true);
+    if (row >= Lq) return;
+    T *to = static_cast<T *>(p.o) + (int64_t)(q0 + row) * p.ldo + (int64_t)h * p.D;
 #pragma unroll
-    for (int a = 0; a < QT; ++a) {
-        const int row = row0 + (wave * QT + a) * 32 + r;
-        const bool any = min(Lk - 1, row + off) >= 0;
-        // (a row whose every score is -inf has a sum of 0 and comes out as NaN, as its definition does; a row without keys as 0)
-        const float w = 1.0f / across32(l[a], true);
-        if (row >= Lq) continue;
-        T *to = static_cast<T *>(p.o) + (int64_t)(q0 + row) * p.ldo + (int64_t)h * p.D;
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int col = 32 * d + 2 * i + 4 * half;
-                const uint2 y = any ? make_uint2(pair16<T>(o[a][d][i] * w, o[a][d][i + 1] * w), pair16<T>(o[a][d][i + 2] * w, o[a][d][i + 3] * w)) : make_uint2(0, 0);
-                if (col < p.D) __builtin_memcpy(to + col, &y, 8);
-            }
-    }
+        for (int i = 0; i < 16; i += 4) {
+            const int col = 32 * d + 2 * i + 4 * half;
+            const uint2 y = any ? make_uint2(pair16<T>(o[d][i] * w, o[d][i + 1] * w), pair16<T>(o[d][i + 2] * w, o[d][i + 3] * w)) : make_uint2(0, 0);
+            if (col < p.D) __builtin_memcpy(to + col, &y, 8);
+        }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------
 
-template <typename T, int DP, int QT>
+template <typename T, int DP, bool SPLIT>
 static nq_status launch_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
-    constexpr int BYTES = 4 * keys_of(DP) * pitch_of(DP) * 2 + 16;
-    p.tiles = p.q_rows / (128 * QT) + p.sequences;
+    constexpr int TILES = 2 * stages_of(DP, SPLIT) * keys_of(DP, SPLIT) * pitch_of(DP) * 2, SUMS = SPLIT ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;
+    constexpr int BYTES = (TILES > SUMS ? TILES : SUMS) + 16;
+    p.tiles = p.q_rows / (SPLIT ? 32 : 128) + p.sequences;
     auto launch = [&](auto kernel, std::atomic<uint64_t> &granted) {
         const nq_status st = grant_lds(kernel, BYTES, granted);
         if (st != NQ_OK) return st;
@@ -470,17 +492,20 @@ static nq_status launch_prompt(PromptParams &p, bool direct, hipStream_t s)
         return launch_status();
     };
     static std::atomic<uint64_t> granted[2] = {};
-    return direct ? launch(k_attention_prompt<T, DP, QT, true>, granted[1]) : launch(k_attention_prompt<T, DP, QT, false>, granted[0]);
+    return direct ? launch(k_attention_prompt<T, DP, SPLIT, true>, granted[1]) : launch(k_attention_prompt<T, DP, SPLIT, false>, granted[0]);
 }
 
 template <typename T>
 static nq_status run_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
-    if (p.D <= 64) return launch_prompt<T, 64, 1>(p, direct, s);
-    if (p.D <= 96) return launch_prompt<T, 96, 1>(p, direct, s);
-    if (p.D <= 128) return launch_prompt<T, 128, 1>(p, direct, s);
-    if (p.D <= 192) return launch_prompt<T, 192, 1>(p, direct, s);
-    return launch_prompt<T, 256, 1>(p, direct, s);
+    // 32 rows to a workgroup and the keys dealt to its waves, where that still makes one round or two of workgroups and there are keys to deal: 512
+    // rows of 32 heads 11.8 us, 128 rows to a workgroup 14.8; 1024 of 8 15.7 and 23.2; 1024 of 32 28.8 and 25.0; 64 rows over 173 keys 9.2 and 8.6
+    const bool split = p.D <= 128 && (p.q_rows / 32 + p.sequences) * (int64_t)p.Hq <= 576 && p.k_rows >= 192 * (int64_t)p.sequences;
+    if (p.D <= 64) return split ? launch_prompt<T, 64, true>(p, direct, s) : launch_prompt<T, 64, false>(p, direct, s);
+    if (p.D <= 96) return split ? launch_prompt<T, 96, true>(p, direct, s) : launch_prompt<T, 96, false>(p, direct, s);
+    if (p.D <= 128) return split ? launch_prompt<T, 128, true>(p, direct, s) : launch_prompt<T, 128, false>(p, direct, s);
+    if (p.D <= 192) return launch_prompt<T, 192, false>(p, direct, s);
+    return launch_prompt<T, 256, false>(p, direct, s);
 }
 
 }  // namespace nq

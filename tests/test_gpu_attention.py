@@ -250,6 +250,11 @@ PROMPT = [  # query lengths, key lengths or None, Hq, Hkv, D, dtype, causal, sca
     ([40], [90], 2, 1, 136, BF16, False, 0.0, 0),
     ([515], None, 2, 2, 128, F16, True, 0.2, 0),
     ([2, 700], [2, 1300], 1, 1, 64, BF16, True, 0.15, 0),
+    ([1100, 300, 5], None, 32, 8, 64, BF16, True, 0.15, 0),
+    ([1030], None, 40, 4, 96, F16, False, 0.1, 0),
+    ([130, 900], [130, 1111], 32, 8, 128, F16, True, 0.1, 0),
+    ([300] * 70, None, 2, 2, 64, BF16, True, 0.1, 0),
+    ([7 * i % 60 for i in range(300)], [11 * i % 90 for i in range(300)], 1, 1, 64, BF16, True, 0.1, 0),
 ]
 
 
@@ -284,7 +289,7 @@ def check_prompt(got, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, scal
             ref.check(got[qb[s]:qb[s + 1], h * D:h * D + D], o, bound, f"{what} sequence {s} head {h}")
 
 
-@pytest.mark.parametrize("case", PROMPT, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c))
+@pytest.mark.parametrize("case", PROMPT, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "")[:40] for x in c))
 def test_attention_prompt(nq, case):
     lengths, keys, Hq, Hkv, D, dtype, causal, scale, gap = case
     first, behind = (3, 5) if len(lengths) > 1 else (0, 0)
@@ -305,22 +310,28 @@ def test_attention_prompt(nq, case):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
-@pytest.mark.parametrize("D", [64, 128, 256])
-def test_prompt_values_that_are_not_finite(nq, dtype, D):
-    """Keys and values that a row does not see do not reach it, whatever they are; those that it sees do."""
+@pytest.mark.parametrize("D,heads,gap", [(64, 1, 0), (128, 1, 0), (256, 1, 0), (64, 140, 0), (128, 140, 0), (128, 1, 4), (64, 140, 4)])
+def test_prompt_values_that_are_not_finite(nq, dtype, D, heads, gap):
+    """Keys and values that a row does not see do not reach it, whatever they are; those that it sees do.  Many heads and few: both ways to divide the
+    work; rows on 16 bytes and not."""
     n = 150
-    q, k, v = (randn(70 + i, n, D) for i in range(3))
+    one = [randn(70 + i, n, D) for i in range(3)]
+    q, k, v = (x.clone() for x in one)
     v[70, 5], v[71, 6], v[72, 7] = float("inf"), -float("inf"), float("nan")
     v[130] = float("nan")
     k[100, 0] = float("nan")
     q, k, v = (x.to(dtype) for x in (q, k, v))
-    out, _ = run_prompt(nq, q, k, v, begins([n]), None, 1, 1, 1, D, dtype, True, 0.1)
-    got = out.cpu()
-    check_prompt(got[:100], q[:100], k[:100], v[:100], begins([100]), None, 1, 1, D, dtype, True, 0.1)
-    assert torch.isnan(got[100:]).all()
+    wide = lambda x: x.repeat(1, heads)  # noqa: E731
+    some = {0, heads - 1}
+    got = run_prompt(nq, wide(q), k, v, begins([n]), None, 1, heads, 1, D, dtype, True, 0.1, gap)[0].cpu()
+    for h in some:
+        part = got[:, h * D:(h + 1) * D]
+        check_prompt(part[:100], q[:100], k[:100], v[:100], begins([100]), None, 1, 1, D, dtype, True, 0.1)
+        assert torch.isnan(part[100:]).all()
     k[100] = 0
-    out, _ = run_prompt(nq, q, k, v, begins([n]), None, 1, 1, 1, D, dtype, True, 0.1)
-    check_prompt(out.cpu(), q, k, v, begins([n]), None, 1, 1, D, dtype, True, 0.1)
+    got = run_prompt(nq, wide(q), k, v, begins([n]), None, 1, heads, 1, D, dtype, True, 0.1, gap)[0].cpu()
+    for h in some:
+        check_prompt(got[:, h * D:(h + 1) * D], q, k, v, begins([n]), None, 1, 1, D, dtype, True, 0.1)
 
 
 def test_prompt_scores_of_no_weight(nq):
