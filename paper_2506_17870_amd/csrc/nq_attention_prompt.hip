@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
     constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP, SPLIT), STAGES = stages_of(DP, SPLIT), U = SPLIT ? 1 : KEYS / 32, KJ = DP / 16, DT = DP / 32;
     constexpr int ROWS = SPLIT ? 32 : 128, TILE = KEYS * PITCH;
     constexpr int PIECES = DIRECT ? PITCH / 8 : DP / 8, CH = KEYS * PIECES / 256;      // pieces of 16 bytes of a row; of a thread and tile
+    constexpr bool THROUGH = !SPLIT && DP <= 128;                        // Q and O travel through LDS, too
     constexpr int SUMS = SPLIT ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;    // bytes for the waves' sums
     constexpr bool F16 = __is_same(T, _Float16);
     constexpr uint32_t EXP = F16 ? 0x7c00 : 0x7f80;                      // the exponent of infinities and NaN
@@ -290,11 +291,28 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
     const int first_row = row0 + (SPLIT ? 0 : wave * 32), row = first_row + r;
     uint4 q[KJ];
     const T *q_row = static_cast<const T *>(p.q) + (int64_t)(q0 + row) * p.ldq + (int64_t)h * p.D;
+    uint16_t *const own = lds + 2 * TILE + wave * 32 * PITCH;            // of the second stage, free before the first step and after the last
+    if constexpr (THROUGH && DIRECT) {
+        // a wave's rows by whole lines, as those of K
+        const T *from = static_cast<const T *>(p.q) + (int64_t)(q0 + first_row) * p.ldq + (int64_t)h * p.D;
+        const __amdgpu_buffer_rsrc_t qr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(from), 0, RANGE, 0x00020000);
+        constexpr int PER = PITCH / 8;
 #pragma unroll
-    for (int j = 0; j < KJ; ++j) {
-        const int d = 16 * j + 8 * half;
-        q[j] = make_uint4(0, 0, 0, 0);
-        if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[j], q_row + d, 16);
+        for (int i = 0; i < PER / 2; ++i) {
+            const int at = (i * 64 + lane) / PER, d = k_piece<PITCH>(at, (i * 64 + lane) % PER) * 8;
+            const int q_off = first_row + at < Lq && d < p.D && !p.zero ? (int)(at * p.ldq + d) * 2 : NOWHERE;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_ptr)(own + i * 512), 16, q_off, 0, 0, 0);
+        }
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));             // (this wave's alone: nobody else reads them)
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) q[j] = *reinterpret_cast<const uint4 *>(own + r * PITCH + k_piece<PITCH>(r, 2 * j + half) * 8);
+    } else {
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) {
+            const int d = 16 * j + 8 * half;
+            q[j] = make_uint4(0, 0, 0, 0);
+            if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[j], q_row + d, 16);
+        }
     }
     if (p.flip) {
 #pragma unroll
@@ -465,16 +483,38 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
     const bool any = row_last >= 0;
     // (a row whose every score is -inf has a sum of 0 and comes out as NaN, as its definition does; a row without keys as 0)
     const float w = 1.0f / across32(l, true);
-    if (row >= Lq) return;
-    T *to = static_cast<T *>(p.o) + (int64_t)(q0 + row) * p.ldo + (int64_t)h * p.D;
+    T *const to = static_cast<T *>(p.o) + (int64_t)(q0 + first_row) * p.ldo + (int64_t)h * p.D;     // the wave's first row
+    if constexpr (THROUGH) {
+        // whole rows leave, 16 bytes a lane (the second stage of the two is free where the last step was of the first, else the first)
+        uint16_t *const out = lds + (end > 0 && ((end - 1) / KEYS) % 2 ? 0 : 2 * TILE) + wave * 32 * PITCH;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int col = 32 * d + 2 * i + 4 * half;
-            const uint2 y = any ? make_uint2(pair16<T>(o[d][i] * w, o[d][i + 1] * w), pair16<T>(o[d][i + 2] * w, o[d][i + 3] * w)) : make_uint2(0, 0);
-            if (col < p.D) __builtin_memcpy(to + col, &y, 8);
+            for (int i = 0; i < 16; i += 4) {
+                const int col = 32 * d + 2 * i + 4 * half;
+                const uint2 y = any ? make_uint2(pair16<T>(o[d][i] * w, o[d][i + 1] * w), pair16<T>(o[d][i + 2] * w, o[d][i + 3] * w)) : make_uint2(0, 0);
+                *reinterpret_cast<uint2 *>(out + r * PITCH + k_piece<PITCH>(r, col >> 3) * 8 + (col & 4)) = y;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();                                 // (LDS serves a wave's requests in order)
+        constexpr int PER = PITCH / 8;
+#pragma unroll
+        for (int i = 0; i < PER / 2; ++i) {
+            const int at = (i * 64 + lane) / PER, d = (i * 64 + lane) % PER * 8;
+            const uint4 y = *reinterpret_cast<const uint4 *>(out + at * PITCH + k_piece<PITCH>(at, d >> 3) * 8);
+            if (first_row + at < Lq && d < p.D) __builtin_memcpy(to + at * p.ldo + d, &y, 16);
         }
+    } else {
+        if (row >= Lq) return;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int col = 32 * d + 2 * i + 4 * half;
+                const uint2 y = any ? make_uint2(pair16<T>(o[d][i] * w, o[d][i + 1] * w), pair16<T>(o[d][i + 2] * w, o[d][i + 3] * w)) : make_uint2(0, 0);
+                if (col < p.D) __builtin_memcpy(to + r * p.ldo + col, &y, 8);
+            }
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------
@@ -557,6 +597,7 @@ extern "C" nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream)
     p.flip = j.scale < 0.0f ? 0x80008000u : 0u;
     p.zero = j.scale == 0.0f;
     // rows on 16 bytes, a tile's offsets within 31 bits
-    const bool direct = aligned16(j.d_k) && aligned16(j.d_v) && j.ldk % 8 == 0 && j.ldv % 8 == 0 && std::max(j.ldk, j.ldv) < (int64_t(1) << 23);
+    const bool direct = aligned16(j.d_q) && aligned16(j.d_k) && aligned16(j.d_v) && j.ldq % 8 == 0 && j.ldk % 8 == 0 && j.ldv % 8 == 0 &&
+                        std::max(std::max(j.ldq, j.ldk), j.ldv) < (int64_t(1) << 23);
     return j.dtype == NQ_DT_F16 ? run_prompt<_Float16>(p, direct, (hipStream_t)stream) : run_prompt<bf16_t>(p, direct, (hipStream_t)stream);
 }
