@@ -544,7 +544,9 @@ nq_status nq_cache_read(const nq_kv_cache *cache, const int64_t *d_slot, int64_t
  * d_q, d_o [q_rows][q_heads][head_dim], d_k, d_v [k_rows][kv_heads][head_dim] of dtype, f16 or bf16 (fp32: NQ_ERR_UNSUPPORTED).
  * Sums and softmax in fp32, the probabilities (relative to a row's largest) rounded to dtype for the second product,
  * outputs rounded once.  The order of the sums depends on the sizes alone, so equal calls give equal bits.
- * Begins are not to fall and to end within the rows; ones that do not are cut off there.  d_o must not overlap the inputs. */
+ * Begins are not to fall and to end within the rows: what of a sequence lies outside is cut off, and where they fall some rows may be left
+ * as they were.  d_o must not overlap the inputs.  (q_rows / 128 + sequences) * q_heads < 2^24 (NQ_ERR_SHAPE).  Rows of q, k and v on 16 bytes
+ * are fast. */
 typedef struct {
     const void *d_q, *d_k, *d_v;
     void *d_o;
@@ -559,7 +561,8 @@ nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream);
 /* The same for one row of each sequence, over the cache: row s of d_q and d_o [sequences][q_heads][head_dim] sees the first
  * d_length[s] tokens of the pages d_table[s * ldtable ..].  No tokens: 0.  A length counts up to max_length (which sizes the launch and
  * the workspace: the nearer to the longest, the better), tokens of a page that the cache does not have (-1, say) are left out; ldtable *
- * page_tokens >= max_length.  dtype: f16 or bf16; the cache e4m3 or of the same type (NQ_ERR_UNSUPPORTED).
+ * page_tokens >= max_length.  At most 65535 sequences (NQ_ERR_SHAPE).  dtype: f16 or bf16; the cache e4m3 or of the same type
+ * (NQ_ERR_UNSUPPORTED).
  * Sums, softmax and probabilities as exact as fp32 makes them.  A sequence's tokens are split over workgroups whose results the
  * workspace holds until they are joined; how depends on all lengths of the call.  d_workspace: 16-byte aligned, of
  * nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length) or more (0: NULL will do); its

@@ -42,7 +42,7 @@ __device__ __forceinline__ int before(int v, int *all)
 // ---- host ------------------------------------------------------------------------------------------------------
 
 // (a row of heads of floats is at most 2^32 elements away from the next, as check_matrix has it)
-constexpr int64_t KV_MAX_STEP = int64_t(1) << 26, KV_MAX_PAGE_STEP = int64_t(1) << 40, ATT_MAX_ROWS = int64_t(1) << 30;
+constexpr int64_t KV_MAX_STEP = int64_t(1) << 26, KV_MAX_PAGE_STEP = int64_t(1) << 40, ATT_MAX_ROWS = (int64_t(1) << 30) - 4096;     // (two of them and a tile fit 31 bits)
 
 inline nq_status check_heads(int q_heads, int kv_heads, int head_dim)
 {
