@@ -544,6 +544,7 @@ nq_status nq_cache_read(const nq_kv_cache *cache, const int64_t *d_slot, int64_t
  * d_q, d_o [q_rows][q_heads][head_dim], d_k, d_v [k_rows][kv_heads][head_dim] of dtype, f16 or bf16 (fp32: NQ_ERR_UNSUPPORTED).
  * Sums and softmax in fp32, the probabilities (relative to a row's largest) rounded to dtype for the second product,
  * outputs rounded once.  The order of the sums depends on the sizes alone, so equal calls give equal bits.
+ * An infinite or NaN value that a row sees makes its column not finite (which of the two is left open), one that it does not see has no part in it.
  * Begins are not to fall and to end within the rows: what of a sequence lies outside is cut off, and where they fall some rows may be left
  * as they were.  d_o must not overlap the inputs.  (q_rows / 128 + sequences) * q_heads < 2^24 (NQ_ERR_SHAPE).  Rows of q, k and v on 16 bytes
  * are fast. */
@@ -563,8 +564,8 @@ nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream);
  * the workspace: the nearer to the longest, the better), tokens of a page that the cache does not have (-1, say) are left out; ldtable *
  * page_tokens >= max_length.  At most 65535 sequences (NQ_ERR_SHAPE).  dtype: f16 or bf16; the cache e4m3 or of the same type
  * (NQ_ERR_UNSUPPORTED).
- * Sums, softmax and probabilities as exact as fp32 makes them.  A sequence's tokens are split over workgroups whose results the
- * workspace holds until they are joined; how depends on all lengths of the call.  d_workspace: 16-byte aligned, of
+ * Sums, softmax and probabilities as exact as fp32 makes them; infinities and NaN as above.  A sequence's tokens are split over workgroups
+ * (in calls of up to 1024 sequences) whose results the workspace holds until they are joined; how depends on all lengths of the call.  d_workspace: 16-byte aligned, of
  * nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length) or more (0: NULL will do); its
  * contents count only while the call runs, so calls that may run at the same time (on two streams, in two graphs) need one each. */
 typedef struct {

@@ -7,6 +7,8 @@
 // empty, which the matrix core has time for), then O^T = V^T P^T of 32 tokens.  The lane that holds four tokens' scores of a head
 // after the first product holds the same tokens' place in the second one's operand, because the order in which a product sums its
 // tokens is free: the probabilities never leave their registers, and a lane keeps the maximum and the sum of one head.
+// 4 sequences of 65536 tokens, 8 key heads of 128 bf16: 189 us, 5.7 TB/s; 96 of 64 to 4096, e4m3, 56 us, 3.8 TB/s, the rest of it the pieces'
+// uneven ends and the planning; one sequence of 517 tokens 9.6 us, a launch and the chain of five steps of one workgroup to a key head.
 #include "nq_attention.h"
 
 namespace nq {
@@ -18,7 +20,7 @@ typedef float at_f4 __attribute__((ext_vector_type(4)));
 constexpr int TK_TILE = 32, TK_COLS = 16;                  // tokens of a wave's step; query heads of a matrix tile
 constexpr float TK_LOG2E = 1.44269504088896340736f;
 
-constexpr int TK_LEAST = 128;                              // tokens of a piece, at least
+constexpr int TK_LEAST = 128, TK_MOST_PLANNED = 1024;      // tokens of a piece, at least; sequences of a call that is split, at most
 // Workgroups to a compute unit, by their registers.
 __host__ __device__ constexpr int workgroups_of(int head_dim, bool codes) { return head_dim <= 128 ? 3 : codes ? 2 : 1; }
 
@@ -27,6 +29,7 @@ struct TokenParams {
     void *o;
     const int32_t *table, *length;
     float *partial;                       // sums of o [pieces][q_heads][D], then m and l [pieces][q_heads][2]
+    int2 *dealt;                          // for each sequence: its first piece, how many it has
     CacheView cache;
     int64_t ldq, ldo, ldtable;
     int32_t sequences, max_length, Hq, Hkv, group, col_tiles, D, pieces;   // pieces: 0 where no sequence is split
@@ -38,8 +41,6 @@ struct TokenParams {
 // of more than half a chunk goes into pieces of equal size, as few as have a chunk at most; those come first, and the shorter sequences,
 // a piece each, fill the gaps that they leave.  So there are as many pieces as workgroups wanted, and one more for each sequence, at most.
 // Every wave that asks makes the same sums in the same order.
-constexpr int TK_MOST_PLANNED = 1024;     // sequences: sixteen to a lane
-
 __device__ __forceinline__ int length_of(const TokenParams &p, int i) { return i < p.sequences ? min(max(p.length[i], 0), p.max_length) : 0; }
 
 // The call's lengths, a lane each of 64 sequences, 256 asked for at once and kept if there are no more.
@@ -87,7 +88,7 @@ __device__ __forceinline__ void each_sequence(const TokenParams &p, F found)
     Lengths lengths(p);
     const int chunk = chunk_of(p, lengths);
     auto pieces = [&](int length) {
-        const int n = max((length + chunk - 1) / chunk, 1), size = max(((length + n - 1) / n + TK_TILE - 1) / TK_TILE * TK_TILE, TK_TILE);
+        const int n = max((int)(((uint32_t)length + (uint32_t)chunk - 1) / (uint32_t)chunk), 1), size = max(((length + n - 1) / n + TK_TILE - 1) / TK_TILE * TK_TILE, TK_TILE);
         return Pieces{0, max((length + size - 1) / size, 1), size};
     };
     auto large = [&](int length) { return length > chunk / 2; };
@@ -194,7 +195,10 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : workgroups_of(DP,
             s = __builtin_amdgcn_readlane(i, from);
             begin = __builtin_amdgcn_readlane(at, from);
             end = __builtin_amdgcn_readlane(at + min(length - at, x.size), from);
-            whole = __builtin_amdgcn_readlane(x.count, from) == 1;
+            const int count = __builtin_amdgcn_readlane(x.count, from), first_piece = __builtin_amdgcn_readlane(x.first, from);
+            whole = count == 1;
+            // (for the join; every sequence has a first piece)
+            if (blockIdx.x == 0 && piece == first_piece && threadIdx.x == 0) p.dealt[s] = make_int2(first_piece, count);
             return true;
         });
         if (s < 0) return;
@@ -462,12 +466,8 @@ __global__ void __launch_bounds__(256) k_attention_join(const TokenParams p)
     constexpr int AHEAD = TH == 64 ? 8 : 4, HEADS = 256 / TH;
     __shared__ float sums[HEADS][TH][5], weight[HEADS][TH], tops[4];
     const int s = blockIdx.y, group = threadIdx.x / TH, tid = threadIdx.x % TH, h = min((int)blockIdx.x * HEADS + group, p.Hq - 1);
-    Pieces all{0, 0, 0};
-    each_sequence(p, [&](int i, int, const Pieces &x) {
-        if (s >= (i & ~63) + 64) return false;
-        all = Pieces{__builtin_amdgcn_readlane(x.first, s & 63), __builtin_amdgcn_readlane(x.count, s & 63), 0};
-        return true;
-    });
+    const int2 dealt = p.dealt[s];
+    const Pieces all{dealt.x, dealt.y, 0};
     if (all.count <= 1) return;                                          // (k_attention_token has written the row)
     const f8_f2 *ml = reinterpret_cast<const f8_f2 *>(p.partial + (int64_t)p.pieces * p.Hq * p.D);
     const int per = p.D / 4, at = tid % per, mine = tid / per, step = TH / per;
@@ -547,11 +547,15 @@ static bool short_call(int64_t sequences, int64_t blocks, int64_t max_length, in
 
 // Pieces of the call's tokens for each of `blocks` head blocks, 0: a sequence is one.  `target` workgroups are wanted.  Two to a compute unit carry the
 // memory's rate and leave the third's place to what is short (64 sequences of 1024 tokens, 128 columns e4m3, 32.4 us, for three 37.6; 64 columns bf16,
-// whose tiles are smaller, 42.6 and 39.8).  From twice that many sequences on they even out by themselves (256 of up to 1024 tokens 49.2 us, in pieces 60.7).
+// whose tiles are smaller, 42.6 and 39.8).  From twice that many sequences on they even out by themselves, unless one may be so long that its
+// workgroup is the last for a while; against that stands the planning, which each workgroup does over all sequences.  8 key heads of 128 e4m3, whole
+// and in pieces: 256 sequences of up to 1024 tokens 40.7 and 43.6 us, to 2048 72.5 and 67.1, one of 65536 among 255 of some 200 609 and 59;
+// 512 of up to 4096 235 and 265, one of 32768 among short ones 354 and 95; one of 16384 among 999 232 and 220.
 static int64_t pieces_of(int64_t sequences, int64_t blocks, int64_t max_length, int head_dim, int64_t *target)
 {
     *target = 256 * (head_dim <= 64 ? 3 : 2);
-    if (max_length <= TK_LEAST || sequences > TK_MOST_PLANNED || sequences * blocks >= 2 * *target) return 0;
+    if (max_length <= TK_LEAST || sequences > TK_MOST_PLANNED) return 0;
+    if (sequences * blocks >= 2 * *target && (max_length < 2048 || sequences * sequences * blocks > 256 * max_length)) return 0;
     if (short_call(sequences, blocks, max_length, head_dim)) return 0;
     return std::min(ceil_div(*target, blocks) + 1, sequences * (max_length / TK_LEAST)) + sequences;
 }
@@ -614,7 +618,7 @@ extern "C" size_t nq_attention_token_workspace_bytes(int64_t sequences, int32_t 
     int64_t target;
     const int64_t blocks = head_blocks(q_heads, kv_heads);
     const int64_t pieces = pieces_of(sequences, blocks, max_length, head_dim, &target);
-    return (size_t)pieces * q_heads * (head_dim + 2) * sizeof(float);
+    return pieces ? (size_t)pieces * q_heads * (head_dim + 2) * sizeof(float) + (size_t)sequences * sizeof(int2) : 0;
 }
 
 extern "C" nq_status nq_attention_token(const nq_token_job *job, void *stream)
@@ -658,6 +662,7 @@ extern "C" nq_status nq_attention_token(const nq_token_job *job, void *stream)
     int64_t target;
     const int64_t blocks = head_blocks(j.q_heads, c.heads);
     p.pieces = (int32_t)pieces_of(p.sequences, blocks, j.max_length, c.head_dim, &target);
+    p.dealt = reinterpret_cast<int2 *>(p.partial + (int64_t)p.pieces * p.Hq * (p.D + 2));
     p.share = (float)blocks / (float)target;
     if (p.pieces) {
         if (!j.d_workspace) return NQ_ERR_INVALID_ARG;

@@ -86,14 +86,14 @@ def grants(nq, stub):  # noqa: F811
 
 def pieces(nq, stub):  # noqa: F811
     """The pieces that a call is launched with are those that its workspace was sized for, and a smaller one is refused."""
-    for S, longest, Hq, Hkv, dim in ((1, 4096, 32, 8, 128), (1, 65536, 1, 1, 64), (96, 4096, 32, 8, 128), (1000, 300, 4, 1, 256), (3, 129, 8, 8, 96)):
+    for S, longest, Hq, Hkv, dim in ((1, 4096, 32, 8, 128), (1, 65536, 1, 1, 64), (96, 4096, 32, 8, 128), (1000, 300, 4, 1, 256), (256, 1 << 16, 32, 8, 128), (256, 1024, 32, 8, 128), (1024, 1 << 20, 8, 8, 64), (3, 129, 8, 8, 96)):
         c = cache(nq, 3, Hkv, dim)
         job = token_job(nq, c, S, longest, Hq)
         nq.nq_attention_token(job, stream=0)
         got = stub.take()
         blocks = Hkv * -(-(Hq // Hkv) // 16)
         if job.workspace_bytes:
-            assert len(got) == 2 and got[0][1] // blocks * Hq * (dim + 2) * 4 == job.workspace_bytes
+            assert len(got) == 2 and got[0][1] // blocks * Hq * (dim + 2) * 4 + S * 8 == job.workspace_bytes
             job.workspace_bytes -= 1
             try:
                 nq.nq_attention_token(job, stream=0)

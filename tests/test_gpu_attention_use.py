@@ -271,3 +271,80 @@ def test_a_cache_on_any_byte(nq, cached):
         ref.check(out[:, h * D:(h + 1) * D].cpu(), o, bound)
     for t in raw:                                  # between the heads, and before the first: nobody's
         assert (t[:3] == 0).all() and (torch.as_strided(t, (pages * page, H - 1, 3), (step, D + 3, 1), 3 + D) == 0).all()
+
+
+@pytest.mark.parametrize("cached", [BF16, E4M3])
+def test_one_long_sequence_among_many(nq, cached):
+    """More sequences than the card needs to be full, one of them long, so that it is split all the same; some empty."""
+    lengths = [(i * 37) % 150 for i in range(200)]
+    lengths[70], lengths[199] = 9000, 1500
+    case = TokenCase(nq, lengths, None, 6, 6, 16, BF16, cached, 16, "head", seed=77)
+    job = case.job()
+    assert job.workspace_bytes > 0
+    nq.nq_attention_token(job)
+    case.check(case.out.cpu())
+
+
+def test_more_threads_than_32_bits_count(nq):
+    """65535 sequences of 512 key heads: 2^33 threads in one launch.  A sequence of one token gets that token's value, an empty one zeros."""
+    S, H, D = 65535, 512, 8
+    k, v = (randn(40 + i, 3, 1, H, D).to(F16).cuda() for i in range(2))
+    table = (torch.arange(S, dtype=torch.int32, device="cuda") % 3)[:, None].contiguous()
+    length = (torch.arange(S, device="cuda") % 2).to(torch.int32)
+    q = torch.ones(S, H * D, dtype=F16, device="cuda")
+    o = torch.full((S, H * D), 7.0, dtype=F16, device="cuda")
+    nq.nq_attention_token(nq.make_attention_token(q, H * D, o, H * D, nq.make_kv_cache(k, v), table, length, S, 1, nq.NQ_DT_F16, H, 0.3))
+    for i in range(3):
+        want = v[i].reshape(1, H * D)
+        mine = o[i::3]
+        there = length[i::3, None] > 0
+        assert torch.equal(mine, torch.where(there, want, torch.zeros_like(want)))
+
+
+@pytest.mark.parametrize("cached", [BF16, E4M3])
+def test_a_cache_past_32_bits(nq, cached):
+    """Two pages 2^32 elements apart, heads and tokens far apart within them."""
+    H, D, page, n, dtype = 2, 64, 32, 60, BF16
+    step, head = (1 << 32) + 64, 1 << 24
+    size = step + head + page * D
+    raw = [torch.empty(size, dtype=torch.uint8 if cached == E4M3 else cached, device="cuda") for _ in range(2)]
+    views = [torch.as_strided(t, (2, page, H, D), (step, D, head, 1)) for t in raw]
+    scales = [torch.ones(2, page, H, device="cuda") for _ in range(2)] if cached == E4M3 else [None, None]
+    cache = nq.make_kv_cache(*views, *scales)
+    x = randn(9, n, 2 * H * D).to(dtype).cuda()
+    none = nq.make_norm(nq.NQ_NORM_NONE)
+    at = torch.arange(n)
+    slot = ((1 - at // page) * page + at % page).cuda()                # the second page first
+    nq.nq_head_norm(nq.make_head_norm(None, 0, x, 2 * H * D, x[:, H * D:], 2 * H * D, dt(nq, dtype), H, H, D, none, none, None, 0, 0, None, None, 0, None, 0, cache, slot), n)
+    back = [torch.zeros(n, H * D, device="cuda") for _ in range(2)]
+    nq.nq_cache_read(cache, slot, n, back[0], H * D, back[1], H * D, nq.NQ_DT_F32)
+    for b, y in zip(back, (x[:, :H * D], x[:, H * D:])):
+        y = y.double().cpu().view(n, H, D)
+        bound = ref.codes_bound(y, torch.zeros_like(y)) if cached == E4M3 else torch.zeros_like(y)
+        ref.check(b.view(n, H, D), y, bound)
+    q = randn(10, 1, 4 * D).to(dtype)
+    out = torch.zeros(1, 4 * D, dtype=dtype, device="cuda")
+    table, length = torch.tensor([[1, 0]], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+    nq.nq_attention_token(nq.make_attention_token(q.cuda(), 4 * D, out, 4 * D, cache, table, length, 1, n, dt(nq, dtype), 4, 0.2))
+    k, v = (b.cpu().double().view(n, H, D) for b in back)
+    for h in range(4):
+        o, bound = ref.attention(q[:, h * D:(h + 1) * D].double(), k[:, h // 2], v[:, h // 2], 0.2, torch.ones(1, n, dtype=torch.bool), dtype, False)
+        ref.check(out[:, h * D:(h + 1) * D].cpu(), o, bound)
+
+
+@pytest.mark.parametrize("ld,rows", [(1 << 22, 1100), ((1 << 24) + 8, 290)])
+def test_prompt_rows_past_32_bits(nq, ld, rows):
+    """Rows whose offsets pass 2^32 elements, below and above the step up to which tiles travel by direct loads."""
+    H, D = 2, 64
+    width = H * D
+    store, to = (torch.empty((rows - 1) * ld + 3 * width, dtype=BF16, device="cuda") for _ in range(2))
+    assert (rows - 1) * ld > 1 << 32
+    parts = [torch.as_strided(store, (rows, width), (ld, 1), i * width) for i in range(3)]
+    host = [randn(60 + i, rows, width).to(BF16) for i in range(3)]
+    for p, x in zip(parts, host):
+        p.copy_(x)
+    out = torch.as_strided(to, (rows, width), (ld, 1))
+    lengths = [rows - 150, 150]
+    begin = begins(lengths).cuda()
+    nq.nq_attention_prompt(nq.make_attention_prompt(parts[0], ld, parts[1], ld, parts[2], ld, out, ld, begin, None, 2, rows, rows, nq.NQ_DT_BF16, H, H, D, True, 0.125))
+    check_prompt(out.cpu(), *host, begins(lengths), None, H, H, D, BF16, True, 0.125)
