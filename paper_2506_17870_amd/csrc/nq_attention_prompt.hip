@@ -4,7 +4,7 @@
 //
 // Bound by the matrix core, by the exponentials next to it, and for long prompts by the card's power: 8192 causal rows of 32 heads of 128 bf16
 // take 524 us (1.05 PFLOP/s; the library's matrix product reaches 1.22), at 1.8 GHz with the matrix core busy 57 % of the time.  A workgroup takes
-// 128 rows of a head, a wave 32 of them, and goes over the keys 64 (32) at a time; two workgroups to a compute unit do one's exponentials
+// 128 rows of a head, a wave 32 of them, and goes over the keys 64 (32) at a time (short calls: enum Share); two workgroups to a compute unit do one's exponentials
 // beside the other's products.  Both products are transposed: S^T = K Q^T, O^T = V^T P^T.  A lane then holds scores of
 // one row only, its maximum and sum need one exchange with another lane, and because the order in which a product sums its keys is
 // free, the scores' places after the first product are the probabilities' places in the second one's operand: they never leave
@@ -93,9 +93,12 @@ template <int PITCH>
 __device__ __forceinline__ int v_piece(int row, int piece) { return piece ^ (PITCH == 64 ? (row & 2) << 1 : ((row & 3) << 2) | ((row >> 2) & 3)); }
 
 constexpr int pitch_of(int DP) { return DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
-// keys of a step: as many as the registers hold beside the outputs
-constexpr int stages_of(int DP, bool split) { return split && DP > 64 ? 1 : 2; }
-constexpr int keys_of(int DP, bool split) { return split ? 128 : DP <= 128 ? 64 : 32; }
+// How a workgroup's waves share its work.  ROWS: four waves of 32 rows each; KEYS: of the same 32 rows, the keys dealt to them; ALONE: one wave of
+// 32 rows.  Keys of a step: as many as the registers hold beside the outputs.
+enum Share { SHARE_ROWS, SHARE_KEYS, SHARE_ALONE };
+constexpr int stages_of(int DP, Share share) { return share == SHARE_ALONE || (share == SHARE_KEYS && DP > 64) ? 1 : 2; }
+constexpr int keys_of(int DP, Share share) { return share == SHARE_ALONE ? 32 : share == SHARE_KEYS ? 128 : DP <= 128 ? 64 : 32; }
+constexpr int waves_of(Share share) { return share == SHARE_ALONE ? 1 : 4; }
 
 // Which rows a workgroup takes: number w in the order of the keys that they see, the most first (in steps of PR_LEVEL keys), so that what
 // is left for the end is short.  For up to PR_PLANNED sequences, a lane each of 64; every wave makes the same sums.
@@ -180,14 +183,29 @@ __device__ __forceinline__ Rows rows_of(const PromptParams &p, int w)
     return Rows{-1, 0};
 }
 
-// DIRECT: K and V travel global -> LDS by direct loads a step ahead, which want rows on 16 bytes; else through registers, when they are used.
-template <typename T, int DP, bool SPLIT, bool DIRECT>
-__global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 3) k_attention_prompt(const PromptParams p)
+// The same for SHARE_ALONE, whose sequences have one tile mostly: nothing to look for there.  Behind the first 32 rows of each come as many tiles as
+// multiples of 32 lie in the call's rows: that of x belongs to the sequence with rows on both sides of x, which has one for each such tile.
+__device__ __forceinline__ Rows rows_alone(const PromptParams &p, int w)
 {
-    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP, SPLIT), STAGES = stages_of(DP, SPLIT), U = SPLIT ? 1 : KEYS / 32, KJ = DP / 16, DT = DP / 32;
-    constexpr int ROWS = SPLIT ? 32 : 128, TILE = KEYS * PITCH;
-    constexpr int PIECES = DIRECT ? PITCH / 8 : DP / 8, CH = KEYS * PIECES / 256;      // pieces of 16 bytes of a row; of a thread and tile
-    constexpr bool THROUGH = !SPLIT && DP <= 128;                        // Q and O travel through LDS, too
+    const int t = p.q_rows / 32 - w;                                     // the multiple 32 t, the last first
+    if (t <= 0) return Rows{-t, 0};
+    int lo = -1, hi = p.sequences;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.q_begin[mid] < 32 * t) lo = mid; else hi = mid;
+    }
+    return lo < 0 ? Rows{-1, 0} : Rows{lo, t - max(p.q_begin[lo], 0) / 32};
+}
+
+// DIRECT: K and V travel global -> LDS by direct loads a step ahead, which want rows on 16 bytes; else through registers, when they are used.
+template <typename T, int DP, Share SHARE, bool DIRECT>
+__global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == SHARE_KEYS || DP > 64 ? 2 : 3) k_attention_prompt(const PromptParams p)
+{
+    constexpr bool SPLIT = SHARE == SHARE_KEYS;
+    constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP, SHARE), STAGES = stages_of(DP, SHARE), U = SPLIT ? 1 : KEYS / 32, KJ = DP / 16, DT = DP / 32;
+    constexpr int WAVES = waves_of(SHARE), THREADS = WAVES * 64, ROWS = SHARE == SHARE_ROWS ? 128 : 32, TILE = KEYS * PITCH;
+    constexpr int PIECES = DIRECT ? PITCH / 8 : DP / 8, CH = KEYS * PIECES / THREADS;  // pieces of 16 bytes of a row; of a thread and tile
+    constexpr bool THROUGH = SHARE == SHARE_ROWS && DP <= 128;           // Q and O travel through LDS, too
     constexpr int SUMS = SPLIT ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;    // bytes for the waves' sums
     constexpr bool F16 = __is_same(T, _Float16);
     constexpr uint32_t EXP = F16 ? 0x7c00 : 0x7f80;                      // the exponent of infinities and NaN
@@ -200,7 +218,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
     const uint32_t number = divide(blockIdx.x, p.by_heads);
     uint32_t h = blockIdx.x - number * p.by_heads.d;
     if (p.Hq % 8 == 0) h = (h & 7) * (p.Hq >> 3) + (h >> 3);
-    const Rows mine = rows_of<ROWS>(p, (int)number);
+    const Rows mine = SHARE == SHARE_ALONE ? rows_alone(p, (int)number) : rows_of<ROWS>(p, (int)number);
     if (mine.sequence < 0) return;
     const int lo = mine.sequence, first = mine.tile;
     const int q0 = min(max(p.q_begin[lo], 0), p.q_rows), q1 = min(max(p.q_begin[lo + 1], q0), p.q_rows), Lq = q1 - q0;
@@ -278,7 +296,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int id = i * 256 + threadIdx.x, row = id / PIECES, piece = id % PIECES, d = piece * 8;
+                const int id = i * THREADS + threadIdx.x, row = id / PIECES, piece = id % PIECES, d = piece * 8;
                 uint4 k = make_uint4(0, 0, 0, 0), v = make_uint4(0, 0, 0, 0);
                 if (j0 + row < end && d < p.D) {
                     __builtin_memcpy(&k, k_base + (int64_t)(j0 + row) * p.ldk + d, 16);
@@ -427,11 +445,12 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
         arrived(stage, j0);                                              // (and nobody reads the other stage any more)
         step(lds + stage * 2 * TILE, lds + stage * 2 * TILE + TILE, lds + (stage ^ 1) * 2 * TILE, j0);
         if (STAGES == 1 && j0 + KEYS < end) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);                          // (what is read is in registers before anything is on its way into its place)
             __syncthreads();
             fetch(j0 + KEYS, lds);
         }
     }
-    const bool odd = end > partial && (odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3]);
+    const bool odd = end > partial && (odd_of[0] | odd_of[WAVES / 4] | odd_of[WAVES / 2] | odd_of[WAVES - 1]);
 
     if constexpr (SPLIT) {
         // ---- the four waves' sums, by way of LDS: a lane's are of the same row and columns in all of them
@@ -525,33 +544,51 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : SPLIT ? 2 : DP > 64 ? 2 : 
 
 // ---- host ------------------------------------------------------------------------------------------------------
 
-template <typename T, int DP, bool SPLIT>
+template <typename T, int DP, Share SHARE>
 static nq_status launch_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
-    constexpr int TILES = 2 * stages_of(DP, SPLIT) * keys_of(DP, SPLIT) * pitch_of(DP) * 2, SUMS = SPLIT ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;
+    constexpr int TILES = 2 * stages_of(DP, SHARE) * keys_of(DP, SHARE) * pitch_of(DP) * 2, SUMS = SHARE == SHARE_KEYS ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;
     constexpr int BYTES = (TILES > SUMS ? TILES : SUMS) + 16;
-    p.tiles = p.q_rows / (SPLIT ? 32 : 128) + p.sequences;
+    p.tiles = p.q_rows / (SHARE == SHARE_ROWS ? 128 : 32) + p.sequences;
     auto launch = [&](auto kernel, std::atomic<uint64_t> &granted) {
         const nq_status st = grant_lds(kernel, BYTES, granted);
         if (st != NQ_OK) return st;
-        kernel<<<(unsigned)p.tiles * (unsigned)p.Hq, 256, BYTES, s>>>(p);
+        kernel<<<(unsigned)p.tiles * (unsigned)p.Hq, waves_of(SHARE) * 64, BYTES, s>>>(p);
         return launch_status();
     };
     static std::atomic<uint64_t> granted[2] = {};
-    return direct ? launch(k_attention_prompt<T, DP, SPLIT, true>, granted[1]) : launch(k_attention_prompt<T, DP, SPLIT, false>, granted[0]);
+    if constexpr (SHARE == SHARE_ALONE && DP > 128)                      // (by way of registers, of which a wave alone has too few there)
+        return launch(k_attention_prompt<T, DP, SHARE, true>, granted[1]);
+    else
+        return direct ? launch(k_attention_prompt<T, DP, SHARE, true>, granted[1]) : launch(k_attention_prompt<T, DP, SHARE, false>, granted[0]);
+}
+
+template <typename T, int DP>
+static nq_status launch_share(PromptParams &p, bool direct, hipStream_t s)
+{
+    const int64_t S = p.sequences, blocks = (p.q_rows / 32 + S) * p.Hq;
+    // Sequences of up to 32 rows and 192 keys, on average, a wave each where four to a workgroup would take more than a round, or have nothing to
+    // share: 256 of 16 rows, 32 heads of 128, 29.8 us, 128 rows to a workgroup 113; 1000 of up to 5 91.8 and 359; 64 of up to 32 15.4 and 29.2; 2 of up
+    // to 30, 8 heads, 6.0 and 7.3; 10 of up to 10, 32 heads of 192, 9.0 and 14.4; 13 rows alone, 4 heads of 256, 10.0 and 9.2
+    if (p.q_rows <= 32 * S && p.k_rows <= 192 * S && (DP > 128 ? direct && S * p.Hq > 256 : S * p.Hq > 512 || p.k_rows <= 64 * S))
+        return launch_prompt<T, DP, SHARE_ALONE>(p, direct, s);
+    // 32 rows to a workgroup and the keys dealt to its waves, where that still makes one round or two of workgroups and there are keys to deal: 512
+    // rows of 32 heads 11.8 us, 128 rows to a workgroup 14.8; 1024 of 8 15.7 and 23.2; 1024 of 32 28.8 and 25.0; 64 rows over 173 keys 9.2 and 8.6; where a
+    // sequence has no more than 32 rows, a round more: 16 of up to 16 over up to 2000 keys 32.0 and 41.0
+    if constexpr (DP <= 128) {
+        if (blocks <= (p.q_rows <= 32 * S ? 1024 : 576) && p.k_rows >= 192 * S) return launch_prompt<T, DP, SHARE_KEYS>(p, direct, s);
+    }
+    return launch_prompt<T, DP, SHARE_ROWS>(p, direct, s);
 }
 
 template <typename T>
 static nq_status run_prompt(PromptParams &p, bool direct, hipStream_t s)
 {
-    // 32 rows to a workgroup and the keys dealt to its waves, where that still makes one round or two of workgroups and there are keys to deal: 512
-    // rows of 32 heads 11.8 us, 128 rows to a workgroup 14.8; 1024 of 8 15.7 and 23.2; 1024 of 32 28.8 and 25.0; 64 rows over 173 keys 9.2 and 8.6
-    const bool split = p.D <= 128 && (p.q_rows / 32 + p.sequences) * (int64_t)p.Hq <= 576 && p.k_rows >= 192 * (int64_t)p.sequences;
-    if (p.D <= 64) return split ? launch_prompt<T, 64, true>(p, direct, s) : launch_prompt<T, 64, false>(p, direct, s);
-    if (p.D <= 96) return split ? launch_prompt<T, 96, true>(p, direct, s) : launch_prompt<T, 96, false>(p, direct, s);
-    if (p.D <= 128) return split ? launch_prompt<T, 128, true>(p, direct, s) : launch_prompt<T, 128, false>(p, direct, s);
-    if (p.D <= 192) return launch_prompt<T, 192, false>(p, direct, s);
-    return launch_prompt<T, 256, false>(p, direct, s);
+    if (p.D <= 64) return launch_share<T, 64>(p, direct, s);
+    if (p.D <= 96) return launch_share<T, 96>(p, direct, s);
+    if (p.D <= 128) return launch_share<T, 128>(p, direct, s);
+    if (p.D <= 192) return launch_share<T, 192>(p, direct, s);
+    return launch_share<T, 256>(p, direct, s);
 }
 
 }  // namespace nq

@@ -348,3 +348,47 @@ def test_prompt_rows_past_32_bits(nq, ld, rows):
     begin = begins(lengths).cuda()
     nq.nq_attention_prompt(nq.make_attention_prompt(parts[0], ld, parts[1], ld, parts[2], ld, out, ld, begin, None, 2, rows, rows, nq.NQ_DT_BF16, H, H, D, True, 0.125))
     check_prompt(out.cpu(), *host, begins(lengths), None, H, H, D, BF16, True, 0.125)
+
+
+SHORT = [
+    # lengths, keys, Hq, Hkv, D, dtype, causal, scale, gap
+    ([1 + 5 * i % 40 for i in range(50)], None, 12, 3, 128, BF16, True, 0.1, 0),
+    ([i % 23 for i in range(300)], None, 4, 4, 64, F16, True, 0.15, 0),
+    ([5 * i % 37 for i in range(90)], [7 * i % 150 for i in range(90)], 8, 2, 96, BF16, True, -0.1, 0),
+    ([200] + [3] * 60, [200] + [100] * 60, 9, 3, 72, F16, False, 0.1, 4),
+    ([2, 17, 0, 30], [90, 17, 8, 31], 2, 1, 128, F16, True, 0.1, 3),
+    ([1 + 7 * i % 33 for i in range(30)], [40 + i for i in range(30)], 10, 5, 192, BF16, True, 0.08, 0),
+    ([1 + 7 * i % 33 for i in range(70)], None, 4, 1, 256, F16, True, 0.08, 0),
+    ([1 + 7 * i % 33 for i in range(70)], None, 4, 1, 256, BF16, False, 0.0, 4),
+]
+
+
+@pytest.mark.parametrize("case", SHORT, ids=lambda c: f"{len(c[0])}-{c[2]}-{c[3]}-{c[4]}-{c[8]}")
+def test_many_short_prompts(nq, case):
+    """Sequences of a few rows, some of more than a tile, some over more keys than a step; rows of no sequence in front and behind."""
+    lengths, keys, Hq, Hkv, D, dtype, causal, scale, gap = case
+    q_begin, k_begin = begins(lengths, 3), begins(keys) if keys else None
+    T = int(q_begin[-1]) + 40
+    K = int(k_begin[-1]) if keys else T
+    q, k, v = (randn(160 + i, *s).to(dtype) for i, s in enumerate(((T, Hq * D), (K, Hkv * D), (K, Hkv * D))))
+    out, _ = run_prompt(nq, q, k, v, q_begin, k_begin, len(lengths), Hq, Hkv, D, dtype, causal, scale, gap)
+    got = out.cpu()
+    check_prompt(got, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, scale)
+    assert (got[:3] == 5).all() and (got[int(q_begin[-1]):] == 5).all(), "rows of no sequence have changed"
+
+
+@pytest.mark.parametrize("D,gap", [(64, 0), (128, 0), (256, 0), (72, 4)])
+def test_short_prompts_with_values_that_are_not_finite(nq, D, gap):
+    """As for long ones: what a row does not see does not reach it."""
+    n, S, H = 24, 60, 6
+    q, k, v = (randn(170 + i, n, D) for i in range(3))
+    v[7, 5], v[9, 6], v[11, 7] = float("inf"), -float("inf"), float("nan")
+    v[20] = float("nan")
+    k[15, 0] = float("nan")
+    q, k, v = (x.to(BF16) for x in (q, k, v))
+    many = lambda x, h: x.repeat(S, h)  # noqa: E731
+    got = run_prompt(nq, many(q, H), many(k, 1), many(v, 1), begins([n] * S), None, S, H, 1, D, BF16, True, 0.1, gap)[0].cpu()
+    for s, h in ((0, 0), (33, 2), (S - 1, H - 1)):
+        part = got[s * n:(s + 1) * n, h * D:(h + 1) * D]
+        check_prompt(part[:15], q[:15], k[:15], v[:15], begins([15]), None, 1, 1, D, BF16, True, 0.1)
+        assert torch.isnan(part[15:]).all()
