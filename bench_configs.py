@@ -2,7 +2,7 @@
 benchmark).  Every kernel time is the begin/end time stamp of the dispatch itself; buffers are rotated so that
 activations and outputs come from HBM, not from the Infinity Cache.
 
-    python bench_configs.py [c1] [c2] [c3] [c4] [c5] [pack] [page] [sweep] [words] [dw] [lib] [fp8] [cpu]
+    python bench_configs.py [c1] [c2] [c3] [c4] [c5] [pack] [page] [sweep] [words] [dw] [lib] [fp8] [attn] [cpu]
 """
 from __future__ import annotations
 
@@ -731,9 +731,51 @@ def fp8():
         print(f"| {tokens} | {us:.1f} | {6.0 * tokens * D * F / us / 1e6:.0f} | {3 * D * F / us / 1e3:.0f} |")
 
 
+def attn():
+    """The attention of a layer of 32 query and 8 key heads of 128 (bf16, e4m3 cache in pages of 16 tokens) on its operators: a prompt's heads, cache
+    and attention, the same prompt's rows back from the cache, and the next token of a batch of sequences of that length."""
+    Hq, Hkv, D, page, dt = 32, 8, 128, 16, nq.NQ_DT_BF16
+    width = (Hq + 2 * Hkv) * D
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    norms = [nq.make_norm(nq.NQ_NORM_RMS, 1e-6, torch.ones(D, device="cuda")) for _ in range(2)]
+    freq = 10000.0 ** (-2 * torch.arange(D // 2, device="cuda") / D)
+
+    print(f"\n### attention, {Hq} query and {Hkv} key heads of {D}, e4m3 cache (back-to-back calls)\n")
+    print("| tokens | heads and cache us | GB/s | causal prompt us | TFLOP/s | rows back us | GB/s |")
+    print("|---|---|---|---|---|---|---|")
+    for T in (1, 33, 512, 2048, 8192, 16384):
+        qkv, q, o, k, back = rand(T, width), rand(T, Hq * D), rand(T, Hq * D), rand(T, Hkv * D), rand(2, T, Hkv * D)
+        cache, slot = nq.KvCache(-(-T // page), page, Hkv, D), torch.randperm(T, generator=gen, device="cuda")
+        v, (keys, values) = qkv[:, (Hq + Hkv) * D:], back
+        heads = nq.make_head_norm(qkv, width, qkv[:, Hq * D:], width, v, width, dt, Hq, Hkv, D, *norms, freq, D, nq.NQ_PAIRS_HALVES,
+                                  torch.arange(T, dtype=torch.int32, device="cuda"), q, Hq * D, k, Hkv * D, cache.desc, slot)
+        prompt = nq.make_attention_prompt(q, Hq * D, k, Hkv * D, v, width, o, Hq * D, torch.tensor([0, T], dtype=torch.int32, device="cuda"), None, 1,
+                                          T, T, dt, Hq, Hkv, D, True, D ** -0.5)
+        a, b = wall_us(lambda: nq.nq_head_norm(heads, T)), wall_us(lambda: nq.nq_attention_prompt(prompt))
+        c = wall_us(lambda: nq.nq_cache_read(cache.desc, slot, T, keys, Hkv * D, values, Hkv * D, dt))
+        codes = 2 * Hkv * (D + 4)
+        print(f"| {T} | {a:.1f} | {T * (2 * width * 2 - Hkv * D * 2 + codes) / a / 1e3:.0f} | {b:.1f} | {2.0 * T * T * Hq * D / b / 1e6:.0f} | {c:.1f} "
+              f"| {T * (4 * Hkv * D + codes) / c / 1e3:.0f} |")
+    print(f"\n### the next token of sequences over the cache, {Hq} query and {Hkv} key heads of {D}\n")
+    print("| sequences | tokens each | bf16 cache us | GB/s | e4m3 cache us | GB/s |")
+    print("|---|---|---|---|---|---|")
+    for S, n in ((1, 512), (1, 8192), (8, 2048), (64, 1024), (64, 8192), (256, 1024), (4, 65536)):
+        cells = []
+        for dtype, size in ((torch.bfloat16, 2 * D), (torch.float8_e4m3fn, D + 4)):
+            cache = nq.KvCache(S * n // page, page, Hkv, D, dtype)
+            q, o, length = rand(S, Hq * D), rand(S, Hq * D), torch.full((S,), n, dtype=torch.int32, device="cuda")
+            table = torch.randperm(S * n // page, generator=gen, device="cuda").view(S, -1).to(torch.int32)
+            workspace = torch.empty(nq.nq_attention_token_workspace_bytes(S, Hq, Hkv, D, n), dtype=torch.uint8, device="cuda")
+            job = nq.make_attention_token(q, Hq * D, o, Hq * D, cache.desc, table, length, S, n, dt, Hq, D ** -0.5, workspace)
+            us = wall_us(lambda: nq.nq_attention_token(job))
+            cells.append(f"{us:.1f} | {2 * S * n * Hkv * size / us / 1e3:.0f}")
+        print(f"| {S} | {n} | {' | '.join(cells)} |")
+
+
 if __name__ == "__main__":
     torch.cuda.set_device(0)
-    which = sys.argv[1:] or ["c1", "c2", "c3", "c4", "c5", "pack", "page", "sweep", "words", "dw", "lib", "fp8", "cpu"]
+    which = sys.argv[1:] or ["c1", "c2", "c3", "c4", "c5", "pack", "page", "sweep", "words", "dw", "lib", "fp8", "attn", "cpu"]
     for name in which:
-        {"c1": c1, "c2": c2, "c3": c3, "c4": c4, "c5": c5, "pack": pack, "page": page, "sweep": sweep, "dw": dw, "lib": lib, "fp8": fp8, "cpu": cpu,
+        {"c1": c1, "c2": c2, "c3": c3, "c4": c4, "c5": c5, "pack": pack, "page": page, "sweep": sweep, "dw": dw, "lib": lib, "fp8": fp8, "attn": attn, "cpu": cpu,
          "words": words}[name]()

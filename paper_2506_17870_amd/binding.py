@@ -650,6 +650,12 @@ def _row_count(t, ld, width):
     return 0 if there < width else 1 << 62 if ld <= 0 else (there - width) // ld + 1
 
 
+def _rows_fit(name, t, dtype, rows, ld, width):
+    _typed(name, t, dtype)
+    if rows > _row_count(t, ld, width):
+        raise ValueError(f"{name} is too small for {rows} rows, {ld} apart")
+
+
 def make_head_norm(d_q, ldq, d_k, ldk, d_v, ldv, dtype, q_heads, kv_heads, head_dim, q_norm: nq_norm, k_norm: nq_norm, d_freq, rotary, pairs,
                    d_position, d_q_out, ldq_out, d_k_out, ldk_out, cache: nq_kv_cache | None = None, d_slot=None) -> nq_head_job:
     """Descriptor of nq_head_norm calls; None for what is not there.  It keeps everything it names alive."""
@@ -685,11 +691,13 @@ def nq_head_norm(job: nq_head_job, T, stream=None):
 
 
 def nq_cache_read(cache: nq_kv_cache, d_slot, T, d_k, ldk, d_v, ldv, dtype, stream=None):
+    # (of a call of some microseconds the checks are a good part: contiguous rows need no second look)
     _indices("d_slot", d_slot, torch.int64, T)
-    for name, t, ld in (("d_k", d_k, ldk), ("d_v", d_v, ldv)):
-        _typed(name, t, dtype)
-        if isinstance(t, torch.Tensor) and T > _row_count(t, ld, cache.heads * cache.head_dim):
-            raise ValueError(f"{name} is too small for {T} rows, {ld} apart")
+    of = _TORCH_OF.get(dtype)
+    if isinstance(d_k, torch.Tensor) and not (d_k.dtype is of and d_k.is_contiguous() and d_k.numel() >= T * ldk):
+        _rows_fit("d_k", d_k, dtype, T, ldk, cache.heads * cache.head_dim)
+    if isinstance(d_v, torch.Tensor) and not (d_v.dtype is of and d_v.is_contiguous() and d_v.numel() >= T * ldv):
+        _rows_fit("d_v", d_v, dtype, T, ldv, cache.heads * cache.head_dim)
     st = _fast.cache_read(cache, d_slot, T, d_k, ldk, d_v, ldv, dtype, stream if stream is None else _stream(stream))
     if st >= 0:
         return _check(st, "nq_cache_read")
