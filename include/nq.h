@@ -546,8 +546,11 @@ nq_status nq_cache_read(const nq_kv_cache *cache, const int64_t *d_slot, int64_t
  * outputs rounded once.  The order of the sums depends on the sizes alone, so equal calls give equal bits.
  * An infinite or NaN value that a row sees makes its column not finite (which of the two is left open), one that it does not see has no part in it.
  * Begins are not to fall and to end within the rows: what of a sequence lies outside is cut off, and where they fall some rows may be left
- * as they were.  d_o must not overlap the inputs.  (q_rows / 128 + sequences) * q_heads < 2^24 (NQ_ERR_SHAPE).  Rows of q, k and v on 16 bytes
- * are fast. */
+ * as they were or hold anything.  d_o must not overlap the inputs.  (q_rows / 128 + sequences) * q_heads < 2^24 (NQ_ERR_SHAPE).  Rows of q, k and v on 16 bytes
+ * are fast.
+ * d_workspace: NULL, or 16-byte aligned, of nq_attention_prompt_workspace_bytes(...) or more (NQ_ERR_RANGE; 0: it is not used).  With it the keys
+ * of a few rows over many are split over workgroups whose sums it holds until they are joined.  Its contents count only while the call runs,
+ * so calls that may run at the same time need one each. */
 typedef struct {
     const void *d_q, *d_k, *d_v;
     void *d_o;
@@ -556,7 +559,10 @@ typedef struct {
     int64_t sequences, q_rows, k_rows;
     int32_t dtype, q_heads, kv_heads, head_dim, causal;
     float scale;
+    void *d_workspace;
+    uint64_t workspace_bytes;
 } nq_prompt_job;
+size_t nq_attention_prompt_workspace_bytes(int64_t sequences, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
 nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream);
 
 /* The same for one row of each sequence, over the cache: row s of d_q and d_o [sequences][q_heads][head_dim] sees the first

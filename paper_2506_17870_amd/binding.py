@@ -42,7 +42,8 @@ EXPORTS = ["nq_version", "nq_status_string", "nq_packed_bytes", "nq_quantize", "
            "nq_gemm_full", "nq_gemm_part", "nq_gemm_batch_workspace_bytes", "nq_gemm_batch", "nq_gemm_batch_static", "nq_conv_full", "nq_conv_part", "nq_gconv_full", "nq_gconv_part",
            "nq_set_tuning", "nq_profile_next_launch", "nq_profile_last_kernel", "nq_event_create", "nq_event_destroy",
            "nq_event_elapsed_ms", "nq_maxpool_i8", "nq_avgpool_i8", "nq_quantize_fp8", "nq_gemm_fp8", "nq_block_norm",
-           "nq_head_norm", "nq_cache_read", "nq_attention_prompt", "nq_attention_token_workspace_bytes", "nq_attention_token"]
+           "nq_head_norm", "nq_cache_read", "nq_attention_prompt_workspace_bytes", "nq_attention_prompt",
+           "nq_attention_token_workspace_bytes", "nq_attention_token"]
 
 
 class nq_cfg(ctypes.Structure):
@@ -126,7 +127,8 @@ class nq_prompt_job(ctypes.Structure):
     _fields_ = [("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_o", ctypes.c_void_p), ("ldq", ctypes.c_int64),
                 ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64), ("d_q_begin", ctypes.c_void_p), ("d_k_begin", ctypes.c_void_p),
                 ("sequences", ctypes.c_int64), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64), ("dtype", ctypes.c_int32),
-                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float)]
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64)]
 
 
 class nq_token_job(ctypes.Structure):
@@ -187,6 +189,7 @@ _SIGS = {
     "nq_head_norm": (_int, [ctypes.POINTER(nq_head_job), _i64, _vp]),
     "nq_cache_read": (_int, [ctypes.POINTER(nq_kv_cache), _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
     "nq_attention_prompt": (_int, [ctypes.POINTER(nq_prompt_job), _vp]),
+    "nq_attention_prompt_workspace_bytes": (ctypes.c_size_t, [_i64, _i64, _i64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
     "nq_attention_token_workspace_bytes": (ctypes.c_size_t, [_i64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _i64]),
     "nq_attention_token": (_int, [ctypes.POINTER(nq_token_job), _vp]),
 }
@@ -632,6 +635,10 @@ def make_kv_cache(d_k, d_v, d_k_scale=None, d_v_scale=None) -> nq_kv_cache:
     return cache
 
 
+def _bytes_of(t):
+    return t.numel() * t.element_size() if isinstance(t, torch.Tensor) else 0
+
+
 def _ptr_of(t):
     return None if t is None else t.data_ptr()
 
@@ -705,8 +712,9 @@ def nq_cache_read(cache: nq_kv_cache, d_slot, T, d_k, ldk, d_v, ldv, dtype, stre
 
 
 def make_attention_prompt(d_q, ldq, d_k, ldk, d_v, ldv, d_o, ldo, d_q_begin, d_k_begin, sequences, q_rows, k_rows, dtype, q_heads, kv_heads,
-                          head_dim, causal, scale) -> nq_prompt_job:
-    """Descriptor of nq_attention_prompt calls; it keeps everything it names alive."""
+                          head_dim, causal, scale, d_workspace=None) -> nq_prompt_job:
+    """Descriptor of nq_attention_prompt calls; it keeps everything it names alive.  d_workspace: of nq_attention_prompt_workspace_bytes(...)
+    bytes, or None: a tile's keys are one workgroup's."""
     for name, t, ld, heads, rows in (("d_q", d_q, ldq, q_heads, q_rows), ("d_k", d_k, ldk, kv_heads, k_rows), ("d_v", d_v, ldv, kv_heads, k_rows),
                                      ("d_o", d_o, ldo, q_heads, q_rows)):
         _typed(name, t, dtype)
@@ -715,8 +723,8 @@ def make_attention_prompt(d_q, ldq, d_k, ldk, d_v, ldv, d_o, ldo, d_q_begin, d_k
     _indices("d_q_begin", d_q_begin, torch.int32, sequences + 1)
     _indices("d_k_begin", d_k_begin, torch.int32, sequences + 1)
     job = nq_prompt_job(_rows(d_q), _rows(d_k), _rows(d_v), _rows(d_o), ldq, ldk, ldv, ldo, _ptr(d_q_begin), _ptr(d_k_begin), sequences, q_rows,
-                        k_rows, dtype, q_heads, kv_heads, head_dim, int(causal), scale)
-    job._keep = (d_q, d_k, d_v, d_o, d_q_begin, d_k_begin)
+                        k_rows, dtype, q_heads, kv_heads, head_dim, int(causal), scale, _ptr(d_workspace), _bytes_of(d_workspace))
+    job._keep = (d_q, d_k, d_v, d_o, d_q_begin, d_k_begin, d_workspace)
     return job
 
 
@@ -725,6 +733,10 @@ def nq_attention_prompt(job: nq_prompt_job, stream=None):
     if st >= 0:
         return _check(st, "nq_attention_prompt")
     _check(_lib.nq_attention_prompt(ctypes.byref(job), _stream(stream)), "nq_attention_prompt")
+
+
+def nq_attention_prompt_workspace_bytes(sequences, q_rows, k_rows, q_heads, kv_heads, head_dim) -> int:
+    return int(_lib.nq_attention_prompt_workspace_bytes(sequences, q_rows, k_rows, q_heads, kv_heads, head_dim))
 
 
 def nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length) -> int:
@@ -747,8 +759,7 @@ def make_attention_token(d_q, ldq, d_o, ldo, cache: nq_kv_cache, d_table, d_leng
             raise ValueError(f"a row of d_table has {d_table.shape[1]} pages of {cache.page_tokens} tokens, max_length is {max_length}")
         ldtable = d_table.stride(0) if d_table.shape[0] > 1 else d_table.shape[1]
     job = nq_token_job(_rows(d_q), _rows(d_o), ldq, ldo, ctypes.pointer(cache), _rows(d_table), _ptr(d_length), ldtable or 0, sequences, max_length,
-                       dtype, q_heads, scale, 0, _ptr(d_workspace),
-                       d_workspace.numel() * d_workspace.element_size() if isinstance(d_workspace, torch.Tensor) else 0)
+                       dtype, q_heads, scale, 0, _ptr(d_workspace), _bytes_of(d_workspace))
     job._keep = (d_q, d_o, cache, d_table, d_length, d_workspace)
     return job
 

@@ -39,6 +39,8 @@ struct PromptParams {
     uint32_t flip;                              // sign bits for q where the scale is negative
     int32_t first_half;                         // tiles of which one is on each compute unit before any has two
     int32_t zero;                               // a scale of 0
+    float *partial;                             // sums of o [pieces][q_rows][q_heads][D], then m and l [pieces][q_rows][q_heads][2]
+    int32_t pieces;                             // workgroups that share the keys of a tile of rows; 1: they write the rows themselves
 };
 
 template <typename T>
@@ -202,14 +204,15 @@ __device__ __forceinline__ Rows rows_alone(const PromptParams &p, int w)
 }
 
 // DIRECT: K and V travel global -> LDS by direct loads a step ahead, which want rows on 16 bytes; else through registers, when they are used.
-template <typename T, int DP, Share SHARE, bool DIRECT>
+// DEALT: the keys that a tile of rows sees are dealt to p.pieces workgroups, which leave their sums to k_prompt_join.
+template <typename T, int DP, Share SHARE, bool DIRECT, bool DEALT>
 __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == SHARE_KEYS || DP > 64 ? 2 : 3) k_attention_prompt(const PromptParams p)
 {
     constexpr bool SPLIT = SHARE == SHARE_KEYS;
     constexpr int PITCH = pitch_of(DP), KEYS = keys_of(DP, SHARE), STAGES = stages_of(DP, SHARE), U = SPLIT ? 1 : KEYS / 32, KJ = DP / 16, DT = DP / 32;
     constexpr int WAVES = waves_of(SHARE), THREADS = WAVES * 64, ROWS = SHARE == SHARE_ROWS ? 128 : 32, TILE = KEYS * PITCH;
     constexpr int PIECES = DIRECT ? PITCH / 8 : DP / 8, CH = KEYS * PIECES / THREADS;  // pieces of 16 bytes of a row; of a thread and tile
-    constexpr bool THROUGH = SHARE == SHARE_ROWS && DP <= 128;           // Q and O travel through LDS, too
+    constexpr bool THROUGH = SHARE == SHARE_ROWS && DP <= 128;           // Q travels through LDS, too, and O where it leaves as rows
     constexpr int SUMS = SPLIT ? 1024 + 2 * 64 * (DP / 2 + 1) * 4 : 0;    // bytes for the waves' sums
     constexpr bool F16 = __is_same(T, _Float16);
     constexpr uint32_t EXP = F16 ? 0x7c00 : 0x7f80;                      // the exponent of infinities and NaN
@@ -231,6 +234,12 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
     const int row0 = first * ROWS, off = p.causal ? Lk - Lq : Lk;        // row i sees the keys j <= i + off (without causal: all)
     const int end = min(Lk, max(0, min(row0 + ROWS, Lq) + off));         // keys that any row sees
     const int hk = (int)h / p.group;
+    int from = 0, to = end;                                              // this workgroup's keys
+    if constexpr (DEALT) {
+        const int size = ((end + p.pieces - 1) / p.pieces + KEYS - 1) / KEYS * KEYS;
+        from = min((int)blockIdx.y * size, end);
+        to = min(from + size, end);
+    }
 
     const T *k_base = static_cast<const T *>(p.k) + (int64_t)k0 * p.ldk + (int64_t)hk * p.D;
     const T *v_base = static_cast<const T *>(p.v) + (int64_t)k0 * p.ldv + (int64_t)hk * p.D;
@@ -314,7 +323,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         __syncthreads();
     };
 
-    if (end > 0) fetch(0, lds);
+    if (from < to) fetch(from, lds);
     // this wave's rows, this lane's row
     const int first_row = row0 + (SPLIT ? 0 : wave * 32), row = first_row + r;
     uint4 q[KJ];
@@ -355,7 +364,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
 
     // keys that some row of the wave sees, that all of them see; the last that this lane's row sees
-    const int wave_end = first_row < Lq ? min(Lk, max(0, min(first_row + 32, Lq) + off)) : 0, seen_by_all = min(Lk, first_row + 1 + off);
+    const int wave_end = first_row < Lq ? min(to, max(0, min(first_row + 32, Lq) + off)) : 0, seen_by_all = min(Lk, first_row + 1 + off);
     const int row_last = min(Lk - 1, row + off);
     // V^T of the columns 32 d .., keys 16 e + 4 half + (0 .. 3) and eight further on, as the scores lie
     auto v_fragment = [&](const uint16_t *vt, int d, int e) __attribute__((always_inline)) {
@@ -367,7 +376,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
     // One step: the keys from j0 on, whose tiles are kt and vt.  The two stages are named apart so that the compiler knows that what is on its
     // way into one does not hold up reading the other.
     auto step = [&](uint16_t *__restrict kt, uint16_t *__restrict vt, uint16_t *__restrict next, int j0) __attribute__((always_inline)) {
-        if (STAGES == 2 && j0 + KEYS < end) fetch(j0 + KEYS, next);
+        if (STAGES == 2 && j0 + KEYS < to) fetch(j0 + KEYS, next);
         if constexpr (SPLIT) {
             j0 += wave * 32;
             kt += wave * 32 * PITCH;
@@ -445,16 +454,16 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         }
         __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
     };
-    for (int j0 = 0, stage = 0; j0 < end; j0 += KEYS, stage ^= STAGES - 1) {
+    for (int j0 = from, stage = 0; j0 < to; j0 += KEYS, stage ^= STAGES - 1) {
         arrived(stage, j0);                                              // (and nobody reads the other stage any more)
         step(lds + stage * 2 * TILE, lds + stage * 2 * TILE + TILE, lds + (stage ^ 1) * 2 * TILE, j0);
-        if (STAGES == 1 && j0 + KEYS < end) {
+        if (STAGES == 1 && j0 + KEYS < to) {
             __builtin_amdgcn_s_waitcnt(0xc07f);                          // (what is read is in registers before anything is on its way into its place)
             __syncthreads();
             fetch(j0 + KEYS, lds);
         }
     }
-    const bool odd = end > partial && (odd_of[0] | odd_of[WAVES / 4] | odd_of[WAVES / 2] | odd_of[WAVES - 1]);
+    const bool odd = to > partial && (odd_of[0] | odd_of[WAVES / 4] | odd_of[WAVES / 2] | odd_of[WAVES - 1]);
 
     if constexpr (SPLIT) {
         // ---- the four waves' sums, by way of LDS: a lane's are of the same row and columns in all of them
@@ -465,6 +474,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         const float top = fmaxf(fmaxf(tops[lane], tops[64 + lane]), fmaxf(tops[128 + lane], tops[192 + lane]));
         const float w = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top);
         l *= w;
+        m = top;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -494,7 +504,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
     }
 
     if (odd) {
-        for (int j = max(partial, 0) / KEYS * KEYS; j < end; ++j) {
+        for (int j = max(max(partial, 0) / KEYS * KEYS, from); j < to; ++j) {
             const uint16_t *values = reinterpret_cast<const uint16_t *>(v_base + (int64_t)j * p.ldv);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -510,9 +520,25 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
 
     // ---- lane: row r, columns 32 d + 8 (i / 4) + 4 half + i % 4
     const bool any = row_last >= 0;
+    if constexpr (DEALT) {
+        l = across32(l, true);
+        if (row >= Lq) return;
+        const int64_t at = ((int64_t)blockIdx.y * p.q_rows + q0 + row) * p.Hq + h;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int col = 32 * d + 2 * i + 4 * half;
+                const float y[4] = {o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+                if (col < p.D) __builtin_memcpy(__builtin_assume_aligned(p.partial + at * p.D + col, 16), y, 16);
+            }
+        if (half == 0)                                                   // (a sum of -1: the row sees no key)
+            reinterpret_cast<f8_f2 *>(p.partial + (int64_t)p.pieces * p.q_rows * p.Hq * p.D)[at] = f8_f2{m, any ? l : -1.0f};
+        return;
+    }
     // (a row whose every score is -inf has a sum of 0 and comes out as NaN, as its definition does; a row without keys as 0)
     const float w = 1.0f / across32(l, true);
-    T *const to = static_cast<T *>(p.o) + (int64_t)(q0 + first_row) * p.ldo + (int64_t)h * p.D;     // the wave's first row
+    T *const out_row = static_cast<T *>(p.o) + (int64_t)(q0 + first_row) * p.ldo + (int64_t)h * p.D;     // the wave's first row
     if constexpr (THROUGH) {
         // whole rows leave, 16 bytes a lane (the second stage of the two is free where the last step was of the first, else the first)
         uint16_t *const out = lds + (end > 0 && ((end - 1) / KEYS) % 2 ? 0 : 2 * TILE) + wave * 32 * PITCH;
@@ -531,7 +557,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         for (int i = 0; i < PER / 2; ++i) {
             const int at = (i * 64 + lane) / PER, d = (i * 64 + lane) % PER * 8;
             const uint4 y = *reinterpret_cast<const uint4 *>(out + at * PITCH + k_piece<PITCH>(at, d >> 3) * 8);
-            if (first_row + at < Lq && d < p.D) __builtin_memcpy(to + at * p.ldo + d, &y, 16);
+            if (first_row + at < Lq && d < p.D) __builtin_memcpy(out_row + at * p.ldo + d, &y, 16);
         }
     } else {
         if (row >= Lq) return;
@@ -541,9 +567,35 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
             for (int i = 0; i < 16; i += 4) {
                 const int col = 32 * d + 2 * i + 4 * half;
                 const uint2 y = any ? make_uint2(pair16<T>(o[d][i] * w, o[d][i + 1] * w), pair16<T>(o[d][i + 2] * w, o[d][i + 3] * w)) : make_uint2(0, 0);
-                if (col < p.D) __builtin_memcpy(to + r * p.ldo + col, &y, 8);
+                if (col < p.D) __builtin_memcpy(out_row + r * p.ldo + col, &y, 8);
             }
     }
+}
+
+// Joins the pieces of a row and head: a thread for four columns.  Rows in front of the first sequence and behind the last have none.
+template <typename T>
+__global__ void __launch_bounds__(256) k_prompt_join(const PromptParams p, const Divider by_quads)
+{
+    const uint32_t id = blockIdx.x * 256u + threadIdx.x, at = divide(id, by_quads), c = (id - at * by_quads.d) * 4;     // at: row and head
+    const uint32_t row = divide(at, p.by_heads), h = at - row * p.by_heads.d;
+    if (row >= (uint32_t)p.q_rows || (int)row < p.q_begin[0] || (int)row >= p.q_begin[p.sequences]) return;
+    const int64_t step = (int64_t)p.q_rows * p.Hq;
+    const f8_f2 *ml = reinterpret_cast<const f8_f2 *>(p.partial + p.pieces * step * p.D) + at;
+    float top = -__builtin_inff(), l = 0.0f;
+    for (int z = 0; z < p.pieces; ++z) top = fmaxf(top, ml[z * step][0]);
+    float o[4] = {0, 0, 0, 0};
+    for (int z = 0; z < p.pieces; ++z) {
+        const f8_f2 x = ml[z * step];
+        const float w = x[0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[0] - top);
+        float y[4];
+        __builtin_memcpy(y, __builtin_assume_aligned(p.partial + (z * step + at) * p.D + c, 16), 16);
+        l = fmaf(x[1], w, l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(y[i], w, o[i]);
+    }
+    const float r = 1.0f / l;
+    const uint2 y = ml[0][1] == -1.0f ? make_uint2(0, 0) : make_uint2(pair16<T>(o[0] * r, o[1] * r), pair16<T>(o[2] * r, o[3] * r));
+    __builtin_memcpy(static_cast<T *>(p.o) + (int64_t)row * p.ldo + (int64_t)h * p.D + c, &y, 8);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------
@@ -557,20 +609,47 @@ static nq_status launch_prompt(PromptParams &p, bool direct, hipStream_t s)
     auto launch = [&](auto kernel, std::atomic<uint64_t> &granted) {
         const nq_status st = grant_lds(kernel, BYTES, granted);
         if (st != NQ_OK) return st;
-        kernel<<<(unsigned)p.tiles * (unsigned)p.Hq, waves_of(SHARE) * 64, BYTES, s>>>(p);
+        kernel<<<dim3((unsigned)p.tiles * (unsigned)p.Hq, p.pieces), waves_of(SHARE) * 64, BYTES, s>>>(p);
         return launch_status();
     };
-    static std::atomic<uint64_t> granted[2] = {};
+    static std::atomic<uint64_t> granted[3] = {};
+    if constexpr (SHARE != SHARE_ALONE) {
+        if (p.pieces > 1) {
+            const nq_status st = launch(k_attention_prompt<T, DP, SHARE, true, true>, granted[2]);
+            if (st != NQ_OK) return st;
+            k_prompt_join<T><<<(unsigned)ceil_div((int64_t)p.q_rows * p.Hq * (p.D / 4), 256), 256, 0, s>>>(p, make_divider((uint32_t)p.D / 4));
+            return launch_status();
+        }
+    }
     if constexpr (SHARE == SHARE_ALONE && DP > 128)                      // (by way of registers, of which a wave alone has too few there)
-        return launch(k_attention_prompt<T, DP, SHARE, true>, granted[1]);
+        return launch(k_attention_prompt<T, DP, SHARE, true, false>, granted[1]);
     else
-        return direct ? launch(k_attention_prompt<T, DP, SHARE, true>, granted[1]) : launch(k_attention_prompt<T, DP, SHARE, false>, granted[0]);
+        return direct ? launch(k_attention_prompt<T, DP, SHARE, true, false>, granted[1]) : launch(k_attention_prompt<T, DP, SHARE, false, false>, granted[0]);
+}
+
+// Tiles of 32 rows, whose keys the waves share, for few rows to a sequence over keys that are dealt to several workgroups, too.
+static bool few_rows(int64_t sequences, int64_t q_rows, int head_dim) { return head_dim <= 128 && q_rows <= 64 * sequences; }
+
+// Workgroups to a tile of rows, 1: it is not split.  As many as fill two to a compute unit, each with PR_LEAST keys or more, on average.  Whole and
+// split, 32 heads of 128: 16 rows over 2016 keys 24.6 and 16.2 us, over 65552 753 and 88.6 (268 MB, 53 us of a copy's rate), 256 over 4256 46.1 and
+// 36.7, 512 over 33280 406 and 277; 16 heads of 256, 16 rows over 32784 1260 and 98; 2 heads, 2571 causal rows 29.9 and 23.6.
+constexpr int PR_LEAST = 512, PR_MOST_PIECES = 32;
+static int pieces_of(int64_t sequences, int64_t q_rows, int64_t k_rows, int q_heads, int head_dim)
+{
+    const int64_t tiles = (ceil_div(q_rows, few_rows(sequences, q_rows, head_dim) ? 32 : 128) + sequences - 1) * q_heads;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((head_dim <= 128 ? 512 : 256) / tiles, k_rows / sequences / PR_LEAST), PR_MOST_PIECES));
 }
 
 template <typename T, int DP>
 static nq_status launch_share(PromptParams &p, bool direct, hipStream_t s)
 {
     const int64_t S = p.sequences, blocks = (p.q_rows / 32 + S) * p.Hq;
+    if (p.pieces > 1) {
+        if constexpr (DP <= 128) {
+            if (few_rows(S, p.q_rows, DP)) return launch_prompt<T, DP, SHARE_KEYS>(p, direct, s);
+        }
+        return launch_prompt<T, DP, SHARE_ROWS>(p, direct, s);
+    }
     // Sequences of up to 32 rows and 192 keys, on average, a wave each where four to a workgroup would take more than a round, or have nothing to
     // share: 256 of 16 rows, 32 heads of 128, 29.8 us, 128 rows to a workgroup 113; 1000 of up to 5 91.8 and 359; 64 of up to 32 15.4 and 29.2; 2 of up
     // to 30, 8 heads, 6.0 and 7.3; 10 of up to 10, 32 heads of 192, 9.0 and 14.4; 13 rows alone, 4 heads of 256, 10.0 and 9.2
@@ -598,6 +677,14 @@ static nq_status run_prompt(PromptParams &p, bool direct, hipStream_t s)
 }  // namespace nq
 
 using namespace nq;
+
+extern "C" size_t nq_attention_prompt_workspace_bytes(int64_t sequences, int64_t q_rows, int64_t k_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
+{
+    if (sequences < 1 || q_rows < 1 || k_rows < 1 || sequences > ATT_MAX_ROWS || q_rows > ATT_MAX_ROWS || k_rows > ATT_MAX_ROWS) return 0;
+    if (check_heads(q_heads, kv_heads, head_dim) != NQ_OK || q_heads % kv_heads) return 0;
+    const int pieces = pieces_of(sequences, q_rows, k_rows, q_heads, head_dim);
+    return pieces > 1 ? (size_t)pieces * q_rows * q_heads * (head_dim + 2) * sizeof(float) : 0;
+}
 
 extern "C" nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream)
 {
@@ -647,5 +734,13 @@ extern "C" nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream)
     // rows on 16 bytes, a tile's offsets within 31 bits
     const bool direct = aligned16(j.d_q) && aligned16(j.d_k) && aligned16(j.d_v) && j.ldq % 8 == 0 && j.ldk % 8 == 0 && j.ldv % 8 == 0 &&
                         std::max(std::max(j.ldq, j.ldk), j.ldv) < (int64_t(1) << 23);
+    p.partial = static_cast<float *>(j.d_workspace);
+    p.pieces = 1;
+    if (j.d_workspace) {
+        if (!aligned16(j.d_workspace)) return NQ_ERR_ALIGN;
+        if (j.workspace_bytes < nq_attention_prompt_workspace_bytes(j.sequences, j.q_rows, j.k_rows, j.q_heads, j.kv_heads, j.head_dim)) return NQ_ERR_RANGE;
+        // (rows that are not on 16 bytes: not split)
+        if (direct && j.k_rows > 0) p.pieces = pieces_of(j.sequences, j.q_rows, j.k_rows, j.q_heads, j.head_dim);
+    }
     return j.dtype == NQ_DT_F16 ? run_prompt<_Float16>(p, direct, (hipStream_t)stream) : run_prompt<bf16_t>(p, direct, (hipStream_t)stream);
 }

@@ -8,7 +8,7 @@ import pytest
 from test_fp8_launches import A, ROOT, Stub, stub  # noqa: F401
 
 
-@pytest.mark.parametrize("part", ["sizes", "grants", "pieces"])
+@pytest.mark.parametrize("part", ["sizes", "grants", "pieces", "dealt"])
 def test_launches(stub, part):  # noqa: F811
     env = dict(os.environ, PYTHONPATH=os.pathsep.join((ROOT, os.path.join(ROOT, "tests"))))
     r = subprocess.run([sys.executable, os.path.abspath(__file__), stub, part], capture_output=True, text=True, env=env, timeout=300)
@@ -104,6 +104,46 @@ def pieces(nq, stub):  # noqa: F811
         else:
             assert len(got) == 1 and got[0][1] == blocks * S
         assert not stub.take()
+
+
+def prompt_job(nq, S, q_rows, k_rows, Hq, Hkv, D, q=A):
+    job = nq.make_attention_prompt(q, Hq * D, A, Hkv * D, A, Hkv * D, A, Hq * D, A, A, S, q_rows, k_rows, 2, Hq, Hkv, D, True, 0.1, A)
+    job.workspace_bytes = nq.nq_attention_prompt_workspace_bytes(S, q_rows, k_rows, Hq, Hkv, D)
+    return job
+
+
+def dealt(nq, stub):  # noqa: F811
+    """Prompts whose keys are dealt to workgroups: as many as the workspace was sized for, and a join; without a workspace, and where rows are not on
+    16 bytes, one launch."""
+    for S, q_rows, k_rows, Hq, Hkv, D in ((1, 16, 4016, 32, 8, 128), (1, 1, 1 << 20, 1, 1, 64), (4, 300, 20000, 8, 8, 96), (1, 512, 32768, 32, 8, 128), (1, 100, 5000, 4, 4, 256),
+                                          (1, 8192, 8192, 32, 8, 128), (1000, 5000, 9000, 8, 8, 64), (1, 32768, 1 << 29, 1, 1, 8), (1, 1, 512, 1, 1, 8)):
+        job = prompt_job(nq, S, q_rows, k_rows, Hq, Hkv, D)
+        nq.nq_attention_prompt(job, stream=0)
+        got = stub.take()
+        if not job.workspace_bytes:
+            assert len(got) == 1
+            continue
+        pieces = job.workspace_bytes // (q_rows * Hq * (D + 2) * 4)
+        assert len(got) == 2 and 2 <= pieces <= 32 and got[0][1] % pieces == 0 and got[0][1] // pieces >= -(-q_rows // 128) * Hq
+        assert got[1][1] * 256 >= q_rows * Hq * D // 4
+        for q in (A + 2,):
+            nq.nq_attention_prompt(prompt_job(nq, S, q_rows, k_rows, Hq, Hkv, D, q), stream=0)
+            assert len(stub.take()) == 1
+        for field, value, status in (("workspace_bytes", job.workspace_bytes - 1, nq.NQ_ERR_RANGE), ("d_workspace", A + 8, nq.NQ_ERR_ALIGN)):
+            was = getattr(job, field)
+            setattr(job, field, value)
+            try:
+                nq.nq_attention_prompt(job, stream=0)
+            except nq.NQError as e:
+                assert e.status == status
+            else:
+                raise AssertionError(f"{field} was taken")
+            setattr(job, field, was)
+        job.d_workspace, job.workspace_bytes = None, 0
+        nq.nq_attention_prompt(job, stream=0)
+        assert len(stub.take()) == 1
+    assert stub.v["refused"].value == 0
+    assert nq.nq_attention_prompt_workspace_bytes(0, 1, 1, 1, 1, 64) == 0 and nq.nq_attention_prompt_workspace_bytes(1, 16, 4000, 3, 2, 64) == 0
 
 
 if __name__ == "__main__":

@@ -392,3 +392,77 @@ def test_short_prompts_with_values_that_are_not_finite(nq, D, gap):
         part = got[s * n:(s + 1) * n, h * D:(h + 1) * D]
         check_prompt(part[:15], q[:15], k[:15], v[:15], begins([15]), None, 1, 1, D, BF16, True, 0.1)
         assert torch.isnan(part[15:]).all()
+
+
+DEALT = [
+    # rows, keys, Hq, Hkv, D, dtype, causal, scale
+    ([16], [4016], 32, 8, 128, BF16, True, 0.1),
+    ([1], [9000], 2, 1, 64, F16, True, 0.2),
+    ([40, 0, 30], [2000, 1500, 3000], 4, 2, 96, BF16, True, -0.1),
+    ([100], [5000], 6, 2, 72, F16, False, 0.1),
+    ([300], [4100], 4, 1, 128, BF16, True, 0.1),
+    ([129, 50], [3000, 20], 2, 2, 64, F16, True, 0.1),
+    ([70], [2048], 2, 1, 256, BF16, True, 0.08),
+    ([20, 9, 60], [1500, 1600, 0], 2, 2, 192, F16, False, 0.08),
+    ([700], [700], 1, 1, 80, BF16, True, 0.1),
+    ([1100], [1100], 2, 1, 128, F16, True, 0.0),
+    ([1500], [1500], 1, 1, 80, BF16, True, 0.1),
+]
+
+
+def run_dealt(nq, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, scale):
+    S, T, K = len(q_begin) - 1, q.shape[0], k.shape[0]
+    need = nq.nq_attention_prompt_workspace_bytes(S, T, K, Hq, Hkv, D)
+    assert need > 0 or K < 1024 * S, "not split"                # (fewer keys than two pieces have: one workgroup all the same)
+    workspace = torch.full((need + 64,), 0xff, dtype=torch.uint8, device="cuda")         # (NaN, wherever it is read before it is written)
+    out = torch.full((T, Hq * D), 5.0, dtype=dtype, device="cuda")
+    job = nq.make_attention_prompt(q.cuda(), Hq * D, k.cuda(), Hkv * D, v.cuda(), Hkv * D, out, Hq * D, q_begin.cuda(), k_begin.cuda(), S, T, K,
+                                   dt(nq, dtype), Hq, Hkv, D, causal, scale, workspace[:need])
+    nq.nq_attention_prompt(job)
+    got = out.cpu()
+    assert (workspace[need:] == 0xff).all()
+    nq.nq_attention_prompt(job)
+    assert torch.equal(out.cpu().view(torch.int16), got.view(torch.int16)), "equal calls differ"
+    return got
+
+
+@pytest.mark.parametrize("case", DEALT, ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}-{c[3]}-{c[4]}".replace(" ", ""))
+def test_keys_dealt_to_workgroups(nq, case):
+    rows, keys, Hq, Hkv, D, dtype, causal, scale = case
+    q_begin, k_begin = begins(rows, 2), begins(keys, 1)
+    T, K = int(q_begin[-1]) + 3, int(k_begin[-1]) + 1
+    q, k, v = (randn(180 + i, *s).to(dtype) for i, s in enumerate(((T, Hq * D), (K, Hkv * D), (K, Hkv * D))))
+    got = run_dealt(nq, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, scale)
+    check_prompt(got, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, scale)
+    assert (got[:2] == 5).all() and (got[T - 3:] == 5).all(), "rows of no sequence have changed"
+
+
+@pytest.mark.parametrize("n,D", [(150, 64), (30, 128), (150, 128), (150, 256)])
+def test_keys_dealt_with_values_that_are_not_finite(nq, n, D):
+    """What a row does not see does not reach it, in whichever piece it lies."""
+    K, H = 2300, 2
+    q, k, v = (randn(190 + i, m, D) for i, m in enumerate((n, K, K)))
+    a = K - n                                                  # row i sees the keys up to a + i
+    v[a + 7, 5], v[a + 9, 6], v[a + 11, 7] = float("inf"), -float("inf"), float("nan")
+    v[a + 20] = float("nan")
+    k[a + 15, 0] = float("nan")
+    q, k, v = (x.to(BF16) for x in (q, k, v))
+    got = run_dealt(nq, q.repeat(1, H), k, v, begins([n]), begins([K]), H, 1, D, BF16, True, 0.1)
+    for h in range(H):
+        part = got[:, h * D:(h + 1) * D]
+        check_prompt(part[:15], q[:15], k[:a + 15], v[:a + 15], begins([15]), begins([a + 15]), 1, 1, D, BF16, True, 0.1)
+        assert torch.isnan(part[15:]).all()
+
+
+def test_keys_dealt_scores_of_no_weight(nq):
+    """Pieces whose every score is -inf weigh nothing beside others; without others the row is NaN, and 0 where it sees no key at all."""
+    D, K = 64, 2500
+    q, k, v = torch.ones(40, D), randn(200, K, D) * 0.1, randn(201, K, D)
+    k[:1800, 0] = -float("inf")
+    q, k, v = (x.to(BF16) for x in (q, k, v))
+    got = run_dealt(nq, q, k, v, begins([20, 20]), torch.tensor([0, 1500, 2500], dtype=torch.int32), 1, 1, D, BF16, False, 0.1)
+    assert torch.isnan(got[:20]).all()
+    o, bound = ref.attention(q[20:].double(), k[1800:].double(), v[1800:].double(), 0.1, torch.ones(20, 700, dtype=torch.bool), BF16, True)
+    ref.check(got[20:], o, bound)
+    got = run_dealt(nq, q, k[1800:].repeat(5, 1), v[1800:].repeat(5, 1), begins([39, 1]), torch.tensor([0, 0, 3000], dtype=torch.int32), 1, 1, D, BF16, False, 0.1)
+    assert (got[:39] == 0).all() and torch.isfinite(got[39]).all()
