@@ -650,10 +650,13 @@ static nq_status launch_share(PromptParams &p, bool direct, hipStream_t s)
         }
         return launch_prompt<T, DP, SHARE_ROWS>(p, direct, s);
     }
-    // Sequences of up to 32 rows and 192 keys, on average, a wave each where four to a workgroup would take more than a round, or have nothing to
-    // share: 256 of 16 rows, 32 heads of 128, 29.8 us, 128 rows to a workgroup 113; 1000 of up to 5 91.8 and 359; 64 of up to 32 15.4 and 29.2; 2 of up
-    // to 30, 8 heads, 6.0 and 7.3; 10 of up to 10, 32 heads of 192, 9.0 and 14.4; 13 rows alone, 4 heads of 256, 10.0 and 9.2
-    if (p.q_rows <= 32 * S && p.k_rows <= 192 * S && (DP > 128 ? direct && S * p.Hq > 256 : S * p.Hq > 512 || p.k_rows <= 64 * S))
+    // A wave to each 32 rows where four waves have nothing to share, or their workgroups take more than a round: sequences of up to 32 rows and 192
+    // keys, on average (256 of 16 rows, 32 heads of 128, 29.8 us, 128 rows to a workgroup 113; 1000 of up to 5 91.8 and 359; 10 of up to 10, 32 heads of
+    // 192, 9.0 and 14.4, but 13 rows alone, 4 heads of 256, 10.0 and 9.2), or of up to 64 rows and keys (100 of 60 43.2 and 55.0, 20 of 50 10.7 and
+    // 15.0, 2 of up to 30, 8 heads, 6.0 and 7.3, but one of 33 6.8 and 6.5)
+    const bool many = S * p.Hq > (DP > 128 ? 256 : 512);
+    if (DP <= 128 ? (p.k_rows <= 192 * S && p.q_rows <= 32 * S && many) || (p.k_rows <= 64 * S && p.q_rows <= (S * p.Hq >= 128 ? 64 : 32) * S)
+                  : p.k_rows <= 192 * S && p.q_rows <= 32 * S && many && direct)
         return launch_prompt<T, DP, SHARE_ALONE>(p, direct, s);
     // 32 rows to a workgroup and the keys dealt to its waves, where that still makes one round or two of workgroups and there are keys to deal: 512
     // rows of 32 heads 11.8 us, 128 rows to a workgroup 14.8; 1024 of 8 15.7 and 23.2; 1024 of 32 28.8 and 25.0; 64 rows over 173 keys 9.2 and 8.6; where a

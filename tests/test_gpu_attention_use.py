@@ -355,6 +355,7 @@ SHORT = [
     ([1 + 5 * i % 40 for i in range(50)], None, 12, 3, 128, BF16, True, 0.1, 0),
     ([i % 23 for i in range(300)], None, 4, 4, 64, F16, True, 0.15, 0),
     ([5 * i % 37 for i in range(90)], [7 * i % 150 for i in range(90)], 8, 2, 96, BF16, True, -0.1, 0),
+    ([33 + i % 31 for i in range(20)], None, 8, 2, 128, F16, False, 0.1, 0),
     ([200] + [3] * 60, [200] + [100] * 60, 9, 3, 72, F16, False, 0.1, 4),
     ([2, 17, 0, 30], [90, 17, 8, 31], 2, 1, 128, F16, True, 0.1, 3),
     ([1 + 7 * i % 33 for i in range(30)], [40 + i for i in range(30)], 10, 5, 192, BF16, True, 0.08, 0),
@@ -466,3 +467,32 @@ def test_keys_dealt_scores_of_no_weight(nq):
     ref.check(got[20:], o, bound)
     got = run_dealt(nq, q, k[1800:].repeat(5, 1), v[1800:].repeat(5, 1), begins([39, 1]), torch.tensor([0, 0, 3000], dtype=torch.int32), 1, 1, D, BF16, False, 0.1)
     assert (got[:39] == 0).all() and torch.isfinite(got[39]).all()
+
+
+def test_keys_dealt_captured(nq):
+    """A split call in a graph, replayed on other lengths with eager work on the same workspace between: each replay gives the bits of the eager call."""
+    H, D, T, K = 4, 128, 60, 4000
+    q, k, v = (randn(210 + i, n, H * D).to(BF16).cuda() for i, n in enumerate((T, K, K)))
+    out = torch.zeros(T, H * D, dtype=BF16, device="cuda")
+    q_begin, k_begin = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 20, 60], [0, 1000, 4000]))
+    workspace = torch.empty(nq.nq_attention_prompt_workspace_bytes(2, T, K, H, H, D), dtype=torch.uint8, device="cuda")
+    assert workspace.numel() > 0
+    job = nq.make_attention_prompt(q, H * D, k, H * D, v, H * D, out, H * D, q_begin, k_begin, 2, T, K, nq.NQ_DT_BF16, H, H, D, True, 0.1, workspace)
+    nq.nq_attention_prompt(job)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nq.nq_attention_prompt(job)
+    for a, b in (([0, 20, 60], [0, 1000, 4000]), ([0, 0, 60], [0, 3000, 3500]), ([5, 50, 55], [0, 10, 4000]), ([0, 60, 60], [0, 4000, 4000])):
+        q_begin.copy_(torch.tensor(a, dtype=torch.int32))
+        k_begin.copy_(torch.tensor(b, dtype=torch.int32))
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        workspace.fill_(0xff)
+        out.fill_(9.0)
+        nq.nq_attention_prompt(job)
+        torch.cuda.synchronize()
+        assert torch.equal(out, got), (a, b)
+        check_prompt(got.cpu(), q.cpu(), k.cpu(), v.cpu(), torch.tensor(a), torch.tensor(b), H, H, D, BF16, True, 0.1)
