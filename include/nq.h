@@ -543,7 +543,7 @@ nq_status nq_cache_read(const nq_kv_cache *cache, const int64_t *d_slot, int64_t
  * queries': a cached prefix).  A row that sees no key is 0.  Rows of q that belong to no sequence are left as they were.
  * d_q, d_o [q_rows][q_heads][head_dim], d_k, d_v [k_rows][kv_heads][head_dim] of dtype, f16 or bf16 (fp32: NQ_ERR_UNSUPPORTED).
  * Sums and softmax in fp32, the probabilities (relative to a row's largest) rounded to dtype for the second product,
- * outputs rounded once.  The order of the sums depends on the sizes alone, so equal calls give equal bits.
+ * outputs rounded once.  The order of the sums depends on the sizes (and on there being a workspace) alone, so equal calls give equal bits.
  * An infinite or NaN value that a row sees makes its column not finite (which of the two is left open), one that it does not see has no part in it.
  * Begins are not to fall and to end within the rows: what of a sequence lies outside is cut off, and where they fall some rows may be left
  * as they were or hold anything.  d_o must not overlap the inputs.  (q_rows / 128 + sequences) * q_heads < 2^24 (NQ_ERR_SHAPE).  Rows of q, k and v on 16 bytes
