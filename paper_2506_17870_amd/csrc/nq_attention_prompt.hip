@@ -276,8 +276,11 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         }
     };
     // A key that only some rows see has probability 0 in the others, and 0 times an infinite or NaN value is no 0.  So such values become zeros
-    // in the tiles of those keys, and are added at the end to the rows that see them.
-    const int partial = row0 + 1 + off;                                  // keys that all rows see
+    // in the tiles of those keys, and are added at the end to the rows that see them.  Where all rows see all keys there are no such tiles, also where the
+    // last one has places behind the keys (zeros): a value that every row sees stays.
+    int partial = row0 + 1 + off;                                        // keys that all rows see, where some rows see more
+    if (partial >= to) partial = NOWHERE;
+    asm("" : "+s"(partial));                                             // (one number, compared once a step: else the compiler compares twice, 3 % at 256 columns)
     uint32_t *const odd_of = reinterpret_cast<uint32_t *>(lds + (STAGES * 2 * TILE > SUMS / 2 ? STAGES * 2 * TILE : SUMS / 2));    // for each wave: whether it found such values
     if (lane == 0) odd_of[wave] = 0;
     auto tame = [&](uint4 &w) __attribute__((always_inline)) {
@@ -463,7 +466,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
             fetch(j0 + KEYS, lds);
         }
     }
-    const bool odd = to > partial && (odd_of[0] | odd_of[WAVES / 4] | odd_of[WAVES / 2] | odd_of[WAVES - 1]);
+    const bool odd = partial != NOWHERE && (odd_of[0] | odd_of[WAVES / 4] | odd_of[WAVES / 2] | odd_of[WAVES - 1]);
 
     if constexpr (SPLIT) {
         // ---- the four waves' sums, by way of LDS: a lane's are of the same row and columns in all of them

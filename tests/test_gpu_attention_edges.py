@@ -1,0 +1,92 @@
+"""The attention operators on the GPU at values and places where the definition is easily lost: infinities and NaN that a row sees, values whose squares
+are too small, begins outside the rows, memory that another stream fills."""
+import pytest
+import torch
+
+import attention_reference as ref
+from test_gpu_attention import BF16, E4M3, F16, F32, TokenCase, begins, check_prompt, dt, randn, run_prompt
+from test_gpu_attention_use import run_dealt
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def nq():
+    import paper_2506_17870_amd as nq
+    assert torch.cuda.is_available()
+    return nq
+
+
+def check_reached(got, o, bound, reached, what=""):
+    """got against (o, bound) in finite columns, not finite (infinite or NaN, which is left open) in those that a value that is not finite reaches."""
+    assert not torch.isfinite(got[reached]).any(), f"{what}: a value that is seen has no part"
+    ref.check(torch.where(reached, torch.zeros_like(got), got), torch.where(reached, 0.0, o), bound, what)
+
+
+def check_seen(got, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, scale, heads, sequences):
+    qb, kb = q_begin.tolist(), k_begin.tolist()
+    for s in sequences:
+        n, m = qb[s + 1] - qb[s], kb[s + 1] - kb[s]
+        seen = torch.ones(n, m, dtype=torch.bool)
+        if causal:
+            seen = torch.arange(m)[None] <= torch.arange(n)[:, None] + (m - n)
+        for h in heads:
+            g = h // (Hq // Hkv)
+            part = lambda x, b, i: x[b[s]:b[s + 1], i * D:i * D + D].double()  # noqa: E731
+            value = part(v, kb, g)
+            bad = ~torch.isfinite(value)
+            o, bound = ref.attention(part(q, qb, h), part(k, kb, g), value.masked_fill(bad, 0.0), scale, seen, dtype, True)
+            check_reached(got[qb[s]:qb[s + 1], h * D:h * D + D], o, bound, seen.double() @ bad.double() > 0, f"sequence {s} head {h}")
+
+
+# ---- values that are not finite, in keys that every row sees --------------------------------------------------------
+
+SEEN = [  # rows, keys, sequences, Hq, Hkv, D, dtype, causal, elements between rows: each form with the value in the last keys, which do not fill their tile
+    (197, 197, 1, 3, 3, 64, F16, False, 0),
+    (197, 197, 1, 3, 3, 128, BF16, False, 0),
+    (197, 197, 1, 100, 1, 64, BF16, False, 0),
+    (197, 197, 1, 100, 1, 128, F16, False, 4),
+    (60, 60, 1, 2, 1, 96, BF16, False, 0),
+    (70, 133, 1, 2, 1, 256, F16, False, 0),
+    (70, 133, 1, 2, 1, 256, BF16, False, 4),
+    (50, 50, 20, 8, 2, 64, F16, False, 0),
+    (50, 50, 20, 8, 2, 128, BF16, False, 4),
+    (30, 30, 40, 8, 4, 192, BF16, False, 0),
+    (1, 1, 1, 1, 1, 64, BF16, True, 0),
+    (1, 77, 1, 2, 2, 128, F16, True, 0),
+    (1, 77, 1, 2, 2, 128, BF16, True, 4),
+    (1, 1000, 1, 2, 1, 72, BF16, True, 0),
+    (33, 33, 20, 8, 2, 128, BF16, True, 0),
+    (33, 300, 1, 2, 1, 64, F16, True, 0),
+    (129, 129, 1, 2, 1, 64, BF16, True, 0),
+    (129, 150, 1, 2, 1, 128, F16, True, 4),
+    (129, 170, 1, 2, 2, 256, BF16, True, 0),
+    (33, 33, 20, 16, 2, 256, F16, True, 0),
+    (1, 17, 300, 2, 1, 256, F16, True, 0),
+]
+
+
+def seen_inputs(seed, n, m, S, Hq, Hkv, D, dtype):
+    q, k, v = (randn(seed + i, *s) for i, s in enumerate(((S * n, Hq * D), (S * m, Hkv * D), (S * m, Hkv * D))))
+    for s in range(S):                                             # in other columns of each sequence
+        last, c = (s + 1) * m - 1, 8 * (s % 4)
+        v[last, c + 1], v[last, c + 2], v[last, c + 4] = float("inf"), -float("inf"), float("nan")
+        v[s * m + m // 2, c + 5] = float("inf")
+    return (x.to(dtype) for x in (q, k, v))
+
+
+@pytest.mark.parametrize("case", SEEN, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
+def test_prompt_values_that_every_row_sees(nq, case):
+    n, m, S, Hq, Hkv, D, dtype, causal, gap = case
+    q, k, v = seen_inputs(500, n, m, S, Hq, Hkv, D, dtype)
+    q_begin, k_begin = begins([n] * S), begins([m] * S)
+    got = run_prompt(nq, q, k, v, q_begin, k_begin, S, Hq, Hkv, D, dtype, causal, 0.1, gap)[0].cpu()
+    check_seen(got, q, k, v, q_begin, k_begin, Hq, Hkv, D, dtype, causal, 0.1, {0, Hq - 1}, {0, S // 2, S - 1})
+
+
+@pytest.mark.parametrize("n,m,D,causal", [(1, 9001, 64, True), (33, 3000, 128, True), (40, 3001, 96, False), (100, 1500, 72, False), (129, 1100, 128, True), (70, 2060, 256, False),
+                                          (129, 1100, 192, True)])
+def test_prompt_dealt_values_that_every_row_sees(nq, n, m, D, causal):
+    q, k, v = seen_inputs(510, n, m, 1, 2, 1, D, BF16)
+    got = run_dealt(nq, q, k, v, begins([n]), begins([m]), 2, 1, D, BF16, causal, 0.1)
+    check_seen(got, q, k, v, begins([n]), begins([m]), 2, 1, D, BF16, causal, 0.1, {0, 1}, {0})
