@@ -502,12 +502,11 @@ __global__ void __launch_bounds__(256) k_attention_join(const TokenParams p)
         __syncthreads();
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[c] *= keep;
+        // (a piece without weight counts, too: 0 times an infinite or NaN value is no 0; a piece without any token holds zeros)
         auto add = [&](int i, const at_f4 &z) {
             const float v = weight[group][i];
-            if (v != 0.0f) {                                             // (what a piece without weight holds is not used; NaN is one)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) o[c] = fmaf(z[c], v, o[c]);
-            }
+            for (int c = 0; c < 4; ++c) o[c] = fmaf(z[c], v, o[c]);
         };
         if (mine < step) {
 #pragma unroll

@@ -90,3 +90,54 @@ def test_prompt_dealt_values_that_every_row_sees(nq, n, m, D, causal):
     q, k, v = seen_inputs(510, n, m, 1, 2, 1, D, BF16)
     got = run_dealt(nq, q, k, v, begins([n]), begins([m]), 2, 1, D, BF16, causal, 0.1)
     check_seen(got, q, k, v, begins([n]), begins([m]), 2, 1, D, BF16, causal, 0.1, {0, 1}, {0})
+
+
+def hidden_weight(c, n, what, cached):
+    """The first half of sequence 0's keys with scores some thousand below the others' or of -inf, a value of theirs with infinities and a NaN: the columns that are
+    not finite."""
+    slots = c.table[0, torch.arange(n) // c.page].long() * c.page + torch.arange(n) % c.page
+    at = (slots // c.page).cuda(), (slots % c.page).cuda()
+    first = torch.arange(n) < n // 2
+    k, v, ks, vs = c.tensors
+    x = torch.zeros(n, 1, c.D)
+    x[:, 0, 0] = torch.where(first, -float("inf") if what == "-inf" else -60.0, 60.0)
+    c.keys[0] = x.double()
+    token = n // 4                                                 # (in a piece without others, where there are pieces)
+    reached = torch.zeros(c.D, dtype=torch.bool)
+    if cached == E4M3:
+        k.view(torch.uint8)[at] = x.to(E4M3).view(torch.uint8).cuda()
+        ks[at] = 1.0
+        v.view(torch.uint8)[at[0][token], at[1][token], 0, 3] = 0x7f                        # NaN
+        reached[3] = True
+    else:
+        k[at] = x.to(cached).cuda()
+        for column, value in ((3, float("inf")), (4, -float("inf")), (6, float("nan"))):
+            v[at[0][token], at[1][token], 0, column] = value
+            reached[column] = True
+    c.values[0][token, 0, reached] = 0.0
+    c.q = torch.zeros_like(c.q)
+    c.q.view(-1, c.Hq, c.D)[:, :, 0] = 16.0
+    c.scale = 1.0
+    return reached
+
+
+@pytest.mark.parametrize("what", ["low", "-inf"])
+@pytest.mark.parametrize("dtype,cached", [(BF16, BF16), (F16, F16), (BF16, E4M3)])
+@pytest.mark.parametrize("lengths,D", [([2500], 64), ([1000], 128), ([3000, 40], 72), ([90], 64), ([1500] + [1] * 1030, 64), ([5000], 256)])
+def test_token_values_without_weight(nq, lengths, D, dtype, cached, what):
+    """A value that is not finite makes its column not finite however little weight its token has, in a sequence of one piece (short, or in a call of
+    more than 1024) as in one of many."""
+    if what == "-inf" and cached == E4M3:
+        cached_what = "low"                                        # (e4m3 has no infinities)
+    else:
+        cached_what = what
+    c = TokenCase(nq, lengths, None, 2, 1, D, dtype, cached, 16, "head", seed=520)
+    reached = hidden_weight(c, lengths[0], cached_what, cached)[None]
+    job = c.job()
+    assert (job.workspace_bytes > 0) == (lengths[0] > 128 and len(lengths) <= 1024)
+    nq.nq_attention_token(job)
+    got = c.out.cpu()
+    for h in range(2):
+        o, bound = ref.attention(c.q[:1, :D].double(), c.keys[0][:, 0], c.values[0][:, 0], 1.0, torch.ones(1, lengths[0], dtype=torch.bool), dtype, False)
+        check_reached(got[:1, h * D:(h + 1) * D], o, bound, reached, f"head {h}")
+    assert torch.isfinite(got[1:]).all()
