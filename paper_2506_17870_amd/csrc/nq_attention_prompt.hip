@@ -115,14 +115,15 @@ __device__ __forceinline__ Rows rows_of(const PromptParams &p, int w)
 {
     const int lane = threadIdx.x & 63;
     if (p.sequences > PR_PLANNED) {
-        // in the order of the sequences from the last on: tile t belongs to the last sequence s with begin / ROWS + s <= t
+        // in the order of the sequences from the last on: tile t belongs to the last sequence s with begin / ROWS + s <= t (begins in front of the rows: 0)
         const int t = p.tiles - 1 - w;
+        auto first_of = [&](int s) { return max(p.q_begin[s], 0) / ROWS + s; };      // (under 2^31: sequences are under 2^30)
         int lo = -1, hi = p.sequences;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((int64_t)(p.q_begin[mid] / ROWS) + mid <= t) lo = mid; else hi = mid;
+            if (first_of(mid) <= t) lo = mid; else hi = mid;
         }
-        return lo < 0 ? Rows{-1, 0} : Rows{lo, t - (p.q_begin[lo] / ROWS + lo)};
+        return lo < 0 ? Rows{-1, 0} : Rows{lo, t - first_of(lo)};
     }
     if (p.sequences == 1) {
         const int q0 = min(max(p.q_begin[0], 0), p.q_rows), n = (min(max(p.q_begin[1], q0), p.q_rows) - q0 + ROWS - 1) / ROWS;

@@ -141,3 +141,21 @@ def test_token_values_without_weight(nq, lengths, D, dtype, cached, what):
         o, bound = ref.attention(c.q[:1, :D].double(), c.keys[0][:, 0], c.values[0][:, 0], 1.0, torch.ones(1, lengths[0], dtype=torch.bool), dtype, False)
         check_reached(got[:1, h * D:(h + 1) * D], o, bound, reached, f"head {h}")
     assert torch.isfinite(got[1:]).all()
+
+
+# ---- begins outside the rows ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("Hq,D,keys,gap", [(1, 64, 200, 0), (1, 256, None, 4), (2, 128, 200, 0), (1, 256, 200, 0), (1, 64, 200, 4), (3, 64, None, 0)])
+@pytest.mark.parametrize("ahead", [[-200], [-700, -300, -200], [-2 ** 31]])
+def test_many_sequences_that_begin_outside(nq, ahead, Hq, D, keys, gap):
+    """More sequences than are ordered by their keys, the first ones beginning in front of the rows, the last ending behind them: what lies inside is right
+    in each row."""
+    S, T = 300, 599
+    inside = [300] + [300 + i for i in range(1, S - len(ahead))]
+    q_begin = torch.tensor(ahead + inside + [10 ** 9], dtype=torch.int32)
+    assert len(q_begin) == S + 1
+    K = keys * S if keys else T
+    k_begin = begins([keys] * S) if keys else None
+    q, k, v = (randn(540 + i, rows, Hq * D).to(BF16) for i, rows in enumerate((T, K, K)))
+    got = run_prompt(nq, q, k, v, q_begin, k_begin, S, Hq, Hq, D, BF16, True, 0.1, gap)[0].cpu()
+    check_prompt(got, q, k, v, q_begin.clamp(0, T), k_begin, Hq, Hq, D, BF16, True, 0.1)
