@@ -42,14 +42,6 @@ struct BlockSum {
     }
 };
 
-// 1 / sqrt(x), the hardware's (good to a unit) also where x is too small for it.
-__device__ __forceinline__ float inverse_root(float x)
-{
-    const bool small = x < 0x1p-100f;
-    const float r = __builtin_amdgcn_rsqf(small ? x * 0x1p80f : x);
-    return small ? r * 0x1p40f : r;
-}
-
 // The weights and biases of a norm for a thread's columns: in registers for all its rows where it has eight columns, else read for
 // every row (they stay in the caches).
 template <int FIT, int CH>

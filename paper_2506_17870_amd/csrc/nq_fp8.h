@@ -218,6 +218,14 @@ __device__ __forceinline__ float sum64(float v)
     return (row(0) + row(16)) + (row(32) + row(48));
 }
 
+// 1 / sqrt(x), the hardware's (good to a unit) also where x is too small for it (a denormal, which it takes for 0).
+__device__ __forceinline__ float inverse_root(float x)
+{
+    const bool small = x < 0x1p-100f;
+    const float r = __builtin_amdgcn_rsqf(small ? x * 0x1p80f : x);
+    return small ? r * 0x1p40f : r;
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------
 
 inline int dtype_bytes(int dtype) { return dtype == NQ_DT_F32 ? 4 : 2; }

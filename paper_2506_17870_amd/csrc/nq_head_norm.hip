@@ -72,7 +72,7 @@ struct Turn {
     float cos[8], sin[8];                 // NEIGHBOURS: of the lane's four pairs; HALVES: of the pairs of its eight columns, the sine with its sign
 };
 
-// Norm over the head's values, which lie in LPH lanes.  The root's reciprocal is the hardware's, good to a unit.
+// Norm over the head's values, which lie in LPH lanes.
 template <int LPH>
 __device__ __forceinline__ void norm8(float (&v)[8], int kind, const float (&w)[8], const float *b, float eps, float inv_D, int c, bool in)
 {
@@ -88,7 +88,7 @@ __device__ __forceinline__ void norm8(float (&v)[8], int kind, const float (&w)[
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
-    const float r = __builtin_amdgcn_rsqf(sum_lanes<LPH>(sum) * inv_D + eps);
+    const float r = inverse_root(sum_lanes<LPH>(sum) * inv_D + eps);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = v[e] * r * w[e];
     if (b && in) {

@@ -159,3 +159,37 @@ def test_many_sequences_that_begin_outside(nq, ahead, Hq, D, keys, gap):
     q, k, v = (randn(540 + i, rows, Hq * D).to(BF16) for i, rows in enumerate((T, K, K)))
     got = run_prompt(nq, q, k, v, q_begin, k_begin, S, Hq, Hq, D, BF16, True, 0.1, gap)[0].cpu()
     check_prompt(got, q, k, v, q_begin.clamp(0, T), k_begin, Hq, Hq, D, BF16, True, 0.1)
+
+
+# ---- norms of small values ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 72, 128, 256])
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -140])
+def test_norms_of_small_values(nq, D, dtype, kind, eps):
+    """Heads whose squares are below the normal numbers, without anything to speak of added under the root: their norm is as any other's.
+    Off by what attention_reference.norm counts, and by the squares' lost bits: each of a head's D squares and additions, and the mean, are off by half a step of the
+    smallest value, 2^-150, so the mean by 2^-149 and its root's reciprocal by 2^-150 / mean of itself (and a little of second order)."""
+    T, H, page = 6, 3, 4
+    x = randn(560, T, H, D) * torch.tensor([1.0, 1e-15, 1e-18, 1e-19, 1e-20, 1e-21])[:, None, None]
+    x = x.to(dtype)
+    w, b = 1 + 0.2 * randn(561, D), 0.3 * randn(562, D) if kind == "layer" else None
+    norm = nq.make_norm(nq.NQ_NORM_LAYER if kind == "layer" else nq.NQ_NORM_RMS, eps, w.cuda(), b.cuda() if b is not None else None)
+    d = x.reshape(T, H * D).cuda()
+    q_out, k_out = (torch.full_like(d, 7.0) for _ in range(2))
+    cache = nq.KvCache(2, page, H, D, E4M3)
+    torch.cuda.synchronize()
+    nq.nq_head_norm(nq.make_head_norm(d, H * D, d, H * D, None, 0, dt(nq, dtype), H, H, D, norm, norm, None, 0, 0, None, q_out, H * D, k_out, H * D, cache.desc,
+                                      torch.arange(T).cuda()), T)
+    back = torch.empty(T, H * D, device="cuda")
+    nq.nq_cache_read(cache.desc, torch.arange(T).cuda(), T, back, H * D, None, 0, nq.NQ_DT_F32)
+    x = x.double()
+    y, off = ref.norm(kind, x, w.double(), None if b is None else b.double(), eps)
+    c = x - x.mean(-1, keepdim=True) if kind == "layer" else x
+    unbiased = y if b is None else y - b.double()
+    off = off + unbiased.abs() * 1.01 * 2.0 ** -150 / ((c * c).mean(-1, keepdim=True) + eps)
+    y, off, codes = y.reshape(T, -1), off.reshape(T, -1), ref.codes_bound(y, off).reshape(T, -1)
+    for out in (q_out, k_out):
+        ref.check(out, y, y.abs() * ref.half_step(dtype) * (1 + 2 ** -8) + 2 * off + ref.tiny(dtype))
+    ref.check(back, y, codes)
