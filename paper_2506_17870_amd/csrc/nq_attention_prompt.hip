@@ -284,6 +284,8 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
     asm("" : "+s"(partial));                                             // (one number, compared once a step: else the compiler compares twice, 3 % at 256 columns)
     uint32_t *const odd_of = reinterpret_cast<uint32_t *>(lds + (STAGES * 2 * TILE > SUMS / 2 ? STAGES * 2 * TILE : SUMS / 2));    // for each wave: whether it found such values
     if (lane == 0) odd_of[wave] = 0;
+    // (what is infinite or NaN of a pair of values, zeros for the rest)
+    auto not_finite = [&](uint32_t x) __attribute__((always_inline)) { return ((x & EXP) == EXP ? x & 0xffffu : 0u) | ((x >> 16 & EXP) == EXP ? x & 0xffff0000u : 0u); };
     auto tame = [&](uint4 &w) __attribute__((always_inline)) {
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
         uint32_t found = 0;
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
 #pragma unroll
         for (int i = 0; i < PER / 2; ++i) {
             const int at = (i * 64 + lane) / PER, d = k_piece<PITCH>(at, (i * 64 + lane) % PER) * 8;
-            const int q_off = first_row + at < Lq && d < p.D && !p.zero ? (int)(at * p.ldq + d) * 2 : NOWHERE;
+            const int q_off = first_row + at < Lq && d < p.D ? (int)(at * p.ldq + d) * 2 : NOWHERE;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_ptr)(own + i * 512), 16, q_off, 0, 0, 0);
         }
         __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));             // (this wave's alone: nobody else reads them)
@@ -352,8 +354,12 @@ __global__ void __launch_bounds__(waves_of(SHARE) * 64, DP > 128 ? 1 : SHARE == 
         for (int j = 0; j < KJ; ++j) {
             const int d = 16 * j + 8 * half;
             q[j] = make_uint4(0, 0, 0, 0);
-            if (row < Lq && d < p.D && !p.zero) __builtin_memcpy(&q[j], q_row + d, 16);
+            if (row < Lq && d < p.D) __builtin_memcpy(&q[j], q_row + d, 16);
         }
+    }
+    if (p.zero) {                                                        // (of queries times 0 those that are not finite are left; their scores are not either)
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) q[j] = make_uint4(not_finite(q[j].x), not_finite(q[j].y), not_finite(q[j].z), not_finite(q[j].w));
     }
     if (p.flip) {
 #pragma unroll

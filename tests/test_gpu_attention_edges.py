@@ -193,3 +193,41 @@ def test_norms_of_small_values(nq, D, dtype, kind, eps):
     for out in (q_out, k_out):
         ref.check(out, y, y.abs() * ref.half_step(dtype) * (1 + 2 ** -8) + 2 * off + ref.tiny(dtype))
     ref.check(back, y, codes)
+
+
+# ---- a scale of 0 ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,m,S,H,D,gap,dealt", [(40, 90, 1, 2, 136, 0, False), (150, 150, 1, 2, 128, 0, False), (150, 150, 1, 2, 64, 4, False), (30, 300, 1, 2, 64, 0, False),
+                                                 (20, 20, 40, 8, 128, 0, False), (20, 2000, 1, 2, 64, 0, True), (130, 2100, 1, 2, 128, 0, True)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_prompt_scale_of_zero(nq, dtype, n, m, S, H, D, gap, dealt):
+    """0 times a query that is not finite is NaN, and so are its scores and its row; the other rows are the mean of what they see."""
+    q, k, v = (randn(580 + i, rows, H * D) for i, rows in enumerate((S * n, S * m, S * m)))
+    q[3, 5], q[7, 6], q[11, 7] = float("inf"), -float("inf"), float("nan")
+    bad = torch.zeros(S * n, dtype=torch.bool)
+    bad[[3, 7, 11]] = True
+    q, k, v = (x.to(dtype) for x in (q, k, v))
+    q_begin, k_begin = begins([n] * S), begins([m] * S)
+    if dealt:
+        got = run_dealt(nq, q, k, v, q_begin, k_begin, H, H, D, dtype, True, 0.0)
+    else:
+        got = run_prompt(nq, q, k, v, q_begin, k_begin, S, H, H, D, dtype, True, 0.0, gap)[0].cpu()
+    assert torch.isnan(got[bad, :D]).all()
+    q[bad], got[bad, :D] = 0.0, 0.0
+    clean = check_prompt_rows(got, q, k, v, q_begin, k_begin, H, D, dtype)
+    assert clean == S * n * H - 3
+
+
+def check_prompt_rows(got, q, k, v, q_begin, k_begin, H, D, dtype):
+    """Each row but those of zeros against the mean; how many there were."""
+    count = 0
+    for s in range(len(q_begin) - 1):
+        a, b, c, d = (int(x) for x in (q_begin[s], q_begin[s + 1], k_begin[s], k_begin[s + 1]))
+        seen = torch.arange(d - c)[None] <= torch.arange(b - a)[:, None] + (d - c) - (b - a)
+        for h in range(H):
+            part = lambda x, i, j: x[i:j, h * D:(h + 1) * D].double()  # noqa: E731
+            o, bound = ref.attention(part(q, a, b), part(k, c, d), part(v, c, d), 0.0, seen, dtype, True)
+            rows = ~(got[a:b, h * D:(h + 1) * D] == 0).all(-1)
+            ref.check(got[a:b, h * D:(h + 1) * D][rows], o[rows], bound[rows], f"sequence {s} head {h}")
+            count += int(rows.sum())
+    return count
