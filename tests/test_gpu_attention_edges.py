@@ -231,3 +231,32 @@ def check_prompt_rows(got, q, k, v, q_begin, k_begin, H, D, dtype):
             ref.check(got[a:b, h * D:(h + 1) * D][rows], o[rows], bound[rows], f"sequence {s} head {h}")
             count += int(rows.sum())
     return count
+
+
+# ---- memory that another stream fills ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("cached", [BF16, E4M3])
+def test_a_new_cache_on_another_stream(nq, cached, raw):
+    """A cache made behind a busy stream and written on another at once holds what was written, zeros where nothing was."""
+    a, b = torch.ones(8192, 8192, dtype=BF16, device="cuda"), torch.empty(8192, 8192, dtype=BF16, device="cuda")
+    T, H, D, page, pages = 700, 8, 128, 16, 600
+    d, slot = randn(600, T, H * D).to(BF16).cuda(), torch.randperm(page * pages, generator=torch.Generator().manual_seed(1))[:T].cuda()
+    none, side = nq.make_norm(nq.NQ_NORM_NONE), torch.cuda.Stream()
+
+    def write(cache, stream):
+        nq.nq_head_norm(nq.make_head_norm(None, 0, d, H * D, d, H * D, nq.NQ_DT_BF16, H, H, D, none, none, None, 0, 0, None, None, 0, None, 0, cache.desc, slot), T, stream)
+
+    want = nq.KvCache(pages, page, H, D, cached)
+    torch.cuda.synchronize()
+    write(want, None)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        torch.mm(a, a, out=b)
+    got = nq.KvCache(pages, page, H, D, cached)
+    write(got, side.cuda_stream if raw else side)
+    torch.cuda.synchronize()
+    for x, y in zip((got.k, got.v, got.k_scale, got.v_scale), (want.k, want.v, want.k_scale, want.v_scale)):
+        if x is not None:
+            x, y = (t.view(torch.uint8) if t.dtype == E4M3 else t for t in (x, y))
+            assert torch.equal(x, y) and y.any()
