@@ -6,6 +6,7 @@ activations and outputs come from HBM, not from the Infinity Cache.
 """
 from __future__ import annotations
 
+import itertools
 import os
 import sys
 import time
@@ -733,7 +734,8 @@ def fp8():
 
 def attn():
     """The attention of a layer of 32 query and 8 key heads of 128 (bf16, e4m3 cache in pages of 16 tokens) on its operators: a prompt's heads, cache
-    and attention, the same prompt's rows back from the cache, and the next token of a batch of sequences of that length."""
+    and attention, the same prompt's rows back from the cache, and the next token of a batch of sequences of that length; then prompts and tokens of
+    other sizes against their floors."""
     Hq, Hkv, D, page, dt = 32, 8, 128, 16, nq.NQ_DT_BF16
     width = (Hq + 2 * Hkv) * D
     gen = torch.Generator(device="cuda").manual_seed(0)
@@ -771,6 +773,46 @@ def attn():
             us = wall_us(lambda: nq.nq_attention_token(job))
             cells.append(f"{us:.1f} | {2 * S * n * Hkv * size / us / 1e3:.0f}")
         print(f"| {S} | {n} | {' | '.join(cells)} |")
+
+    # floor: the larger of the bytes at a large copy's rate and the operations at a large product's
+    floor = lambda bytes_, flops: max(bytes_ / 5.06e6, flops / 1.2e9)  # noqa: E731
+    at = lambda lengths: torch.tensor([0, *itertools.accumulate(lengths)], dtype=torch.int32, device="cuda")  # noqa: E731
+    print("\n### causal prompts of other sizes, bf16, without and with a workspace (-: it takes none)\n")
+    print("| sequences | rows each | keys ahead of them | heads | columns | floor us | us | with a workspace us |")
+    print("|---|---|---|---|---|---|---|---|")
+    for S, n, ahead, H, Hk, d in ((256, 16, 0, 32, 8, 128), (1000, 0, 0, 32, 8, 128), (100, 60, 0, 32, 8, 128), (1, 16, 4000, 32, 8, 128), (1, 128, 4000, 32, 8, 128),
+                                  (1, 256, 4000, 32, 8, 128), (1, 16, 65536, 32, 8, 128), (1, 512, 32768, 32, 8, 128), (1, 16, 32768, 16, 4, 256),
+                                  (1, 2571, 0, 2, 2, 128), (1, 4096, 0, 16, 4, 192), (1, 4096, 0, 16, 4, 256)):
+        rows = [n or 1 + 3 * i % 5 for i in range(S)]
+        keys = [x + ahead for x in rows]
+        q, o, k, v = rand(sum(rows), H * d), rand(sum(rows), H * d), rand(sum(keys), Hk * d), rand(sum(keys), Hk * d)
+        cells = []
+        need = nq.nq_attention_prompt_workspace_bytes(S, sum(rows), sum(keys), H, Hk, d)
+        for workspace in (None, torch.empty(need, dtype=torch.uint8, device="cuda")):
+            if workspace is not None and need == 0:
+                cells.append("-")
+                continue
+            job = nq.make_attention_prompt(q, H * d, k, Hk * d, v, Hk * d, o, H * d, at(rows), at(keys), S, sum(rows), sum(keys), dt, H, Hk, d, True, d ** -0.5, workspace)
+            cells.append(f"{wall_us(lambda: nq.nq_attention_prompt(job)):.1f}")
+        pairs = sum(x * (x + 1) // 2 + x * ahead for x in rows)
+        print(f"| {S} | {n or 'up to 5'} | {ahead} | {H} / {Hk} | {d} | {floor(4 * d * (sum(rows) * H + sum(keys) * Hk), 4.0 * pairs * H * d):.1f} | {' | '.join(cells)} |")
+    print("\n### the next token, other widths and lengths\n")
+    print("| sequences | tokens | heads | columns | floor us bf16 | bf16 cache us | floor us e4m3 | e4m3 cache us |")
+    print("|---|---|---|---|---|---|---|---|")
+    for S, n, H, Hk, d, last in ((32, 2048, 16, 8, 64, 0), (32, 2048, 16, 8, 72, 0), (32, 2048, 16, 8, 80, 0), (32, 2048, 16, 8, 96, 0), (32, 2048, 16, 8, 128, 0),
+                                 (32, 2048, 16, 8, 192, 0), (32, 2048, 16, 8, 256, 0), (256, 208, 32, 8, 128, 65536), (1040, 208, 32, 8, 128, 16384)):
+        lengths = [n] * (S - 1) + [last or n]
+        pages, cells = [-(-x // page) for x in lengths], []
+        table, of = torch.full((S, max(pages)), -1, dtype=torch.int32), iter(torch.randperm(sum(pages), generator=torch.Generator().manual_seed(0)).tolist())
+        for i, x in enumerate(pages):
+            table[i, :x] = torch.tensor([next(of) for _ in range(x)], dtype=torch.int32)
+        for dtype, size in ((torch.bfloat16, 2 * d), (torch.float8_e4m3fn, d + 4)):
+            cache = nq.KvCache(sum(pages), page, Hk, d, dtype)
+            q, o, length = rand(S, H * d), rand(S, H * d), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+            workspace = torch.empty(nq.nq_attention_token_workspace_bytes(S, H, Hk, d, max(lengths)), dtype=torch.uint8, device="cuda")
+            job = nq.make_attention_token(q, H * d, o, H * d, cache.desc, table.cuda(), length, S, max(lengths), dt, H, d ** -0.5, workspace)
+            cells.append(f"{floor(2 * sum(lengths) * Hk * size + 4 * S * H * d, 0):.1f} | {wall_us(lambda: nq.nq_attention_token(job)):.1f}")
+        print(f"| {S} | {n}{f', one of {last}' if last else ''} | {H} / {Hk} | {d} | {' | '.join(cells)} |")
 
 
 if __name__ == "__main__":

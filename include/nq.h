@@ -570,7 +570,8 @@ nq_status nq_attention_prompt(const nq_prompt_job *job, void *stream);
  * the workspace: the nearer to the longest, the better), tokens of a page that the cache does not have (-1, say) are left out; ldtable *
  * page_tokens >= max_length.  At most 65535 sequences (NQ_ERR_SHAPE).  dtype: f16 or bf16; the cache e4m3 or of the same type
  * (NQ_ERR_UNSUPPORTED).
- * Sums, softmax and probabilities as exact as fp32 makes them; infinities and NaN as above.  A sequence's tokens are split over workgroups
+ * Sums and softmax in fp32.  Each probability goes into the second product as two parts of the cache's type (over an e4m3 cache bf16, times the value's
+ * scale), good to 2^-17 of it in bf16 and 2^-23 in f16; outputs rounded once.  Infinities and NaN as above.  A sequence's tokens are split over workgroups
  * (in calls of up to 1024 sequences) whose results the workspace holds until they are joined; how depends on all lengths of the call.  d_workspace: 16-byte aligned, of
  * nq_attention_token_workspace_bytes(sequences, q_heads, kv_heads, head_dim, max_length) or more (0: NULL will do); its
  * contents count only while the call runs, so calls that may run at the same time (on two streams, in two graphs) need one each. */

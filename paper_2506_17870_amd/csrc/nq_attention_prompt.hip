@@ -3,7 +3,8 @@
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(x_ij - m_i),  x_ij = scale log2(e) (q_i . k_j),  m_i the largest x so far
 //
 // Bound by the matrix core, by the exponentials next to it, and for long prompts by the card's power: 8192 causal rows of 32 heads of 128 bf16
-// take 524 us (1.05 PFLOP/s; the library's matrix product reaches 1.22), at 1.8 GHz with the matrix core busy 55 % of the time.  A workgroup takes
+// take 533 us (1.03 PFLOP/s, 518 to 546 us by the card's clock; the library's matrix product reaches 1.22), at 1.8 GHz with the matrix core busy 55 % of the
+// time.  A workgroup takes
 // 128 rows of a head, a wave 32 of them, and goes over the keys 64 (32) at a time (short calls: enum Share); two workgroups to a compute unit do one's exponentials
 // beside the other's products.  Both products are transposed: S^T = K Q^T, O^T = V^T P^T.  A lane then holds scores of
 // one row only, its maximum and sum need one exchange with another lane, and because the order in which a product sums its keys is

@@ -2,8 +2,8 @@
 //
 //   o = sum_j p_j v_j / sum_j p_j,  p_j = 2^(x_j - m),  x_j = scale log2(e) (q . k_j),  m the largest x so far
 //
-// Bound by the bytes of the cache's keys and values, each of which is read once, straight into registers in the matrix instructions'
-// operand order: S^T = K Q^T of 16 tokens x 32 columns x 16 query heads (those of one key head; a group of fewer leaves columns
+// Bound by the bytes of the cache's keys and values, each of which is read once (once for every 16 query heads of a group), straight into
+// registers in the matrix instructions' operand order: S^T = K Q^T of 16 tokens x 32 columns x 16 query heads (those of one key head; a group of fewer leaves columns
 // empty, which the matrix core has time for), then O^T = V^T P^T of 32 tokens.  The lane that holds four tokens' scores of a head
 // after the first product holds the same tokens' place in the second one's operand, because the order in which a product sums its
 // tokens is free: the probabilities never leave their registers, and a lane keeps the maximum and the sum of one head.
@@ -337,7 +337,8 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : workgroups_of(DP,
 #pragma unroll
             for (int c = 0; c < VC; ++c) o[c] *= alpha;
         }
-        // ---- probabilities, each as the sum of two parts of VT, which together have twice its bits; the matrix core has time for it
+        // ---- probabilities, each as the sum of two parts of VT, which together have twice its bits (off by 2^-17 of it for bf16, 2^-23 for f16); the
+        // matrix core has time for it
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
