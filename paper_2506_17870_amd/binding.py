@@ -774,7 +774,7 @@ def nq_attention_token(job: nq_token_job, stream=None):
 class KvCache:
     """Owner of the memory of one nq_kv_cache descriptor (memory plumbing only): empty pages, the tokens of a head in a page beside each other,
     the order in which nq_attention_token reads longest runs.  dtype: float16, bfloat16 or float8_e4m3fn.  The pages are filled when the
-    constructor returns (it waits for the current stream), so that any stream may write them; their memory belongs to the current stream, as that
+    constructor returns (it waits for the current stream; made in a capture, the graph fills them), so that any stream may write them; their memory belongs to the current stream, as that
     of any tensor made there: work on others has to be done, or recorded with the tensors, before the owner goes."""
 
     def __init__(self, pages, page_tokens, heads, head_dim, dtype=torch.float8_e4m3fn, device="cuda"):
@@ -783,7 +783,7 @@ class KvCache:
         self.k_scale = self.v_scale = None
         if dtype == torch.float8_e4m3fn:
             self.k_scale, self.v_scale = (torch.ones(pages, heads, page_tokens, device=device).transpose(1, 2) for _ in range(2))
-        if self.k.is_cuda:
+        if self.k.is_cuda and not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(self.k.device).synchronize()
         self.desc = make_kv_cache(self.k, self.v, self.k_scale, self.v_scale)
 

@@ -260,3 +260,31 @@ def test_a_new_cache_on_another_stream(nq, cached, raw):
         if x is not None:
             x, y = (t.view(torch.uint8) if t.dtype == E4M3 else t for t in (x, y))
             assert torch.equal(x, y) and y.any()
+
+
+def test_a_cache_made_in_a_capture(nq):
+    """There the graph fills the pages, each time, ahead of the captured calls that write them."""
+    T, H, D = 40, 2, 64
+    d, none, cache = randn(610, T, H * D).to(BF16).cuda(), nq.make_norm(nq.NQ_NORM_NONE), []
+    slot, back = torch.arange(T).cuda(), torch.zeros(2, T + 8, H * D, dtype=BF16, device="cuda")
+    rows = torch.arange(T + 8).cuda()
+
+    def work():
+        cache[:] = [nq.KvCache(3, 16, H, D, BF16)]
+        nq.nq_head_norm(nq.make_head_norm(None, 0, d, H * D, d, H * D, nq.NQ_DT_BF16, H, H, D, none, none, None, 0, 0, None, None, 0, None, 0, cache[0].desc, slot), T)
+        nq.nq_cache_read(cache[0].desc, rows, T + 8, back[0], H * D, back[1], H * D, nq.NQ_DT_BF16)
+
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for i in range(3):
+        back.fill_(9.0)
+        slot.copy_(torch.randperm(T + 8, generator=torch.Generator().manual_seed(i))[:T])
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.zeros(T + 8, H * D, dtype=BF16, device="cuda")
+        want[slot] = d
+        assert torch.equal(back[0], want) and torch.equal(back[1], want)
+        d.copy_(randn(611 + i, T, H * D))
